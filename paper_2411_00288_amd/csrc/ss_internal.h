@@ -58,6 +58,18 @@ inline size_t dense_size(const TileDims &t)
     return (size_t)kHeaderBytes + (size_t)t.Mt * t.Ks * 2048;
 }
 
+// Header of packed weights: its words travel as a kernel argument and are written by the packing kernel's first workgroup.
+constexpr int kHdrWords = kHdrFirstBad + 1;
+struct PackHeader {
+    uint32_t w[kHdrWords];
+};
+
+inline PackHeader pack_header(uint32_t magic, const ss_weight_desc *d, const TileDims &t)
+{
+    return {{magic, 1u, (uint32_t)d->cout, (uint32_t)d->cin, (uint32_t)d->kh, (uint32_t)d->kw, (uint32_t)d->dtype, (uint32_t)d->korder,
+             (uint32_t)t.Mt, (uint32_t)t.Ks, kNoBadBlock}};
+}
+
 // Compute units of the current device (cached per device), or -1 when the runtime cannot say.
 int compute_units();
 

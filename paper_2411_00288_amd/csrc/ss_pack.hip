@@ -11,20 +11,6 @@ namespace ss {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------------------------
-// header: its words travel as a kernel argument and are written by the packing kernel's first workgroup
-// ---------------------------------------------------------------------------------------------
-constexpr int kHdrWords = kHdrFirstBad + 1;
-struct PackHeader {
-    uint32_t w[kHdrWords];
-};
-
-static PackHeader pack_header(uint32_t magic, const ss_weight_desc *d, const TileDims &t)
-{
-    return {{magic, 1u, (uint32_t)d->cout, (uint32_t)d->cin, (uint32_t)d->kh, (uint32_t)d->kw, (uint32_t)d->dtype, (uint32_t)d->korder,
-             (uint32_t)t.Mt, (uint32_t)t.Ks, kNoBadBlock}};
-}
-
-// ---------------------------------------------------------------------------------------------
 // compressor
 //
 // Lane l of value tile (mt, ks) owns row 32*mt + l%32 and the four blocks 8*ks + {0,1,4,5} + 2*(l/32) of that row, i.e. the
