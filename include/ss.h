@@ -65,7 +65,8 @@ enum {
     SS_ERR_HIP         = -5  /* a HIP runtime call failed (launch error, no device, ...) */
 };
 
-enum { SS_F16 = 0, SS_BF16 = 1, SS_I8 = 2, SS_F8 = 3 /* OCP FP8 E4M3 (no infinities; S.1111.111 = NaN) */ };
+enum { SS_F16 = 0, SS_BF16 = 1, SS_I8 = 2, SS_F8 = 3 /* OCP FP8 E4M3 (no infinities; S.1111.111 = NaN) */,
+       SS_F32 = 4 /* activations of the norm and quantisation calls only */ };
 enum { SS_K_CRS = 0, SS_K_RSC = 1 };
 enum { SS_ACT_NONE = 0, SS_ACT_RELU = 1, SS_ACT_GELU = 2 };
 
@@ -422,6 +423,129 @@ int ss_maxpool2d(const void *x, int32_t N, int32_t H, int32_t Wd, int32_t C, int
 int ss_dwconv2d_fwd(const void *x, int32_t N, int32_t H, int32_t Wd, int32_t C, int32_t dtype, const void *w,
                     const float *bias, int32_t kh, int32_t kw, int32_t pad_h, int32_t pad_w, int32_t act,
                     void *y, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * MXFP4: the precision point below the 8-bit ones (OCP microscaling format with E2M1 elements).
+ *
+ * Blocks of 32 consecutive channels of a row share a scale 2^(byte - 127); an element is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  With m
+ * the block's largest magnitude the scale is 2^max(floor(log2 m) - 2, -127) and an element the value over the scale, rounded to nearest even,
+ * at most 6 in magnitude.  A block of zeros has the byte 0.  A NaN or an infinity in a block makes its byte 0xFF: all 32 stand for NaN.
+ *
+ * A quantised activation of `rows` rows (pixels, tokens) and `cols` channels, KB = ceil(cols/32):
+ *   codes   [rows][KB][16] bytes, two elements to the byte, the earlier one in the low four bits; channels past the last are zero.  16-byte aligned.
+ *   scales  [rows][4*ceil(KB/4)] bytes, those past the KB-th zero.  4-byte aligned.
+ * Rows of a 16- or 32-bit tensor may lie further apart than they are long (ld*, in elements), and begin at any element.  rows = 0 does nothing.
+ */
+
+/* x [rows][cols] (dtype SS_F16, SS_BF16 or SS_F32) -> codes, scales.  Asynchronous on `stream`. */
+int ss_mx4_quantize(const void *x, int64_t rows, int32_t cols, int64_t ldx, int32_t dtype, void *codes, void *scales, void *stream);
+
+/* What codes and scales stand for, rounded to dtype.  Asynchronous on `stream`. */
+int ss_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int32_t cols, int32_t dtype, void *y, int64_t ldy, void *stream);
+
+/*
+ * Size in bytes of the weights that ss_mx4_pack writes: with Mt = ceil(cout/32), KB = ceil(cin/32), Ks = ceil(KB/2) and Kq = ceil(Ks/4)
+ *   bytes [0, 256)  header as at ss_packed_bytes (magic 0x344D5353)
+ *   codes           Mt*Ks tiles of 64 lanes x 16 bytes: lane l of tile (mt, ks) holds block 2*ks + l/32 of row 32*mt + l%32
+ *   scales          Mt*Kq tiles of 64 uint32: byte j of lane l of tile (mt, q) is the scale of the same block of step 4*q + j
+ * Rows and blocks past the last are zero.  SS_ERR_UNSUPPORTED unless the kernel is 1x1 and the type SS_F16 or SS_BF16.
+ */
+int ss_mx4_packed_bytes(const ss_weight_desc *desc, size_t *packed_bytes /*[host] out*/);
+
+/*
+ * Quantises M (.) W [cout][cin] (blocks along cin) and lays it out for ss_pw_mx4_fwd.  M == NULL means all ones; a zero byte drops the weight, and
+ * the mask is not validated here (a 2:4 mask leaves 16 survivors to a block).  W is not changed.  packed: 16-byte aligned.  Asynchronous.
+ */
+int ss_mx4_pack(const ss_weight_desc *desc, const void *W, const uint8_t *M, void *packed, void *stream);
+
+/* The values that packed weights stand for, [cout][cin] in desc->dtype (rounded, should the type not hold them).  Asynchronous. */
+int ss_mx4_unpack(const ss_weight_desc *desc, const void *packed, void *W, void *stream);
+
+/*
+ * Pointwise (1x1) layer on MXFP4 operands, and the linear layer of a classifier:
+ *     y[r][o] = act( sum_c Wq[o][c] xq[r][c] + bias[o] + residual[r][o] )
+ * xq is x [rows][cin] (desc->dtype) quantised on the way, to the values of ss_mx4_quantize.  Sums are fp32; one rounding to desc->dtype at the store.
+ *   bias      [cout] fp32 or NULL
+ *   residual  [rows][cout] of desc->dtype or NULL; it may be y.
+ *   workspace ss_pw_mx4_workspace_bytes bytes, 16-byte aligned, not initialised (SS_ERR_WORKSPACE if it is short)
+ * Any cin and cout; rows from 0 to 2^31 - 1.  Asynchronous on `stream`.
+ */
+int ss_pw_mx4_workspace_bytes(const ss_weight_desc *desc, int64_t rows, size_t *bytes /*[host] out*/);
+int ss_pw_mx4_fwd(const ss_weight_desc *desc, const void *x, int64_t rows, int64_t ldx, const void *packed, const float *bias, const void *residual,
+                  int64_t ldr, int32_t act, void *y, int64_t ldy, void *workspace, size_t ws_bytes, void *stream);
+
+/* The same on an activation that is quantised already. */
+int ss_pw_mx4_q_fwd(const ss_weight_desc *desc, const void *codes, const void *scales, int64_t rows, const void *packed, const float *bias,
+                    const void *residual, int64_t ldr, int32_t act, void *y, int64_t ldy, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Norms before and after a block, with its gate, its residual scale and the residual sum, over the channels of each row:
+ *     u = post(h)        x_out = x + scale * gate * u        y = norm(x_out)
+ * LayerNorm: (v - mean) / sqrt(mean of squared differences + eps) * w + b.  RMS: v / sqrt(mean square + eps) * w + b.
+ * Statistics and sums are fp32, y is computed from x_out before its rounding, and x_out and y are rounded once each.
+ */
+enum { SS_NORM_NONE = 0, SS_NORM_LAYER = 1, SS_NORM_RMS = 2 };
+
+/* Plain data, passed by pointer [host]. */
+typedef struct {
+    int32_t cols;       /* channels, at most 16384 */
+    int32_t dtype;      /* SS_F16 | SS_BF16 | SS_F32: every activation of a call */
+    int32_t norm, post; /* SS_NORM_*, of y and of h */
+    float eps, post_eps;
+} ss_norm_desc;
+
+/* Operands of ss_norm_fwd: device pointers, pitches in elements, NULL where there is none.  x_out may be x or h, y may be h; rows begin at any element. */
+typedef struct {
+    int64_t rows;
+    int64_t groups;     /* rows of `gate`; rows r*rows/groups .. (r+1)*rows/groups - 1 share its row r.  Divides rows. */
+    int32_t gate_cols;  /* 1 (one factor for a row) or cols */
+    const void *x;
+    int64_t ldx;
+    const void *h;      /* the block's output; NULL: y = norm(x), and the fields from here to x_out are NULL */
+    int64_t ldh;
+    const void *gate;   /* [groups][gate_cols], contiguous, or NULL */
+    const float *scale, *post_w, *post_b; /* [cols] or NULL */
+    void *x_out;
+    int64_t ldx_out;
+    const float *w, *b; /* [cols] or NULL */
+    void *y;            /* NULL with SS_NORM_NONE, or where the result is quantised: */
+    int64_t ldy;
+    void *codes, *scales; /* y's MXFP4 form instead of y, quantised from fp32, or NULL */
+} ss_norm_io;
+
+/* Asynchronous on `stream`; no workspace. */
+int ss_norm_fwd(const ss_norm_desc *desc, const ss_norm_io *io /*[host]*/, void *stream);
+
+/*
+ * Gradient of ss_norm_fwd for a gradient dy of y and one, dx_out, of x_out (NULL: none; needed with SS_NORM_NONE).  Takes the forward pass's x_out
+ * (x where there was no h) and h; statistics are computed again.  dx is the gradient of x; dh, and dgate in the type and shape of gate, are
+ * needed where there is an h and a gate, the fp32 vectors only where they are not NULL.  Sums over rows are made in a fixed order: the
+ * same call gives the same bits.  dx may be dy or dx_out, dh may be h.  rows = 0 gives zero vectors.
+ *   workspace  ss_norm_bwd_workspace_bytes bytes (gate_cols 0: no gate), 16-byte aligned, not initialised.  Asynchronous on `stream`.
+ */
+typedef struct {
+    int64_t rows, groups;
+    int32_t gate_cols;
+    const void *dy;
+    int64_t lddy;
+    const void *x_out;
+    int64_t ldx_out;
+    const void *dx_out;
+    int64_t lddx_out;
+    const void *h;
+    int64_t ldh;
+    const void *gate;
+    const float *w, *scale, *post_w, *post_b;
+    void *dx;
+    int64_t lddx;
+    void *dh;
+    int64_t lddh;
+    void *dgate;
+    float *dw, *db, *dscale, *dpost_w, *dpost_b;
+} ss_norm_grad_io;
+
+int ss_norm_bwd_workspace_bytes(const ss_norm_desc *desc, int64_t rows, int64_t groups, int32_t gate_cols, size_t *bytes /*[host] out*/);
+int ss_norm_bwd(const ss_norm_desc *desc, const ss_norm_grad_io *io /*[host]*/, void *workspace, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 from pathlib import Path
+from typing import NamedTuple
 
 import torch
 
@@ -21,22 +22,44 @@ LIB_PATH = _HERE / "libss.so"
 
 SS_OK = 0
 SS_ERR_INVALID_ARG, SS_ERR_BAD_MASK, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ERR_HIP = -1, -2, -3, -4, -5
-SS_F16, SS_BF16, SS_I8, SS_F8 = 0, 1, 2, 3
+SS_F16, SS_BF16, SS_I8, SS_F8, SS_F32 = 0, 1, 2, 3, 4
 SS_K_CRS, SS_K_RSC = 0, 1
 SS_ACT_NONE, SS_ACT_RELU, SS_ACT_GELU = 0, 1, 2
+SS_NORM_NONE, SS_NORM_LAYER, SS_NORM_RMS = 0, 1, 2
 
 EXPORTS = ["ss_status_string", "ss_packed_bytes", "ss_dense_bytes", "ss_mask_compress", "ss_mask_decompress",
            "ss_dense_pack", "ss_conv2d_workspace_bytes", "ss_conv2d_fwd", "ss_conv2d_dense_fwd",
            "ss_conv2d_res_fwd", "ss_conv2d_dense_res_fwd", "ss_mask_update_compress", "ss_maxpool2d", "ss_dwconv2d_fwd",
            "ss_conv2d_q8_fwd", "ss_conv2d_q8_dense_fwd", "ss_conv2d_pw_fused_fwd", "ss_conv2d_pw_fused_dense_fwd",
            "ss_weights_check", "ss_conv2d_fwd_static_ws", "ss_conv2d_pw_fused_query", "ss_conv2d_pw2_fused_fwd", "ss_conv2d_pw2_fused_dense_fwd",
-           "ss_conv2d_pw2_fused_query", "ss_conv2d_maxpool_dense_fwd", "ss_conv2d_maxpool_dense_query"]
+           "ss_conv2d_pw2_fused_query", "ss_conv2d_maxpool_dense_fwd", "ss_conv2d_maxpool_dense_query",
+           "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_packed_bytes", "ss_mx4_pack", "ss_mx4_unpack", "ss_pw_mx4_workspace_bytes",
+           "ss_pw_mx4_fwd", "ss_pw_mx4_q_fwd", "ss_norm_fwd", "ss_norm_bwd_workspace_bytes", "ss_norm_bwd"]
 DEBUG_EXPORTS = ["ss_debug_force_tile", "ss_debug_limit_blocks", "ss_debug_force_split", "ss_debug_issue_peak", "ss_debug_lds_bandwidth"]          # include/ss_debug.h: test hooks
 
 
 class ss_weight_desc(ctypes.Structure):
     _fields_ = [("cout", ctypes.c_int32), ("cin", ctypes.c_int32), ("kh", ctypes.c_int32), ("kw", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("korder", ctypes.c_int32)]
+
+
+class ss_norm_desc(ctypes.Structure):
+    _fields_ = [("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("post", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("post_eps", ctypes.c_float)]
+
+
+def _fields(text):
+    """Fields of a struct of ss.h: a name with "#" is an int32, with "=" an int64, any other a pointer."""
+    return [(n.rstrip("#="), ctypes.c_int32 if n.endswith("#") else ctypes.c_int64 if n.endswith("=") else ctypes.c_void_p) for n in text.split()]
+
+
+class ss_norm_io(ctypes.Structure):
+    _fields_ = _fields("rows= groups= gate_cols# x ldx= h ldh= gate scale post_w post_b x_out ldx_out= w b y ldy= codes scales")
+
+
+class ss_norm_grad_io(ctypes.Structure):
+    _fields_ = _fields("rows= groups= gate_cols# dy lddy= x_out ldx_out= dx_out lddx_out= h ldh= gate w scale post_w post_b dx lddx= dh lddh= "
+                       "dgate dw db dscale dpost_w dpost_b")
 
 
 class SSError(RuntimeError):
@@ -86,6 +109,18 @@ def _load() -> ctypes.CDLL:
     lib.ss_conv2d_maxpool_dense_fwd.argtypes = conv_args[:13] + [vp, vp]    # y, pooled, stream
     lib.ss_conv2d_maxpool_dense_query.argtypes = [dp] + [i32] * 8 + [ctypes.POINTER(i32)]
     lib.ss_conv2d_fwd_static_ws.argtypes = conv_args[:13] + [vp]            # no workspace pair
+    i64, nd = ctypes.c_int64, ctypes.POINTER(ss_norm_desc)
+    lib.ss_mx4_quantize.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp]
+    lib.ss_mx4_dequantize.argtypes = [vp, vp, i64, i32, i32, vp, i64, vp]
+    lib.ss_mx4_packed_bytes.argtypes = [dp, ctypes.POINTER(sz)]
+    lib.ss_mx4_pack.argtypes = [dp, vp, vp, vp, vp]
+    lib.ss_mx4_unpack.argtypes = [dp, vp, vp, vp]
+    lib.ss_pw_mx4_workspace_bytes.argtypes = [dp, i64, ctypes.POINTER(sz)]
+    lib.ss_pw_mx4_fwd.argtypes = [dp, vp, i64, i64, vp, vp, vp, i64, i32, vp, i64, vp, sz, vp]
+    lib.ss_pw_mx4_q_fwd.argtypes = [dp, vp, vp, i64, vp, vp, vp, i64, i32, vp, i64, vp]
+    lib.ss_norm_fwd.argtypes = [nd, ctypes.POINTER(ss_norm_io), vp]
+    lib.ss_norm_bwd_workspace_bytes.argtypes = [nd, i64, i64, i32, ctypes.POINTER(sz)]
+    lib.ss_norm_bwd.argtypes = [nd, ctypes.POINTER(ss_norm_grad_io), vp, sz, vp]
     lib.ss_debug_force_tile.argtypes = [i32]
     lib.ss_debug_limit_blocks.argtypes = [i32]
     lib.ss_debug_force_split.argtypes = [i32]
@@ -720,3 +755,338 @@ def ss_dwconv2d_fwd(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None 
     if st != SS_OK:
         raise SSError(st, "ss_dwconv2d_fwd")
     return y
+
+
+# --------------------------------------------------------------------------------------------
+# Rows of channels (pixels, tokens): MXFP4 and the norms around a block
+# --------------------------------------------------------------------------------------------
+_ROW_TYPES = {torch.float16: SS_F16, torch.bfloat16: SS_BF16, torch.float32: SS_F32}
+_ROW_DTYPES = {code: dtype for dtype, code in _ROW_TYPES.items()}
+
+
+def _pitch(t, what, name):
+    """(rows, pitch) of a tensor of rows: the last dimension is dense, and the others step through memory as one."""
+    rows, ld = 1, 0
+    if t.dim() == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: the channels of {name} must be contiguous")
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if rows == 1:
+            ld = stride
+        elif size and stride != ld * rows:
+            raise SSError(SS_ERR_INVALID_ARG, f"{what}: the rows of {name} must be evenly spaced")
+        rows *= size
+    return rows, ld if rows > 1 else t.shape[-1]
+
+
+def _row_tensor(what, name, t, cols, dtype, rows=None):
+    """Checks a tensor of rows; (address, rows, pitch)."""
+    if t is None:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} is None")
+    if not t.is_cuda:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} must live in device memory")
+    if t.dim() == 0 or t.shape[-1] != cols or (dtype is not None and t.dtype != dtype) or t.dtype not in _ROW_TYPES:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} must be [..., {cols}] {dtype or 'float16, bfloat16 or float32'}")
+    n, ld = _pitch(t, what, name)
+    if rows is not None and n != rows:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} has {n} rows, not {rows}")
+    return ctypes.c_void_p(t.data_ptr()), n, ld
+
+
+def _channel_vector(what, name, t, cols):
+    if t is not None and t.numel() != cols:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} holds {t.numel()} values, not {cols}")
+    return _dev_ptr(t, f"{what}: {name}", (torch.float32,), allow_none=True)
+
+
+def _byte_tensor(what, name, t, rows, cols):
+    """Codes or scales of a quantised activation: whole, 8-bit, dense."""
+    p = _dev_ptr(t, f"{what}: {name}", (torch.uint8,))
+    if t.dim() == 0 or t.shape[-1] != cols or (rows is not None and t.numel() != rows * cols):
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} must be [..., {cols}] uint8" + ("" if rows is None else f" of {rows} rows"))
+    return p
+
+
+def _mx4_sizes(cols):
+    """Bytes of a row's codes and scales."""
+    blocks = (cols + 31) // 32
+    return 16 * blocks, (blocks + 3) // 4 * 4
+
+
+def _on(stream, device):
+    """Allocations made inside belong to the stream that the call is enqueued on."""
+    return torch.cuda.stream(torch.cuda.current_stream(device) if stream is None else stream)
+
+
+def ss_mx4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
+    """x [..., cols] float16, bfloat16 or float32 -> (codes [..., 16*ceil(cols/32)], scales [..., 4*ceil(cols/128)]) uint8 (include/ss.h, MXFP4)."""
+    if stream is None:
+        r = _native.mx4_quantize(x, codes, scales)
+        if r is not None:
+            return r if type(r[0]) is not int else _failed(r, "ss_mx4_quantize")
+    what = "ss_mx4_quantize"
+    if x is None or x.dim() == 0 or x.shape[-1] == 0:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: x must be [..., cols]")
+    cols = x.shape[-1]
+    px, rows, ld = _row_tensor(what, "x", x, cols, None)
+    nc, ns = _mx4_sizes(cols)
+    with _on(stream, x.device):
+        codes = torch.empty((*x.shape[:-1], nc), dtype=torch.uint8, device=x.device) if codes is None else codes
+        scales = torch.empty((*x.shape[:-1], ns), dtype=torch.uint8, device=x.device) if scales is None else scales
+    st = _lib.ss_mx4_quantize(px, rows, cols, ld, _ROW_TYPES[x.dtype], _byte_tensor(what, "codes", codes, rows, nc),
+                              _byte_tensor(what, "scales", scales, rows, ns), _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return codes, scales
+
+
+def ss_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, cols: int, dtype=torch.bfloat16, out: torch.Tensor | None = None,
+                      stream=None) -> torch.Tensor:
+    """The values [..., cols] that codes and scales stand for."""
+    if stream is None:
+        r = _native.mx4_dequantize(codes, scales, cols, _ROW_TYPES.get(dtype, -1), out)
+        if r is not None:
+            return r if type(r) is not tuple else _failed(r, "ss_mx4_dequantize")
+    what = "ss_mx4_dequantize"
+    if dtype not in _ROW_TYPES or cols <= 0:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: dtype {dtype}, {cols} channels")
+    nc, ns = _mx4_sizes(cols)
+    pc = _byte_tensor(what, "codes", codes, None, nc)
+    rows = codes.numel() // nc
+    ps = _byte_tensor(what, "scales", scales, rows, ns)
+    with _on(stream, codes.device):
+        out = torch.empty((*codes.shape[:-1], cols), dtype=dtype, device=codes.device) if out is None else out
+    po, _, ld = _row_tensor(what, "out", out, cols, dtype, rows)
+    st = _lib.ss_mx4_dequantize(pc, ps, rows, cols, _ROW_TYPES[dtype], po, ld, _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return out
+
+
+def ss_mx4_packed_bytes(desc: ss_weight_desc) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_mx4_packed_bytes(ctypes.byref(desc), ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_mx4_packed_bytes")
+    return int(out.value)
+
+
+def ss_mx4_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None = None, packed: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """W [cout, cin] 16-bit, M [cout, cin] uint8 or None -> the masked weights in MXFP4, laid out for ss_pw_mx4_fwd."""
+    what = "ss_mx4_pack"
+    need = ss_mx4_packed_bytes(desc)
+    if W is None or W.numel() != desc.cout * desc.cin or (M is not None and M.numel() != desc.cout * desc.cin):
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: W/M size does not match the descriptor")
+    pw, pm = _dev_ptr(W, "W", (torch_dtype(desc.dtype),)), _dev_ptr(M, "M", (torch.uint8, torch.bool), allow_none=True)
+    if packed is None:
+        with _on(stream, W.device):
+            packed = torch.empty(need, dtype=torch.uint8, device=W.device)
+    elif _nbytes(packed) < need:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: packed buffer too small")
+    st = _lib.ss_mx4_pack(ctypes.byref(desc), pw, pm, _dev_ptr(packed, "packed"), _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return packed
+
+
+def ss_mx4_unpack(desc: ss_weight_desc, packed: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The values [cout, cin] that packed weights stand for."""
+    what = "ss_mx4_unpack"
+    if _nbytes(packed) < ss_mx4_packed_bytes(desc):
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: packed buffer too small")
+    if out is None:
+        with _on(stream, packed.device):
+            out = torch.empty((desc.cout, desc.cin), dtype=torch_dtype(desc.dtype), device=packed.device)
+    elif out.numel() != desc.cout * desc.cin:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: out does not match the descriptor")
+    st = _lib.ss_mx4_unpack(ctypes.byref(desc), _dev_ptr(packed, "packed"), _dev_ptr(out, "out", (torch_dtype(desc.dtype),)), _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return out
+
+
+def ss_pw_mx4_workspace_bytes(desc: ss_weight_desc, rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_pw_mx4_workspace_bytes(ctypes.byref(desc), rows, ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_pw_mx4_workspace_bytes")
+    return int(out.value)
+
+
+def _pw_mx4(what, desc, head, rows, lead, device, packed, bias, residual, act, y, workspace, stream):
+    """Checks and makes a pointwise MXFP4 call; `head` is its activation's arguments, `lead` the leading dimensions of y."""
+    if _nbytes(packed) < ss_mx4_packed_bytes(desc):
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: weight buffer holds {_nbytes(packed)} bytes, the descriptor needs {ss_mx4_packed_bytes(desc)}")
+    dtype = torch_dtype(desc.dtype)
+    pb = _channel_vector(what, "bias", bias, desc.cout)
+    pr, ldr = None, 0
+    if residual is not None:
+        pr, _, ldr = _row_tensor(what, "residual", residual, desc.cout, dtype, rows)
+    with _on(stream, device):
+        if y is None:
+            y = torch.empty((*lead, desc.cout), dtype=dtype, device=device)
+        py, _, ldy = _row_tensor(what, "y", y, desc.cout, dtype, rows)
+        args = (ctypes.byref(desc), *head, _dev_ptr(packed, "packed"), pb, pr, ldr, act, py, ldy)
+        if what == "ss_pw_mx4_fwd":
+            need = ss_pw_mx4_workspace_bytes(desc, rows)
+            if need > 0 and workspace is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            st = _lib.ss_pw_mx4_fwd(*args, _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))
+        else:
+            st = _lib.ss_pw_mx4_q_fwd(*args, _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return y
+
+
+def ss_pw_mx4_fwd(desc: ss_weight_desc, x: torch.Tensor, packed: torch.Tensor, bias=None, residual=None, act=SS_ACT_NONE, y=None, workspace=None,
+                  stream=None) -> torch.Tensor:
+    """Pointwise layer on MXFP4 operands: x [..., cin] 16-bit, quantised on the way -> y [..., cout]."""
+    if stream is None:
+        r = _native.pw_mx4(desc, x, None, packed, bias, residual, act, y, workspace)
+        if r is not None:
+            return r if type(r) is not tuple else _failed(r, "ss_pw_mx4_fwd")
+    what = "ss_pw_mx4_fwd"
+    px, rows, ld = _row_tensor(what, "x", x, desc.cin, torch_dtype(desc.dtype))
+    return _pw_mx4(what, desc, (px, rows, ld), rows, x.shape[:-1], x.device, packed, bias, residual, act, y, workspace, stream)
+
+
+def ss_pw_mx4_q_fwd(desc: ss_weight_desc, codes: torch.Tensor, scales: torch.Tensor, packed: torch.Tensor, bias=None, residual=None, act=SS_ACT_NONE,
+                    y=None, stream=None) -> torch.Tensor:
+    """The same on an activation that ss_mx4_quantize (or ss_norm_mx4_fwd) has quantised: [..., cin] as codes and scales -> y [..., cout]."""
+    if stream is None:
+        r = _native.pw_mx4(desc, codes, scales, packed, bias, residual, act, y, None)
+        if r is not None:
+            return r if type(r) is not tuple else _failed(r, "ss_pw_mx4_q_fwd")
+    what = "ss_pw_mx4_q_fwd"
+    nc, ns = _mx4_sizes(desc.cin)
+    pc = _byte_tensor(what, "codes", codes, None, nc)
+    rows = codes.numel() // nc
+    return _pw_mx4(what, desc, (pc, _byte_tensor(what, "scales", scales, rows, ns), rows), rows, codes.shape[:-1], codes.device, packed, bias, residual, act,
+                   y, None, stream)
+
+
+def make_norm_desc(cols, dtype=SS_BF16, norm=SS_NORM_LAYER, eps=1e-6, post=SS_NORM_NONE, post_eps=1e-6) -> ss_norm_desc:
+    """The norm of a block's input, and the one of its output (`post`); dtype: of every activation."""
+    return ss_norm_desc(int(cols), int(dtype), int(norm), int(post), float(eps), float(post_eps))
+
+
+def _norm_io(what, io, desc, lead, rows, gate, vectors, tensors):
+    """Fills a struct of ss.h: the gate, the channel vectors and the tensors of rows, by their names."""
+    dtype = _ROW_DTYPES.get(desc.dtype)
+    io.rows = rows
+    if gate is not None:
+        if gate.dtype != dtype or gate.dim() == 0 or gate.shape[-1] not in (1, desc.cols):
+            raise SSError(SS_ERR_INVALID_ARG, f"{what}: gate must be [..., 1] or [..., {desc.cols}] {dtype}")
+        io.gate_cols = gate.shape[-1]
+        io.groups = gate.numel() // io.gate_cols
+        io.gate = _dev_ptr(gate, f"{what}: gate")
+    for name, t in vectors.items():
+        setattr(io, name, _channel_vector(what, name, t, desc.cols))
+    for name, t in tensors.items():
+        if t is not None:
+            p, _, ld = _row_tensor(what, name, t, desc.cols, dtype, rows)
+            setattr(io, name, p)
+            setattr(io, f"ld{name}", ld)
+
+
+def _norm_fwd(what, desc, x, w, b, h, scale, gate, post_w, post_b, x_out, y, codes, scales, stream):
+    dtype = _ROW_DTYPES.get(desc.dtype)
+    _, rows, _ = _row_tensor(what, "x", x, desc.cols, dtype)
+    io = ss_norm_io()
+    quantised = what == "ss_norm_mx4_fwd"
+    with _on(stream, x.device):
+        if h is not None and x_out is None:
+            x_out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        if quantised:
+            nc, ns = _mx4_sizes(desc.cols)
+            codes = torch.empty((*x.shape[:-1], nc), dtype=torch.uint8, device=x.device) if codes is None else codes
+            scales = torch.empty((*x.shape[:-1], ns), dtype=torch.uint8, device=x.device) if scales is None else scales
+        elif y is None and desc.norm != SS_NORM_NONE:
+            y = torch.empty(x.shape, dtype=dtype, device=x.device)
+    _norm_io(what, io, desc, x.shape[:-1], rows, gate, {"w": w, "b": b, "scale": scale, "post_w": post_w, "post_b": post_b},
+             {"x": x, "h": h, "x_out": x_out, "y": y})
+    if quantised:
+        io.codes, io.scales = _byte_tensor(what, "codes", codes, rows, nc), _byte_tensor(what, "scales", scales, rows, ns)
+    # (an empty tensor has no address, by which the library tells an operand from none)
+    st = _lib.ss_norm_fwd(ctypes.byref(desc), ctypes.byref(io), _stream_ptr(stream)) if rows else SS_OK
+    if st != SS_OK:
+        raise SSError(st, what)
+    out = (codes, scales) if quantised else () if y is None else (y,)
+    out = out if h is None else (x_out, *out)
+    return out if len(out) > 1 else out[0]
+
+
+def ss_norm_fwd(desc: ss_norm_desc, x, w=None, b=None, h=None, scale=None, gate=None, post_w=None, post_b=None, x_out=None, y=None, stream=None):
+    """x_out = x + scale * gate * post(h), y = norm(x_out) -> (x_out, y); without a block output h: y = norm(x) -> y; with SS_NORM_NONE -> x_out.
+
+    x, h [..., cols]; w, b, scale, post_w, post_b [cols] float32; gate [groups, 1] or [groups, cols] of x's type, each of its rows for
+    rows / groups consecutive rows of x."""
+    if stream is None:
+        r = _native.norm_fwd(desc, x, w, b, h, scale, gate, post_w, post_b, x_out, y)
+        if r is not None:
+            return r if type(r) is not tuple or type(r[0]) is not int else _failed(r, "ss_norm_fwd")
+    return _norm_fwd("ss_norm_fwd", desc, x, w, b, h, scale, gate, post_w, post_b, x_out, y, None, None, stream)
+
+
+def ss_norm_mx4_fwd(desc: ss_norm_desc, x, w=None, b=None, h=None, scale=None, gate=None, post_w=None, post_b=None, x_out=None, codes=None, scales=None,
+                    stream=None):
+    """ss_norm_fwd with y in MXFP4: -> (x_out, codes, scales), or (codes, scales) without h."""
+    return _norm_fwd("ss_norm_mx4_fwd", desc, x, w, b, h, scale, gate, post_w, post_b, x_out, None, codes, scales, stream)
+
+
+class NormGrads(NamedTuple):
+    """Gradients of ss_norm_fwd; None where the call had no such operand."""
+    dx: torch.Tensor
+    dh: torch.Tensor | None
+    dgate: torch.Tensor | None
+    dw: torch.Tensor | None
+    db: torch.Tensor | None
+    dscale: torch.Tensor | None
+    dpost_w: torch.Tensor | None
+    dpost_b: torch.Tensor | None
+
+
+def ss_norm_bwd_workspace_bytes(desc: ss_norm_desc, rows: int, groups: int = 0, gate_cols: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_norm_bwd_workspace_bytes(ctypes.byref(desc), rows, groups, gate_cols, ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_norm_bwd_workspace_bytes")
+    return int(out.value)
+
+
+def ss_norm_bwd(desc: ss_norm_desc, dy, x_out, w=None, b=None, h=None, scale=None, gate=None, post_w=None, post_b=None, dx_out=None, workspace=None,
+                stream=None) -> NormGrads:
+    """Gradient of ss_norm_fwd.  dy: of y (None with SS_NORM_NONE); dx_out: of x_out, or None; x_out, h and the other operands as in the forward
+    call (x_out = its x where there was no h).  The gradient of a vector that is None is not returned."""
+    if stream is None:
+        r = _native.norm_bwd(desc, dy, x_out, w, b, h, scale, gate, post_w, post_b, dx_out, workspace)
+        if r is not None:
+            return NormGrads(*r) if len(r) == 8 else _failed(r, "ss_norm_bwd")
+    what = "ss_norm_bwd"
+    dtype = _ROW_DTYPES.get(desc.dtype)
+    like = x_out if desc.norm != SS_NORM_NONE else dx_out
+    _, rows, _ = _row_tensor(what, "x_out" if like is x_out else "dx_out", like, desc.cols, dtype)
+    io = ss_norm_grad_io()
+    with _on(stream, like.device):
+        dx = torch.empty(like.shape, dtype=dtype, device=like.device)
+        dh = None if h is None else torch.empty(h.shape, dtype=dtype, device=like.device)
+        dgate = None if gate is None else torch.empty(gate.shape, dtype=gate.dtype, device=like.device)
+        dw, db, dscale, dpost_w, dpost_b = (None if v is None else torch.empty(v.shape, dtype=torch.float32, device=like.device)
+                                            for v in (w, b, scale, post_w, post_b))
+        _norm_io(what, io, desc, like.shape[:-1], rows, gate,
+                 {"w": w, "scale": scale, "post_w": post_w, "post_b": post_b, "dw": dw, "db": db, "dscale": dscale, "dpost_w": dpost_w, "dpost_b": dpost_b},
+                 {"dy": dy, "x_out": x_out, "dx_out": dx_out, "h": h, "dx": dx, "dh": dh})
+        _channel_vector(what, "b", b, desc.cols)
+        if dgate is not None:
+            io.dgate = _dev_ptr(dgate, "dgate")
+        need = ss_norm_bwd_workspace_bytes(desc, rows, io.groups, io.gate_cols)
+        if rows == 0:                                        # sums over no rows
+            return NormGrads(dx, dh, dgate, *(None if v is None else v.zero_() for v in (dw, db, dscale, dpost_w, dpost_b)))
+        if need > 0 and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        st = _lib.ss_norm_bwd(ctypes.byref(desc), ctypes.byref(io), _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return NormGrads(dx, dh, dgate, dw, db, dscale, dpost_w, dpost_b)

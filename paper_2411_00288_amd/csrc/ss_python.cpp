@@ -17,6 +17,7 @@
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <initializer_list>
 #include <list>
 #include <mutex>
 #include <vector>
@@ -414,6 +415,318 @@ PyObject *pack(PyObject *const *a, Py_ssize_t n)
 }
 
 // ---------------------------------------------------------------------------------------------
+// rows of channels: MXFP4 and the norms around a block
+// ---------------------------------------------------------------------------------------------
+// A descriptor of the type with this name (both kinds are of one size).
+template <typename D>
+bool read_named(PyObject *o, const char *name, D *d)
+{
+    static_assert(sizeof(D) == sizeof(ss_weight_desc), "read_desc copies that many bytes");
+    return strcmp(Py_TYPE(o)->tp_name, name) == 0 && read_desc(o, reinterpret_cast<ss_weight_desc *>(d));
+}
+
+bool row_type(int32_t dtype, at::ScalarType *st)
+{
+    *st = dtype == SS_F16 ? at::kHalf : dtype == SS_BF16 ? at::kBFloat16 : at::kFloat;
+    return dtype == SS_F16 || dtype == SS_BF16 || dtype == SS_F32;
+}
+
+// A tensor of rows [..., cols]: channels dense, rows evenly spaced.
+struct Rows {
+    const at::Tensor *t = nullptr;
+    int64_t rows = 0, ld = 0;
+};
+
+bool read_rows(PyObject *o, Rows *r)
+{
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() == 0) return false;
+    const int64_t cols = t.size(-1);
+    if (cols <= 0 || cols > INT32_MAX || (cols > 1 && t.stride(-1) != 1)) return false;
+    int64_t rows = 1, ld = cols;
+    for (int64_t i = t.dim() - 2; i >= 0; i--) {
+        if (t.size(i) == 1) continue;
+        if (rows == 1)
+            ld = t.stride(i);
+        else if (t.stride(i) != ld * rows)
+            return false;
+        rows *= t.size(i);
+        if (rows == 0) return false;                       // (empty tensors take the other path)
+    }
+    *r = {&t, rows, rows > 1 ? ld : cols};
+    return true;
+}
+
+bool read_rows(PyObject *o, int64_t rows, int64_t cols, at::ScalarType st, Rows *r)
+{
+    return read_rows(o, r) && r->rows == rows && r->t->size(-1) == cols && r->t->scalar_type() == st;
+}
+
+// An optional fp32 vector of exactly n values.
+bool read_channels(PyObject *o, int64_t n, const float **p)
+{
+    if (!read_vector(o, n, p)) return false;
+    return o == Py_None || THPVariable_Unpack(o).numel() == n;
+}
+
+// A dense 8-bit tensor [..., cols] of `rows` rows: `o` when given, a new one with `like`'s leading dimensions otherwise.
+bool bytes_out(PyObject *o, const at::Tensor &like, int64_t rows, int64_t cols, at::Tensor *y)
+{
+    if (o == Py_None) {
+        auto shape = like.sizes().vec();
+        shape.back() = cols;
+        *y = at::detail::empty_cuda(shape, at::kByte, like.device(), c10::nullopt);
+        return true;
+    }
+    const at::Tensor *t = dev_tensor(o);
+    if (!t || t->scalar_type() != at::kByte || t->dim() == 0 || t->size(-1) != cols || t->numel() != rows * cols) return false;
+    *y = *t;
+    return true;
+}
+
+// An output of rows [..., cols]: as above.
+bool rows_out(PyObject *o, const at::Tensor &like, int64_t rows, int64_t cols, at::ScalarType st, at::Tensor *y, int64_t *ld)
+{
+    if (o == Py_None) {
+        auto shape = like.sizes().vec();
+        shape.back() = cols;
+        *y = at::detail::empty_cuda(shape, st, like.device(), c10::nullopt);
+        *ld = cols;
+        return true;
+    }
+    Rows r;
+    if (!read_rows(o, rows, cols, st, &r)) return false;
+    *y = *r.t;
+    *ld = r.ld;
+    return true;
+}
+
+int64_t mx4_code_bytes(int64_t cols) { return (cols + 31) / 32 * 16; }
+int64_t mx4_scale_bytes(int64_t cols) { return (cols + 127) / 128 * 4; }
+
+// A tuple of what calls gave; nullptr (with Python's error) if one failed.
+PyObject *give_all(std::initializer_list<PyObject *> items)
+{
+    PyObject *t = nullptr;
+    bool whole = true;
+    for (PyObject *i : items) whole = whole && i;
+    if (whole) t = PyTuple_New((Py_ssize_t)items.size());
+    Py_ssize_t k = 0;
+    for (PyObject *i : items) {
+        if (t)
+            PyTuple_SET_ITEM(t, k++, i);
+        else
+            Py_XDECREF(i);
+    }
+    return t;
+}
+
+// mx4_quantize(x, codes, scales) -> (codes, scales), (status, row, block) or None
+PyObject *mx4_quantize(PyObject *const *a, Py_ssize_t n)
+{
+    Rows x;
+    if (n != 3 || !read_rows(a[0], &x)) Py_RETURN_NONE;
+    const at::ScalarType st = x.t->scalar_type();
+    const int32_t dtype = st == at::kHalf ? SS_F16 : st == at::kBFloat16 ? SS_BF16 : st == at::kFloat ? SS_F32 : -1, cols = (int32_t)x.t->size(-1);
+    at::Tensor codes, scales;
+    if (dtype < 0 || !bytes_out(a[1], *x.t, x.rows, mx4_code_bytes(cols), &codes) || !bytes_out(a[2], *x.t, x.rows, mx4_scale_bytes(cols), &scales)) Py_RETURN_NONE;
+    const void *xp = x.t->const_data_ptr();
+    void *cp = codes.data_ptr(), *sp = scales.data_ptr();
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] { return ss_mx4_quantize(xp, x.rows, cols, x.ld, dtype, cp, sp, s); });
+    return status == SS_OK ? give_all({give(a[1], codes), give(a[2], scales)}) : refuse(status);
+}
+
+// mx4_dequantize(codes, scales, cols, dtype, out) -> out, (status, row, block) or None
+PyObject *mx4_dequantize(PyObject *const *a, Py_ssize_t n)
+{
+    int32_t cols, dtype;
+    at::ScalarType st;
+    if (n != 5 || !read_int(a[2], &cols) || cols <= 0 || !read_int(a[3], &dtype) || !row_type(dtype, &st)) Py_RETURN_NONE;
+    const at::Tensor *codes = dev_tensor(a[0]), *scales = dev_tensor(a[1]);
+    if (!codes || !scales || codes->scalar_type() != at::kByte || scales->scalar_type() != at::kByte || codes->dim() == 0 || scales->dim() == 0 ||
+        codes->size(-1) != mx4_code_bytes(cols) || scales->size(-1) != mx4_scale_bytes(cols) || codes->numel() == 0)
+        Py_RETURN_NONE;
+    const int64_t rows = codes->numel() / codes->size(-1);
+    if (scales->numel() != rows * scales->size(-1)) Py_RETURN_NONE;
+    at::Tensor y;
+    int64_t ld;
+    if (!rows_out(a[4], *codes, rows, cols, st, &y, &ld)) Py_RETURN_NONE;
+    const void *cp = codes->const_data_ptr(), *sp = scales->const_data_ptr();
+    void *yp = y.data_ptr();
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] { return ss_mx4_dequantize(cp, sp, rows, cols, dtype, yp, ld, s); });
+    return status == SS_OK ? give(a[4], y) : refuse(status);
+}
+
+// pw_mx4(desc, x | codes, None | scales, packed, bias, residual, act, y, workspace) -> y, (status, row, block) or None
+PyObject *pw_mx4(PyObject *const *a, Py_ssize_t n)
+{
+    ss_weight_desc d;
+    int32_t act;
+    size_t need = 0;
+    if (n != 9 || !read_named(a[0], "ss_weight_desc", &d) || !read_int(a[6], &act) || ss_mx4_packed_bytes(&d, &need) != SS_OK) Py_RETURN_NONE;
+    const at::Tensor *packed = dev_tensor(a[3]);
+    const float *bias;
+    if (!packed || packed->nbytes() < need || !read_channels(a[4], d.cout, &bias)) Py_RETURN_NONE;
+    const at::ScalarType st = d.dtype == SS_F16 ? at::kHalf : at::kBFloat16;
+    const bool quantised = a[2] != Py_None;
+    Rows x, residual;
+    const void *scales = nullptr;
+    if (quantised) {
+        const at::Tensor *c = dev_tensor(a[1]), *sc = dev_tensor(a[2]);
+        if (!c || !sc || c->scalar_type() != at::kByte || sc->scalar_type() != at::kByte || c->dim() == 0 || sc->dim() == 0 || c->numel() == 0 ||
+            c->size(-1) != mx4_code_bytes(d.cin) || sc->size(-1) != mx4_scale_bytes(d.cin))
+            Py_RETURN_NONE;
+        x = {c, c->numel() / c->size(-1), 0};
+        if (sc->numel() != x.rows * sc->size(-1)) Py_RETURN_NONE;
+        scales = sc->const_data_ptr();
+    } else if (!read_rows(a[1], &x) || x.t->size(-1) != d.cin || x.t->scalar_type() != st) {
+        Py_RETURN_NONE;
+    }
+    if (a[5] != Py_None && !read_rows(a[5], x.rows, d.cout, st, &residual)) Py_RETURN_NONE;
+    at::Tensor y, ws;
+    int64_t ldy;
+    if (!rows_out(a[7], *x.t, x.rows, d.cout, st, &y, &ldy)) Py_RETURN_NONE;
+    void *wsp = nullptr;
+    size_t ws_bytes = 0;
+    if (a[8] != Py_None) {
+        const at::Tensor *t = dev_tensor(a[8]);
+        if (!t) Py_RETURN_NONE;
+        wsp = t->data_ptr();
+        ws_bytes = t->nbytes();
+    } else if (!quantised) {
+        if (ss_pw_mx4_workspace_bytes(&d, x.rows, &ws_bytes) != SS_OK) Py_RETURN_NONE;
+        if (ws_bytes > 0) {
+            ws = at::detail::empty_cuda({(int64_t)ws_bytes}, at::kByte, x.t->device(), c10::nullopt);
+            wsp = ws.data_ptr();
+        }
+    }
+    const void *xp = x.t->const_data_ptr(), *wp = packed->const_data_ptr(), *rp = residual.t ? residual.t->const_data_ptr() : nullptr;
+    void *yp = y.data_ptr();
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] {
+        return quantised ? ss_pw_mx4_q_fwd(&d, xp, scales, x.rows, wp, bias, rp, residual.ld, act, yp, ldy, s)
+                         : ss_pw_mx4_fwd(&d, xp, x.rows, x.ld, wp, bias, rp, residual.ld, act, yp, ldy, wsp, ws_bytes, s);
+    });
+    return status == SS_OK ? give(a[7], y) : refuse(status);
+}
+
+// The gate of a norm call: [..., 1 or cols], dense, of the activations' type.
+bool read_gate(PyObject *o, int64_t cols, at::ScalarType st, const at::Tensor **t, int64_t *groups, int32_t *gate_cols)
+{
+    *t = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *g = dev_tensor(o);
+    if (!g || g->scalar_type() != st || g->dim() == 0 || g->numel() == 0 || (g->size(-1) != 1 && g->size(-1) != cols)) return false;
+    *t = g;
+    *gate_cols = (int32_t)g->size(-1);
+    *groups = g->numel() / g->size(-1);
+    return true;
+}
+
+// norm_fwd(desc, x, w, b, h, scale, gate, post_w, post_b, x_out, y) -> y, x_out, (x_out, y), (status, row, block) or None
+PyObject *norm_fwd(PyObject *const *a, Py_ssize_t n)
+{
+    ss_norm_desc d;
+    at::ScalarType st;
+    Rows x, h;
+    ss_norm_io io{};
+    if (n != 11 || !read_named(a[0], "ss_norm_desc", &d) || !row_type(d.dtype, &st) || !read_rows(a[1], &x) || x.t->size(-1) != d.cols ||
+        x.t->scalar_type() != st || !read_channels(a[2], d.cols, &io.w) || !read_channels(a[3], d.cols, &io.b) || !read_channels(a[5], d.cols, &io.scale) ||
+        !read_channels(a[7], d.cols, &io.post_w) || !read_channels(a[8], d.cols, &io.post_b))
+        Py_RETURN_NONE;
+    const at::Tensor *gate;
+    if ((a[4] != Py_None && !read_rows(a[4], x.rows, d.cols, st, &h)) || !read_gate(a[6], d.cols, st, &gate, &io.groups, &io.gate_cols)) Py_RETURN_NONE;
+    const bool norm = d.norm != SS_NORM_NONE;
+    if ((!h.t && a[9] != Py_None) || (!norm && (!h.t || a[10] != Py_None))) Py_RETURN_NONE;
+    at::Tensor x_out, y;
+    if (h.t && !rows_out(a[9], *x.t, x.rows, d.cols, st, &x_out, &io.ldx_out)) Py_RETURN_NONE;
+    if (norm && !rows_out(a[10], *x.t, x.rows, d.cols, st, &y, &io.ldy)) Py_RETURN_NONE;
+    io.rows = x.rows;
+    io.x = x.t->const_data_ptr();
+    io.ldx = x.ld;
+    io.h = h.t ? h.t->const_data_ptr() : nullptr;
+    io.ldh = h.ld;
+    io.gate = gate ? gate->const_data_ptr() : nullptr;
+    io.x_out = h.t ? x_out.data_ptr() : nullptr;
+    io.y = norm ? y.data_ptr() : nullptr;
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] { return ss_norm_fwd(&d, &io, s); });
+    if (status != SS_OK) return refuse(status);
+    if (!h.t) return give(a[10], y);
+    return norm ? give_all({give(a[9], x_out), give(a[10], y)}) : give(a[9], x_out);
+}
+
+// norm_bwd(desc, dy, x_out, w, b, h, scale, gate, post_w, post_b, dx_out, workspace)
+//     -> (dx, dh, dgate, dw, db, dscale, dpost_w, dpost_b), (status, row, block) or None
+PyObject *norm_bwd(PyObject *const *a, Py_ssize_t n)
+{
+    ss_norm_desc d;
+    at::ScalarType st;
+    Rows like, dy, x, h, dxo;
+    ss_norm_grad_io io{};
+    const float *b;
+    if (n != 12 || !read_named(a[0], "ss_norm_desc", &d) || !row_type(d.dtype, &st) || !read_channels(a[3], d.cols, &io.w) || !read_channels(a[4], d.cols, &b) ||
+        !read_channels(a[6], d.cols, &io.scale) || !read_channels(a[8], d.cols, &io.post_w) || !read_channels(a[9], d.cols, &io.post_b))
+        Py_RETURN_NONE;
+    const bool norm = d.norm != SS_NORM_NONE;
+    if (!read_rows(norm ? a[2] : a[10], &like) || like.t->size(-1) != d.cols || like.t->scalar_type() != st) Py_RETURN_NONE;
+    const int64_t rows = like.rows;
+    const at::Tensor *gate;
+    if ((norm ? !read_rows(a[1], rows, d.cols, st, &dy) || !read_rows(a[2], rows, d.cols, st, &x) : a[1] != Py_None) ||
+        (a[10] != Py_None && !read_rows(a[10], rows, d.cols, st, &dxo)) || (a[5] != Py_None && !read_rows(a[5], rows, d.cols, st, &h)) ||
+        !read_gate(a[7], d.cols, st, &gate, &io.groups, &io.gate_cols) || (!norm && (io.w || b)) || (!h.t && (gate || io.scale || io.post_w || io.post_b)) ||
+        (d.post == SS_NORM_NONE && (io.post_w || io.post_b)))
+        Py_RETURN_NONE;
+    size_t need = 0;
+    if (ss_norm_bwd_workspace_bytes(&d, rows, io.groups, io.gate_cols, &need) != SS_OK) Py_RETURN_NONE;
+    at::Tensor dx, dh, dgate, ws, vec[5];
+    int64_t ld;
+    if (!rows_out(Py_None, *like.t, rows, d.cols, st, &dx, &ld)) Py_RETURN_NONE;
+    if (h.t && !rows_out(Py_None, *h.t, rows, d.cols, st, &dh, &ld)) Py_RETURN_NONE;
+    if (gate) dgate = at::detail::empty_cuda(gate->sizes(), st, gate->device(), c10::nullopt);
+    float **grads[5] = {&io.dw, &io.db, &io.dscale, &io.dpost_w, &io.dpost_b};
+    PyObject *const of[5] = {a[3], a[4], a[6], a[8], a[9]};
+    for (int i = 0; i < 5; i++)
+        if (of[i] != Py_None) {
+            vec[i] = at::detail::empty_cuda(THPVariable_Unpack(of[i]).sizes(), at::kFloat, like.t->device(), c10::nullopt);
+            *grads[i] = static_cast<float *>(vec[i].data_ptr());
+        }
+    void *wsp;
+    size_t ws_bytes = need;
+    if (a[11] != Py_None) {
+        const at::Tensor *t = dev_tensor(a[11]);
+        if (!t) Py_RETURN_NONE;
+        wsp = t->data_ptr();
+        ws_bytes = t->nbytes();
+    } else {
+        ws = at::detail::empty_cuda({(int64_t)need}, at::kByte, like.t->device(), c10::nullopt);
+        wsp = ws.data_ptr();
+    }
+    const auto address_of = [](const Rows &r) { return r.t ? r.t->const_data_ptr() : nullptr; };
+    io.rows = rows;
+    io.dy = address_of(dy); io.lddy = dy.ld;
+    io.x_out = address_of(x); io.ldx_out = x.ld;
+    io.dx_out = address_of(dxo); io.lddx_out = dxo.ld;
+    io.h = address_of(h); io.ldh = h.ld;
+    io.gate = gate ? gate->const_data_ptr() : nullptr;
+    io.dx = dx.data_ptr(); io.lddx = d.cols;
+    io.dh = h.t ? dh.data_ptr() : nullptr; io.lddh = d.cols;
+    io.dgate = gate ? dgate.data_ptr() : nullptr;
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] { return ss_norm_bwd(&d, &io, wsp, ws_bytes, s); });
+    if (status != SS_OK) return refuse(status);
+    const auto made = [](const at::Tensor &t) {
+        if (t.defined()) return give(Py_None, t);
+        Py_INCREF(Py_None);
+        return Py_None;
+    };
+    return give_all({made(dx), made(dh), made(dgate), made(vec[0]), made(vec[1]), made(vec[2]), made(vec[3]), made(vec[4])});
+}
+
+// ---------------------------------------------------------------------------------------------
 // Prepared launches: the arguments of a call, marshalled once by the binding; calling the object enqueues it on torch's
 // current stream.
 // ---------------------------------------------------------------------------------------------
@@ -584,6 +897,11 @@ PyMethodDef methods[] = {
     {"maxpool", reinterpret_cast<PyCFunction>(entry<maxpool>), METH_FASTCALL, nullptr},
     {"dwconv", reinterpret_cast<PyCFunction>(entry<dwconv>), METH_FASTCALL, nullptr},
     {"pack", reinterpret_cast<PyCFunction>(entry<pack>), METH_FASTCALL, nullptr},
+    {"mx4_quantize", reinterpret_cast<PyCFunction>(entry<mx4_quantize>), METH_FASTCALL, nullptr},
+    {"mx4_dequantize", reinterpret_cast<PyCFunction>(entry<mx4_dequantize>), METH_FASTCALL, nullptr},
+    {"pw_mx4", reinterpret_cast<PyCFunction>(entry<pw_mx4>), METH_FASTCALL, nullptr},
+    {"norm_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd>), METH_FASTCALL, nullptr},
+    {"norm_bwd", reinterpret_cast<PyCFunction>(entry<norm_bwd>), METH_FASTCALL, nullptr},
     {"launch", launch, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

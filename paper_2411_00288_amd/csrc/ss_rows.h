@@ -1,0 +1,93 @@
+// Rows of channels-last activations in registers: runs of 8 channels of a row, 16- or 32-bit, at any address that is a multiple of
+// an element.  (Not a multiple of 16 bytes: an odd number of channels, or a view of a wider tensor.  gfx950 takes such 16-byte accesses as they
+// are, so there is one path for all of them.)
+#ifndef SS_ROWS_H_
+#define SS_ROWS_H_
+#include "ss_math.h"
+
+namespace ss {
+
+// (By value: __builtin_bit_cast of an element of a vector variable takes the vector's first one.)
+__device__ __forceinline__ float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ uint32_t as_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
+
+template <int DT> constexpr int item_bytes() { return DT == SS_F32 ? 4 : 2; }
+
+struct __attribute__((packed, aligned(2))) Vec16 { u32x4 v; };
+struct __attribute__((packed, aligned(4))) Vec32 { u32x4 v; };
+
+// One value of type DT at p.
+template <int DT>
+__device__ __forceinline__ float load1(const void *p)
+{
+    if constexpr (DT == SS_F32)
+        return *static_cast<const float *>(p);
+    else
+        return widen<DT>(*static_cast<const uint16_t *>(p));
+}
+
+template <int DT>
+__device__ __forceinline__ void store1(void *p, float v)
+{
+    if constexpr (DT == SS_F32)
+        *static_cast<float *>(p) = v;
+    else
+        *static_cast<uint16_t *>(p) = (uint16_t)cvt_pack2<DT>(v, 0.f);
+}
+
+// v[0..n) = p[0..n), the others `fill`; n <= 0: nothing is read.
+template <int DT>
+__device__ __forceinline__ void load8(const void *p, int n, float (&v)[8], float fill = 0.f)
+{
+    if (n >= 8) {
+        if constexpr (DT == SS_F32) {
+            const u32x4 a = static_cast<const Vec32 *>(p)[0].v, b = static_cast<const Vec32 *>(p)[1].v;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                v[e] = as_float(a[e]);
+                v[4 + e] = as_float(b[e]);
+            }
+        } else {
+            const u32x4 a = static_cast<const Vec16 *>(p)->v;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                v[2 * e] = widen<DT>((uint16_t)a[e]);
+                v[2 * e + 1] = DT == SS_BF16 ? as_float(a[e] & 0xFFFF0000u) : widen<DT>((uint16_t)(a[e] >> 16));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = e < n ? load1<DT>(static_cast<const char *>(p) + e * item_bytes<DT>()) : fill;
+    }
+}
+
+// p[0..n) = v[0..n), rounded to nearest even.
+template <int DT>
+__device__ __forceinline__ void store8(void *p, int n, const float (&v)[8])
+{
+    if (n >= 8) {
+        if constexpr (DT == SS_F32) {
+            u32x4 a, b;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                a[e] = as_bits(v[e]);
+                b[e] = as_bits(v[4 + e]);
+            }
+            static_cast<Vec32 *>(p)[0].v = a;
+            static_cast<Vec32 *>(p)[1].v = b;
+        } else {
+            u32x4 a;
+#pragma unroll
+            for (int e = 0; e < 4; e++) a[e] = cvt_pack2<DT>(v[2 * e], v[2 * e + 1]);
+            static_cast<Vec16 *>(p)->v = a;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (e < n) store1<DT>(static_cast<char *>(p) + e * item_bytes<DT>(), v[e]);
+    }
+}
+
+}  // namespace ss
+
+#endif
