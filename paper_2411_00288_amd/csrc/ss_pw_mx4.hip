@@ -1,8 +1,12 @@
 // Pointwise layer on MXFP4 operands: y = act(Wq xq + bias + residual).
 #include "ss_mx4.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace ss {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+struct __attribute__((packed, aligned(2))) Half16 { u32x2 v; };        // four 16-bit values
 
 struct PwArgs {
     const uint8_t *codes, *scales;         // quantised activation
@@ -24,42 +28,196 @@ __device__ __forceinline__ f32x16 mma_mx4(const u32x4 &a, const u32x4 &b, const 
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide_a, wide_b, c, 4, 4, SEL, (int)scale_a, SEL, (int)scale_b);
 }
 
-// A wave makes one 32 x 32 tile, straight from memory.
-template <int DT>
-__global__ __launch_bounds__(256) void pw_mx4_kernel(PwArgs p)
+constexpr int kChunk = 8;                                  // blocks of a reduction chunk: 256 channels, four steps, one scale word
+
+// A wave's MI x NI tiles of sums, finished and stored: bias, residual, activation, rounding, whole 16-byte runs where the channels allow it.
+template <int DT, int MI, int NI>
+__device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI][NI], int mt0, long long px0, int lane)
 {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, KB = (p.K + 31) / 32, S = (KB + 3) / 4 * 4, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4;
-    const int mt = blockIdx.y * 2 + wave / 2;
-    const long long px = ((long long)blockIdx.x * 2 + wave % 2) * 32 + lane % 32;
-    if (mt * 32 >= p.cout) return;
-    const bool in = px < p.P;
-    f32x16 acc = {};
-    for (int ks = 0; ks < Ks; ks++) {
-        const int b = 2 * ks + lane / 32;
-        const u32x4 wa = *reinterpret_cast<const u32x4 *>(p.w + (((size_t)mt * Ks + ks) * 64 + lane) * 16);
-        const uint32_t sa = p.w_scales[(((size_t)mt * Kq + ks / 4) * 64 + lane) * 4 + ks % 4];
-        u32x4 xb = {};
-        uint32_t sb = 0;
-        if (in && b < KB) {
-            xb = *reinterpret_cast<const u32x4 *>(p.codes + (px * KB + b) * 16);
-            sb = p.scales[px * S + b];
+    const int half = lane / 32;
+#pragma unroll
+    for (int i = 0; i < MI; i++) {
+        const int o0 = (mt0 + i) * 32;
+        if (o0 >= p.cout) return;
+        float bias[16];
+#pragma unroll
+        for (int v = 0; v < 16; v++) {
+            const int o = o0 + 8 * (v / 4) + 4 * half + v % 4;
+            bias[v] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
         }
-        acc = mma_mx4<0>(wa, xb, acc, sa, sb);
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+            __builtin_amdgcn_sched_barrier(0);
+            const long long px = px0 + j * 32 + lane % 32;
+            const bool in = px < p.P;
+            float z[16];
+#pragma unroll
+            for (int v = 0; v < 16; v++) z[v] = acc[i][j][v] + bias[v];
+            if (p.residual != nullptr && in) {
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const int o = o0 + 8 * q + 4 * half;
+                    const uint16_t *src = p.residual + px * p.ldr + o;
+                    if (o + 4 <= p.cout) {
+                        const u32x2 r = reinterpret_cast<const Half16 *>(src)->v;
+                        z[4 * q] += widen<DT>((uint16_t)r[0]);
+                        z[4 * q + 1] += widen<DT>((uint16_t)(r[0] >> 16));
+                        z[4 * q + 2] += widen<DT>((uint16_t)r[1]);
+                        z[4 * q + 3] += widen<DT>((uint16_t)(r[1] >> 16));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (o + e < p.cout) z[4 * q + e] += widen<DT>(src[e]);
+                    }
+                }
+            }
+            if (p.act == SS_ACT_RELU) {
+#pragma unroll
+                for (int v = 0; v < 16; v++) z[v] = floor_at(z[v], 0.f);
+            } else if (p.act == SS_ACT_GELU) {
+#pragma unroll
+                for (int v = 0; v < 16; v++) z[v] = gelu_cdf<DT>(z[v]);
+            }
+            // the two lanes of a pixel trade runs of four channels, so that each holds 16 in a row
+            uint32_t d[4][2];
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                d[q][0] = cvt_pack2<DT>(z[4 * q], z[4 * q + 1]);
+                d[q][1] = cvt_pack2<DT>(z[4 * q + 2], z[4 * q + 3]);
+            }
+            u32x4 run[2];
+#pragma unroll
+            for (int q = 0; q < 2; q++)
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const auto s = __builtin_amdgcn_permlane32_swap(d[q][e], d[q + 2][e], false, false);
+                    run[q][e] = s[0];
+                    run[q][2 + e] = s[1];
+                }
+            if (!in) continue;
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const int o = o0 + 16 * half + 8 * q;
+                uint16_t *dst = p.y + px * p.ldy + o;
+                if (o + 8 <= p.cout) {
+                    reinterpret_cast<Vec16 *>(dst)->v = run[q];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        if (o + e < p.cout) dst[e] = (uint16_t)(run[q][e / 2] >> (16 * (e % 2)));
+                }
+            }
+        }
     }
-    if (!in) return;
+}
+
+// Large products: four waves, MI x NI tiles of 32 x 32 each, make 64 MI output channels and 64 NI pixels.
+//   weights     straight from memory into registers, in the instruction's own order, three steps (of 64 reduction indices) ahead
+//   activation  256 channels at a time through two LDS buffers, filled from registers that were loaded a chunk earlier; 16-byte pieces trade
+//               places within their row so that neither the fill nor a wave's read of 32 rows meets a bank twice
+// A reduction past the last block meets zero scales on both sides; rows past the last read zeros from the buffer's end.
+template <int DT, int MI, int NI>
+__global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel(PwArgs p, int tiles_m, int tiles_n)
+{
+    constexpr int BN = 64 * NI, PIECES = BN * kChunk / 256;
+    __shared__ __attribute__((aligned(16))) uint8_t codes_s[2][BN * kChunk * 16];
+    __shared__ uint32_t scales_s[2][2][BN];                // [buffer][half][pixel]: the four steps' bytes
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int KB = (p.K + 31) / 32, S = (KB + 3) / 4 * 4, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
+    // An XCD (workgroups b, b + 8, ...) works on neighbouring tiles, in bands of eight tiles of channels: 32 of them in flight read 8 + 4 panels.
+    const int total = tiles_m * tiles_n, xcd = blockIdx.x % 8;
+    const int id = xcd * (total / 8) + min(xcd, total % 8) + blockIdx.x / 8;
+    const int band = id / (8 * tiles_n), band_m = min(8, tiles_m - band * 8), in_band = id - band * 8 * tiles_n;
+    const int tm = band * 8 + in_band % band_m, tn = in_band / band_m;
+    const int mt0 = tm * 2 * MI + __builtin_amdgcn_readfirstlane(wave / 2) * MI;
+    const long long row0 = (long long)tn * BN;
+    const unsigned pitch = (unsigned)KB * 16u;
+    const int rows = (int)min((long long)BN, p.P - row0);
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.codes) + row0 * pitch, 0, (int)(rows * pitch), 0x00020000);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.scales) + row0 * S, 0, rows * S, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 256, 0x00020000);
+    u32x4 piece[PIECES];
+    uint32_t ps[2];
+    auto fetch = [&](int q) {                               // chunk q of the activation, to registers
 #pragma unroll
-    for (int q = 0; q < 4; q++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int o = mt * 32 + 8 * q + 4 * (lane / 32) + e;
-            if (o >= p.cout) continue;
-            float v = acc[4 * q + e];
-            if (p.bias != nullptr) v += p.bias[o];
-            if (p.residual != nullptr) v += widen<DT>(p.residual[px * p.ldr + o]);
-            if (p.act == SS_ACT_RELU) v = floor_at(v, 0.f);
-            if (p.act == SS_ACT_GELU) v = gelu_cdf<DT>(v);
-            store1<DT>(p.y + px * p.ldy + o, v);
+        for (int i = 0; i < PIECES; i++) {
+            const int at = tid + 256 * i, row = at / 8, b = q * kChunk + at % 8;
+            piece[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)(row * pitch + b * 16), 0, 0));
         }
+#pragma unroll
+        for (int d = 0; d < 2; d++) {
+            const int b = q * kChunk + 4 * d;              // (past a row's scales: past the buffer's end, which reads zero)
+            ps[d] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, b < S ? tid * S + b : -4, 0, 0);
+        }
+    };
+    auto fill = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) {
+            const int at = tid + 256 * i, row = at / 8, b = at % 8;
+            *reinterpret_cast<u32x4 *>(codes_s[buf] + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16)) = piece[i];
+        }
+        if (BN >= 256 || tid < BN) {
+            scales_s[buf][0][tid] = __builtin_amdgcn_perm(ps[1], ps[0], 0x06040200u);
+            scales_s[buf][1][tid] = __builtin_amdgcn_perm(ps[1], ps[0], 0x07050301u);
+        }
+    };
+    u32x4 wa[4][MI];
+    uint32_t sa[MI], na[MI];
+    auto weights = [&](int ks, u32x4 (&to)[MI]) {
+        const int k = min(ks, Ks - 1);                     // (a step past the last has zero scales, a tile past the last is not stored)
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+            to[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (min(mt0 + i, Mt - 1) * Ks + k) * 1024, 0));
+    };
+    auto weight_scales = [&](int q, uint32_t (&to)[MI]) {
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+            to[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (min(mt0 + i, Mt - 1) * Kq + min(q, Kq - 1)) * 256, 0);
+    };
+    f32x16 acc[MI][NI] = {};
+    fetch(0);
+    weight_scales(0, sa);
+#pragma unroll
+    for (int s = 0; s < 3; s++) weights(s, wa[s]);
+    fill(0);
+    __syncthreads();
+    const int px0 = (wave % 2) * NI * 32, half = lane / 32;
+    // (no branches: the compiler moves matrix instructions behind one, away from their loads; what is fetched behind the last chunk is not used)
+    for (int q = 0; q < Kq; q++) {
+        const int buf = q & 1;
+        fetch(q + 1);
+        weight_scales(q + 1, na);
+        uint32_t sb[NI];
+#pragma unroll
+        for (int j = 0; j < NI; j++) sb[j] = scales_s[buf][half][px0 + j * 32 + lane % 32];
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            __builtin_amdgcn_sched_barrier(0);              // (loads stay in their step: moved ahead they take more registers than there are)
+            weights(q * 4 + s + 3, wa[(s + 3) % 4]);
+            u32x4 xb[NI];
+#pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const int row = px0 + j * 32 + lane % 32, b = 2 * s + half;
+                xb[j] = *reinterpret_cast<const u32x4 *>(codes_s[buf] + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16));
+            }
+#pragma unroll
+            for (int i = 0; i < MI; i++)
+#pragma unroll
+                for (int j = 0; j < NI; j++) {
+                    if (s == 0) acc[i][j] = mma_mx4<0>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
+                    if (s == 1) acc[i][j] = mma_mx4<1>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
+                    if (s == 2) acc[i][j] = mma_mx4<2>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
+                    if (s == 3) acc[i][j] = mma_mx4<3>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
+                }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        fill(buf ^ 1);
+#pragma unroll
+        for (int i = 0; i < MI; i++) sa[i] = na[i];
+        lds_barrier();
+    }
+    pw_store<DT, MI, NI>(p, acc, mt0, row0 + px0, lane);
 }
 
 namespace {
@@ -97,10 +255,23 @@ int product(const ss_weight_desc *d, const uint8_t *codes, const uint8_t *scales
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
-    const dim3 grid((unsigned)((rows + 63) / 64), (unsigned)((t.Mt + 1) / 2));
-    if (grid.y > 65535) return SS_ERR_UNSUPPORTED;
-    d->dtype == SS_F16 ? pw_mx4_kernel<SS_F16><<<grid, dim3(256), 0, s>>>(a) : pw_mx4_kernel<SS_BF16><<<grid, dim3(256), 0, s>>>(a);
-    return launched();
+    const auto go = [&](auto mi, auto ni) -> int {
+        constexpr int MI = decltype(mi)::value, NI = decltype(ni)::value;
+        const long long tm = (t.Mt + 2 * MI - 1) / (2 * MI), tn = (rows + 64 * NI - 1) / (64 * NI);
+        if (tm * tn > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
+        const dim3 grid((unsigned)(tm * tn)), block(256);
+        d->dtype == SS_F16 ? pw_mx4_tile_kernel<SS_F16, MI, NI><<<grid, block, 0, s>>>(a, (int)tm, (int)tn)
+                           : pw_mx4_tile_kernel<SS_BF16, MI, NI><<<grid, block, 0, s>>>(a, (int)tm, (int)tn);
+        return launched();
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    const long long cus = std::max(compute_units(), 1);
+    const auto tiles = [&](int mi, int ni) { return (long long)((t.Mt + 2 * mi - 1) / (2 * mi)) * ((rows + 64 * ni - 1) / (64 * ni)); };
+    if (tiles(4, 4) >= cus) return go(Four{}, Four{});
+    if (tiles(2, 2) >= cus) return go(Two{}, Two{});
+    return go(One{}, One{});
 }
 
 }  // namespace
