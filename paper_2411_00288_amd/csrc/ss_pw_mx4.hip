@@ -1,6 +1,8 @@
 // Pointwise layer on MXFP4 operands: y = act(Wq xq + bias + residual).
 #include "ss_mx4.h"
+#include "ss_conv_params.h"
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 namespace ss {
@@ -220,6 +222,236 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
     pw_store<DT, MI, NI>(p, acc, mt0, row0 + px0, lane);
 }
 
+// The product of step s of a scale word.
+template <int MI, int NI>
+__device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x4 (&b)[NI], f32x16 (&acc)[MI][NI], const uint32_t (&sa)[MI], const uint32_t (&sb)[NI])
+{
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+            if (s == 0) acc[i][j] = mma_mx4<0>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+            if (s == 1) acc[i][j] = mma_mx4<1>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+            if (s == 2) acc[i][j] = mma_mx4<2>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+            if (s == 3) acc[i][j] = mma_mx4<3>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+        }
+}
+
+// 16-bit input rows of a workgroup, quantised into LDS.  Block b of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
+// pieces, and with an odd `pad` the quads of a row's neighbouring blocks write to different banks.  The scale of b = 8 q + 2 s + half is byte s of word
+// (q * 2 + half) * pad + r, the four steps of a lane.  Blocks 0 .. 2 Ks - 1, rows 0 .. count - 1; what is past the matrix is zero.
+template <int DT, int THREADS, int U>
+__device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, int rows, int count, int K, int Ks, int pad, unsigned mul, unsigned sh, uint8_t *codes_s,
+                                              uint8_t *scales_s)
+{
+    const int runs = 8 * Ks, total = count * runs;
+    for (int base = 0; base < total; base += THREADS * U) {
+        float v[U][8];
+        int row[U], run[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int i = base + u * THREADS + (int)threadIdx.x;
+            row[u] = (int)(((unsigned long long)(unsigned)i * mul) >> sh);
+            run[u] = i - row[u] * runs;
+            load8<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int b = run[u] / 4;
+            const uint32_t byte = mx4_scale(quad_max(magnitude8(v[u])));
+            const uint32_t c = mx4_codes8(v[u], byte);
+            if (base + u * THREADS + (int)threadIdx.x >= total) continue;
+            *reinterpret_cast<uint32_t *>(codes_s + (b * pad + row[u]) * 16 + run[u] % 4 * 4) = c;
+            if (run[u] % 4 == 0) scales_s[((b / 8 * 2 + b % 2) * pad + row[u]) * 4 + b % 8 / 2] = (uint8_t)byte;
+        }
+    }
+}
+
+struct PwRowsArgs {
+    const uint16_t *x;
+    long long ldx;
+    unsigned mul, sh;                      // division by a row's runs, 8 Ks
+};
+
+// Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves walk down the output channels, 64 at a
+// time, the next chunk of weights on its way from the L2 while the current one is multiplied.  The input is read once, whatever the number of channels.
+template <int DT, int NT>
+__global__ __launch_bounds__(256, 2) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    constexpr int PX = 32 * NT, PAD = PX + 1;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
+    const long long row0 = (long long)blockIdx.x * PX;
+    uint8_t *const codes_s = smem, *const scales_s = smem + 2 * Ks * PAD * 16;
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 256, 0x00020000);
+    u32x4 wa[4][2], wn[4][2];
+    uint32_t sa[2], sn[2];
+    auto fetch = [&](int mt, int q) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int m = min(mt + i, Mt - 1);
+            sn[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (m * Kq + q) * 256, 0);
+#pragma unroll
+            for (int s = 0; s < 4; s++)
+                wn[s][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (m * Ks + min(q * 4 + s, Ks - 1)) * 1024, 0));
+        }
+    };
+    int mt = wave * 2, q = 0;
+    if (mt < Mt) fetch(mt, 0);
+    quantise_rows<DT, 256, 4>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
+    __syncthreads();
+    f32x16 acc[2][NT] = {};
+    while (mt < Mt) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            sa[i] = sn[i];
+#pragma unroll
+            for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
+        }
+        const bool done = q + 1 == Kq;
+        const int nmt = done ? mt + 8 : mt, nq = done ? 0 : q + 1;
+        fetch(min(nmt, Mt - 1), nq);
+        uint32_t sb[NT];
+#pragma unroll
+        for (int j = 0; j < NT; j++) sb[j] = *reinterpret_cast<const uint32_t *>(scales_s + ((q * 2 + half) * PAD + j * 32 + lane % 32) * 4);
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            if (q * 4 + s < Ks) {
+                u32x4 xb[NT];
+#pragma unroll
+                for (int j = 0; j < NT; j++) xb[j] = *reinterpret_cast<const u32x4 *>(codes_s + ((8 * q + 2 * s + half) * PAD + j * 32 + lane % 32) * 16);
+                step_mx4<2, NT>(s, wa[s], xb, acc, sa, sb);
+            }
+        }
+        if (done) {
+            pw_store<DT, 2, NT>(p, acc, mt, row0, lane);
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int j = 0; j < NT; j++) acc[i][j] = f32x16{};
+        }
+        mt = nmt;
+        q = nq;
+    }
+}
+
+// Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
+// the reduction and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first weights are on their way.
+template <int DT, int NW, int NI, bool QUANT>
+__global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArgs r)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    static_assert(!QUANT || NI == 1, "rows in LDS");
+    constexpr int U = NI == 4 ? 2 : 4;                     // steps whose operands are in flight together
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int KB = (p.K + 31) / 32, S = (KB + 3) / 4 * 4, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
+    const int mt = blockIdx.x % Mt;
+    const long long row0 = (long long)(blockIdx.x / Mt) * (32 * NI);
+    const int rows = (int)min((long long)(32 * NI), p.P - row0), pad = rows | 1;
+    const int per = (Ks + NW - 1) / NW, k0 = min(wave * per, Ks), k1 = min(k0 + per, Ks);
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w) + (size_t)mt * Ks * 1024, 0, Ks * 1024, 0x00020000);
+    const uint8_t *const ws = p.w_scales + (size_t)mt * Kq * 256 + lane * 4;
+    auto weights = [&](int k, u32x4 (&wa)[U], uint32_t (&sa)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {                      // (past the wave's share: past the buffer's end)
+            wa[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, k + u < k1 ? (k + u) * 1024 + lane * 16 : -16, 0, 0));
+            sa[u] = ws[(size_t)(min(k + u, Ks - 1) / 4) * 256 + min(k + u, Ks - 1) % 4];
+        }
+    };
+    u32x4 wa[U];
+    uint32_t sa[U];
+    weights(k0, wa, sa);
+    uint8_t *const scales_s = smem + 2 * Ks * pad * 16;
+    if constexpr (QUANT) {
+        quantise_rows<DT, NW * 64, 4>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
+        __syncthreads();
+    }
+    f32x16 acc[1][NI] = {};
+    int px[NI];
+#pragma unroll
+    for (int j = 0; j < NI; j++) px[j] = min(j * 32 + lane % 32, rows - 1);     // (lanes past the last row repeat it)
+    for (int k = k0; k < k1; k += U) {
+        u32x4 xb[U][NI], wn[U];
+        uint32_t sb[U][NI], sn[U];
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const int b = 2 * min(k + u, Ks - 1) + half;
+                if constexpr (QUANT) {
+                    xb[u][j] = *reinterpret_cast<const u32x4 *>(smem + (b * pad + px[j]) * 16);
+                    sb[u][j] = scales_s[((b / 8 * 2 + half) * pad + px[j]) * 4 + b % 8 / 2];
+                } else {
+                    const long long row = row0 + px[j];
+                    xb[u][j] = *reinterpret_cast<const u32x4 *>(p.codes + (row * KB + min(b, KB - 1)) * 16);
+                    sb[u][j] = b < KB ? p.scales[row * S + b] : 0u;
+                }
+            }
+        weights(k + U, wn, sn);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int j = 0; j < NI; j++) acc[0][j] = mma_mx4<0>(wa[u], xb[u][j], acc[0][j], k + u < k1 ? sa[u] : 0u, k + u < k1 ? sb[u][j] : 0u);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            wa[u] = wn[u];
+            sa[u] = sn[u];
+        }
+    }
+    // the waves' sums, 32 rows at a time: register v of lane l at (wave * 16 + v) * 65 + l, so that 32 channels of a row are 32 banks
+    float *const sums = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int j = 0; j < NI; j++) {
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < 16; v++) sums[(wave * 16 + v) * 65 + lane] = acc[0][j][v];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16 / NW; i++) {
+            const int at = i * NW * 64 + threadIdx.x, c = at % 32, row = j * 32 + at / 32, o = mt * 32 + c;
+            if (row >= rows || o >= p.cout) continue;
+            const int v = c / 8 * 4 + c % 4, l = c / 4 % 2 * 32 + at / 32;
+            float z = p.bias != nullptr ? p.bias[o] : 0.f;
+            if (p.residual != nullptr) z += widen<DT>(p.residual[(row0 + row) * p.ldr + o]);
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; w++) s += sums[(w * 16 + v) * 65 + l];
+            z += s;
+            if (p.act == SS_ACT_RELU) z = floor_at(z, 0.f);
+            if (p.act == SS_ACT_GELU) z = gelu_cdf<DT>(z);
+            store1<DT>(p.y + (row0 + row) * p.ldy + o, z);
+        }
+    }
+}
+
+// A kernel's shared memory may pass 64 KB once its limit is raised, which is done at its first such launch on a device.
+template <auto KERNEL>
+int allow_lds(size_t bytes)
+{
+    if (bytes <= 65536) return SS_OK;
+    static std::atomic<unsigned long long> done{0};
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return SS_ERR_HIP;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev >= 64 || !(done.load(std::memory_order_acquire) & bit)) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return SS_ERR_HIP;
+        if (dev < 64) done.fetch_or(bit, std::memory_order_release);
+    }
+    return SS_OK;
+}
+
+template <auto KERNEL>
+int launch_lds(long long blocks, int threads, size_t bytes, hipStream_t s, const PwArgs &a, const PwRowsArgs &r)
+{
+    if (blocks > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
+    const int st = allow_lds<KERNEL>(bytes);
+    if (st != SS_OK) return st;
+    KERNEL<<<dim3((unsigned)blocks), dim3(threads), bytes, s>>>(a, r);
+    return launched();
+}
+
 namespace {
 
 int check_pw(const ss_weight_desc *d, int64_t rows, const void *packed, const float *bias, const void *residual, int64_t ldr, int32_t act, void *y, int64_t ldy)
@@ -237,13 +469,10 @@ int check_pw(const ss_weight_desc *d, int64_t rows, const void *packed, const fl
 
 size_t codes_bytes(const Mx4Dims &t, int64_t rows) { return ((size_t)rows * t.KB * 16 + 255) / 256 * 256; }
 
-int product(const ss_weight_desc *d, const uint8_t *codes, const uint8_t *scales, int64_t rows, const void *packed, const float *bias, const void *residual, int64_t ldr,
-            int32_t act, void *y, int64_t ldy, hipStream_t s)
+PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const float *bias, const void *residual, int64_t ldr, int32_t act, void *y, int64_t ldy)
 {
     const Mx4Dims t = mx4_dims(d->cout, d->cin);
     PwArgs a{};
-    a.codes = codes;
-    a.scales = scales;
     a.w = static_cast<const uint8_t *>(packed) + kHeaderBytes;
     a.w_scales = a.w + (size_t)t.Mt * t.Ks * 1024;
     a.bias = bias;
@@ -255,23 +484,80 @@ int product(const ss_weight_desc *d, const uint8_t *codes, const uint8_t *scales
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
+    return a;
+}
+
+// LDS of the few-row kernel: its quantised rows, later the waves' sums.
+size_t few_lds(const Mx4Dims &t, int waves, int quantised_rows)
+{
+    const size_t pad = (size_t)(quantised_rows | 1), rows = quantised_rows ? (size_t)2 * t.Ks * pad * 16 + (size_t)t.Kq * 2 * pad * 4 : 0;
+    return std::max(rows, (size_t)waves * 16 * 65 * 4);
+}
+
+size_t rows_lds(const Mx4Dims &t, int px) { return (size_t)2 * t.Ks * (px + 1) * 16 + (size_t)t.Kq * 2 * (px + 1) * 4; }
+
+enum { KIND_TILE = 0, KIND_FEW, KIND_ROWS };
+
+// Which kernel takes a layer on 16-bit input: KIND_TILE stands for a quantisation of its own and the product on its codes.
+struct PwPlan {
+    int kind, px;
+};
+
+PwPlan plan16(const Mx4Dims &t, int64_t rows)
+{
+    if (rows <= 32 && few_lds(t, 16, (int)rows) <= 160 * 1024) return {KIND_FEW, 32};
+    if (rows_lds(t, 32) <= 80 * 1024) return {KIND_ROWS, rows >= 64 * 512 && rows_lds(t, 64) <= 40 * 1024 ? 64 : 32};
+    return {KIND_TILE, 0};
+}
+
+template <int DT>
+int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
+{
     const auto go = [&](auto mi, auto ni) -> int {
         constexpr int MI = decltype(mi)::value, NI = decltype(ni)::value;
-        const long long tm = (t.Mt + 2 * MI - 1) / (2 * MI), tn = (rows + 64 * NI - 1) / (64 * NI);
+        const long long tm = (t.Mt + 2 * MI - 1) / (2 * MI), tn = ((long long)a.P + 64 * NI - 1) / (64 * NI);
         if (tm * tn > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
-        const dim3 grid((unsigned)(tm * tn)), block(256);
-        d->dtype == SS_F16 ? pw_mx4_tile_kernel<SS_F16, MI, NI><<<grid, block, 0, s>>>(a, (int)tm, (int)tn)
-                           : pw_mx4_tile_kernel<SS_BF16, MI, NI><<<grid, block, 0, s>>>(a, (int)tm, (int)tn);
+        pw_mx4_tile_kernel<DT, MI, NI><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
         return launched();
     };
     using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;
     using Four = std::integral_constant<int, 4>;
     const long long cus = std::max(compute_units(), 1);
-    const auto tiles = [&](int mi, int ni) { return (long long)((t.Mt + 2 * mi - 1) / (2 * mi)) * ((rows + 64 * ni - 1) / (64 * ni)); };
+    const auto tiles = [&](int mi, int ni) { return (long long)((t.Mt + 2 * mi - 1) / (2 * mi)) * (((long long)a.P + 64 * ni - 1) / (64 * ni)); };
     if (tiles(4, 4) >= cus) return go(Four{}, Four{});
     if (tiles(2, 2) >= cus) return go(Two{}, Two{});
-    return go(One{}, One{});
+    if (tiles(1, 1) >= cus / 2) return go(One{}, One{});
+    const long long px = ((long long)a.P + 31) / 32;
+    const PwRowsArgs none{};
+    if (px * t.Mt <= cus || px == 1) {
+        if (t.Ks <= 16) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, false>>(px * t.Mt, 256, few_lds(t, 4, 0), s, a, none);
+        return launch_lds<pw_mx4_few_kernel<DT, 16, 1, false>>(px * t.Mt, 1024, few_lds(t, 16, 0), s, a, none);
+    }
+    if (t.Ks <= 16) return launch_lds<pw_mx4_few_kernel<DT, 4, 2, false>>((px + 1) / 2 * t.Mt, 256, few_lds(t, 4, 0), s, a, none);
+    return launch_lds<pw_mx4_few_kernel<DT, 16, 2, false>>((px + 1) / 2 * t.Mt, 1024, few_lds(t, 16, 0), s, a, none);
+}
+
+template <int DT>
+int product16(const PwArgs &a, const Mx4Dims &t, const PwPlan &plan, const void *x, int64_t ldx, hipStream_t s)
+{
+    PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0};
+    fast_div_setup((unsigned)t.Ks * 8u, &r.mul, &r.sh);
+    if (plan.kind == KIND_FEW) {
+        if (t.Ks <= 16) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
+        return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
+    }
+    const long long blocks = ((long long)a.P + plan.px - 1) / plan.px;
+    return plan.px == 64 ? launch_lds<pw_mx4_rows_kernel<DT, 2>>(blocks, 256, rows_lds(t, 64), s, a, r)
+                         : launch_lds<pw_mx4_rows_kernel<DT, 1>>(blocks, 256, rows_lds(t, 32), s, a, r);
+}
+
+int product(const ss_weight_desc *d, PwArgs a, const uint8_t *codes, const uint8_t *scales, hipStream_t s)
+{
+    const Mx4Dims t = mx4_dims(d->cout, d->cin);
+    a.codes = codes;
+    a.scales = scales;
+    return d->dtype == SS_F16 ? product_codes<SS_F16>(a, t, s) : product_codes<SS_BF16>(a, t, s);
 }
 
 }  // namespace
@@ -286,7 +572,7 @@ extern "C" int ss_pw_mx4_q_fwd(const ss_weight_desc *desc, const void *codes, co
     if (st != SS_OK) return st;
     if (rows == 0) return SS_OK;
     if (!codes || !scales || !aligned(codes, 16) || !aligned(scales, 4)) return SS_ERR_INVALID_ARG;
-    return product(desc, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), rows, packed, bias, residual, ldr, act, y, ldy,
+    return product(desc, pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy), static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales),
                    static_cast<hipStream_t>(stream));
 }
 
@@ -298,7 +584,7 @@ extern "C" int ss_pw_mx4_workspace_bytes(const ss_weight_desc *desc, int64_t row
     if (!bytes || rows < 0) return SS_ERR_INVALID_ARG;
     if (rows > INT32_MAX) return SS_ERR_UNSUPPORTED;
     const Mx4Dims t = mx4_dims(desc->cout, desc->cin);
-    *bytes = codes_bytes(t, rows) + (size_t)rows * t.S;
+    *bytes = plan16(t, rows).kind == KIND_TILE ? codes_bytes(t, rows) + (size_t)rows * t.S : 0;
     return SS_OK;
 }
 
@@ -316,8 +602,12 @@ extern "C" int ss_pw_mx4_fwd(const ss_weight_desc *desc, const void *x, int64_t 
     if (st != SS_OK) return st;
     if (need > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < need)) return SS_ERR_WORKSPACE;
     const Mx4Dims t = mx4_dims(desc->cout, desc->cin);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const PwArgs a = pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy);
+    const PwPlan plan = plan16(t, rows);
+    if (plan.kind != KIND_TILE) return desc->dtype == SS_F16 ? product16<SS_F16>(a, t, plan, x, ldx, s) : product16<SS_BF16>(a, t, plan, x, ldx, s);
     uint8_t *codes = static_cast<uint8_t *>(workspace), *scales = codes + codes_bytes(t, rows);
-    st = mx4_quantize(x, rows, desc->cin, ldx, desc->dtype, codes, scales, static_cast<hipStream_t>(stream));
+    st = mx4_quantize(x, rows, desc->cin, ldx, desc->dtype, codes, scales, s);
     if (st != SS_OK) return st;
-    return product(desc, codes, scales, rows, packed, bias, residual, ldr, act, y, ldy, static_cast<hipStream_t>(stream));
+    return product(desc, a, codes, scales, s);
 }

@@ -148,7 +148,7 @@ def _layer(ss, rows, cin, cout, dtype, seed, masked=True, spread=0.7):
 # one row to several tiles of pixels; reductions of less than a block to several chunks; output channels of less than a vector to several tiles
 SHAPES = [(1, 1, 1), (1, 32, 8), (1, 2048, 1000), (2, 96, 33), (5, 100, 64), (16, 512, 40), (17, 1024, 136), (31, 64, 96), (32, 8192, 32), (33, 288, 300), (49, 768, 264),
           (64, 256, 256), (65, 320, 31), (100, 1000, 777), (129, 96, 384), (200, 384, 96), (257, 544, 288), (300, 2048, 64), (515, 160, 520), (1000, 33, 7), (1, 8192, 1024),
-          (3, 4000, 2000), (2049, 128, 128), (1531, 1000, 777)]
+          (3, 4000, 2000), (2049, 128, 128), (1531, 1000, 777), (70, 5000, 100), (33, 8192, 40), (600, 4800, 700)]
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
@@ -263,8 +263,9 @@ def test_refusals(ss):
     refused(ss.ss_pw_mx4_fwd, desc, x, packed, None, residual[:4])
     refused(ss.ss_pw_mx4_fwd, desc, x, packed, None, None, 3)
     refused(ss.ss_pw_mx4_fwd, desc, x, packed, y=torch.empty((8, 48), dtype=BF16, device="cuda"))
-    if ss.ss_pw_mx4_workspace_bytes(desc, 8) > 0:
-        refused(ss.ss_pw_mx4_fwd, desc, x, packed, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"), status=ss.SS_ERR_WORKSPACE)
+    long, xl, pl, _, _, _, _ = _layer(ss, 64, 8192, 8, F16, 4)                     # (its codes are made in the workspace)
+    assert ss.ss_pw_mx4_workspace_bytes(long, 64) >= 64 * 4352
+    refused(ss.ss_pw_mx4_fwd, long, xl, pl, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"), status=ss.SS_ERR_WORKSPACE)
     refused(ss.ss_pw_mx4_q_fwd, desc, codes[:, :16], scales, packed)
     refused(ss.ss_pw_mx4_q_fwd, desc, codes, scales[:4], packed)
     refused(ss.ss_pw_mx4_q_fwd, desc, x, scales, packed)
