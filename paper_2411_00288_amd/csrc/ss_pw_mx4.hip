@@ -32,85 +32,105 @@ __device__ __forceinline__ f32x16 mma_mx4(const u32x4 &a, const u32x4 &b, const 
 
 constexpr int kChunk = 8;                                  // blocks of a reduction chunk: 256 channels, four steps, one scale word
 
-// A wave's MI x NI tiles of sums, finished and stored: bias, residual, activation, rounding, whole 16-byte runs where the channels allow it.
+// The bias of a lane's 16 channels of the tile from channel o0 on; ALL: the tile ends within the matrix.
+template <bool ALL>
+__device__ __forceinline__ void tile_bias(const PwArgs &p, int o0, int half, float (&bias)[16])
+{
+#pragma unroll
+    for (int q = 0; q < 4; q++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int o = o0 + 8 * q + 4 * half + e;
+            bias[4 * q + e] = p.bias != nullptr && (ALL || o < p.cout) ? p.bias[o] : 0.f;
+        }
+}
+
+// A 32 x 32 tile of sums, finished and stored: bias, residual, activation, rounding, and whole 16-byte runs where the channels allow it.
+template <int DT, bool ALL>
+__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, const float (&bias)[16], int o0, long long px, int half)
+{
+    const bool in = ALL || px < p.P;
+    float z[16];
+#pragma unroll
+    for (int v = 0; v < 16; v++) z[v] = acc[v] + bias[v];
+    if (p.residual != nullptr && in) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int o = o0 + 8 * q + 4 * half;
+            const uint16_t *src = p.residual + px * p.ldr + o;
+            if (ALL || o + 4 <= p.cout) {
+                const u32x2 r = reinterpret_cast<const Half16 *>(src)->v;
+                z[4 * q] += widen<DT>((uint16_t)r[0]);
+                z[4 * q + 1] += widen<DT>((uint16_t)(r[0] >> 16));
+                z[4 * q + 2] += widen<DT>((uint16_t)r[1]);
+                z[4 * q + 3] += widen<DT>((uint16_t)(r[1] >> 16));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (o + e < p.cout) z[4 * q + e] += widen<DT>(src[e]);
+            }
+        }
+    }
+    if (p.act == SS_ACT_RELU) {
+#pragma unroll
+        for (int v = 0; v < 16; v++) z[v] = floor_at(z[v], 0.f);
+    } else if (p.act == SS_ACT_GELU) {
+#pragma unroll
+        for (int v = 0; v < 16; v++) z[v] = gelu_cdf<DT>(z[v]);
+    }
+    // the two lanes of a pixel trade runs of four channels, so that each holds 16 in a row
+    uint32_t d[4][2];
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        d[q][0] = cvt_pack2<DT>(z[4 * q], z[4 * q + 1]);
+        d[q][1] = cvt_pack2<DT>(z[4 * q + 2], z[4 * q + 3]);
+    }
+    u32x4 run[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            const auto s = __builtin_amdgcn_permlane32_swap(d[q][e], d[q + 2][e], false, false);
+            run[q][e] = s[0];
+            run[q][2 + e] = s[1];
+        }
+    if (!in) return;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int o = o0 + 16 * half + 8 * q;
+        uint16_t *dst = p.y + px * p.ldy + o;
+        if (ALL || o + 8 <= p.cout) {
+            reinterpret_cast<Vec16 *>(dst)->v = run[q];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (o + e < p.cout) dst[e] = (uint16_t)(run[q][e / 2] >> (16 * (e % 2)));
+        }
+    }
+}
+
+// A wave's MI x NI tiles, from row tile mt0 and pixel px0 on.
 template <int DT, int MI, int NI>
 __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI][NI], int mt0, long long px0, int lane)
 {
     const int half = lane / 32;
+    const bool all = (mt0 + MI) * 32 <= p.cout && px0 + NI * 32 <= p.P;       // uniform
+    const auto put = [&](auto whole) {
+        constexpr bool ALL = decltype(whole)::value;
 #pragma unroll
-    for (int i = 0; i < MI; i++) {
-        const int o0 = (mt0 + i) * 32;
-        if (o0 >= p.cout) return;
-        float bias[16];
+        for (int i = 0; i < MI; i++) {
+            const int o0 = (mt0 + i) * 32;
+            if (!ALL && o0 >= p.cout) return;
+            float bias[16];
+            tile_bias<ALL>(p, o0, half, bias);
 #pragma unroll
-        for (int v = 0; v < 16; v++) {
-            const int o = o0 + 8 * (v / 4) + 4 * half + v % 4;
-            bias[v] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < NI; j++) {
-            __builtin_amdgcn_sched_barrier(0);
-            const long long px = px0 + j * 32 + lane % 32;
-            const bool in = px < p.P;
-            float z[16];
-#pragma unroll
-            for (int v = 0; v < 16; v++) z[v] = acc[i][j][v] + bias[v];
-            if (p.residual != nullptr && in) {
-#pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    const int o = o0 + 8 * q + 4 * half;
-                    const uint16_t *src = p.residual + px * p.ldr + o;
-                    if (o + 4 <= p.cout) {
-                        const u32x2 r = reinterpret_cast<const Half16 *>(src)->v;
-                        z[4 * q] += widen<DT>((uint16_t)r[0]);
-                        z[4 * q + 1] += widen<DT>((uint16_t)(r[0] >> 16));
-                        z[4 * q + 2] += widen<DT>((uint16_t)r[1]);
-                        z[4 * q + 3] += widen<DT>((uint16_t)(r[1] >> 16));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (o + e < p.cout) z[4 * q + e] += widen<DT>(src[e]);
-                    }
-                }
-            }
-            if (p.act == SS_ACT_RELU) {
-#pragma unroll
-                for (int v = 0; v < 16; v++) z[v] = floor_at(z[v], 0.f);
-            } else if (p.act == SS_ACT_GELU) {
-#pragma unroll
-                for (int v = 0; v < 16; v++) z[v] = gelu_cdf<DT>(z[v]);
-            }
-            // the two lanes of a pixel trade runs of four channels, so that each holds 16 in a row
-            uint32_t d[4][2];
-#pragma unroll
-            for (int q = 0; q < 4; q++) {
-                d[q][0] = cvt_pack2<DT>(z[4 * q], z[4 * q + 1]);
-                d[q][1] = cvt_pack2<DT>(z[4 * q + 2], z[4 * q + 3]);
-            }
-            u32x4 run[2];
-#pragma unroll
-            for (int q = 0; q < 2; q++)
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const auto s = __builtin_amdgcn_permlane32_swap(d[q][e], d[q + 2][e], false, false);
-                    run[q][e] = s[0];
-                    run[q][2 + e] = s[1];
-                }
-            if (!in) continue;
-#pragma unroll
-            for (int q = 0; q < 2; q++) {
-                const int o = o0 + 16 * half + 8 * q;
-                uint16_t *dst = p.y + px * p.ldy + o;
-                if (o + 8 <= p.cout) {
-                    reinterpret_cast<Vec16 *>(dst)->v = run[q];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        if (o + e < p.cout) dst[e] = (uint16_t)(run[q][e / 2] >> (16 * (e % 2)));
-                }
+            for (int j = 0; j < NI; j++) {
+                __builtin_amdgcn_sched_barrier(0);
+                store_tile<DT, ALL>(p, acc[i][j], bias, o0, px0 + j * 32 + lane % 32, half);
             }
         }
-    }
+    };
+    all ? put(std::true_type{}) : put(std::false_type{});
 }
 
 // Large products: four waves, MI x NI tiles of 32 x 32 each, make 64 MI output channels and 64 NI pixels.
@@ -273,15 +293,16 @@ struct PwRowsArgs {
     unsigned mul, sh;                      // division by a row's runs, 8 Ks
 };
 
-// Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves walk down the output channels, 64 at a
-// time, the next chunk of weights on its way from the L2 while the current one is multiplied.  The input is read once, whatever the number of channels.
+// Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves take units of 64 output channels and 32 rows
+// in turn (the units of one 64 channels side by side, so that their weights are in the L1), the next chunk of weights on its way from the L2 while the
+// current one is multiplied.  The input is read once, whatever the number of channels.
 template <int DT, int NT>
-__global__ __launch_bounds__(256, 2) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
+__global__ __launch_bounds__(256, 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     constexpr int PX = 32 * NT, PAD = PX + 1;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
+    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32, units = (Mt + 1) / 2 * NT;
     const long long row0 = (long long)blockIdx.x * PX;
     uint8_t *const codes_s = smem, *const scales_s = smem + 2 * Ks * PAD * 16;
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
@@ -298,12 +319,13 @@ __global__ __launch_bounds__(256, 2) void pw_mx4_rows_kernel(PwArgs p, PwRowsArg
                 wn[s][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (m * Ks + min(q * 4 + s, Ks - 1)) * 1024, 0));
         }
     };
-    int mt = wave * 2, q = 0;
-    if (mt < Mt) fetch(mt, 0);
+    int unit = wave, q = 0;
+    fetch(min(unit / NT * 2, Mt - 1), 0);
     quantise_rows<DT, 256, 4>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
     __syncthreads();
-    f32x16 acc[2][NT] = {};
-    while (mt < Mt) {
+    f32x16 acc[2][1] = {};
+    while (unit < units) {
+        const int mt = unit / NT * 2, at = unit % NT * 32;
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             sa[i] = sn[i];
@@ -311,28 +333,21 @@ __global__ __launch_bounds__(256, 2) void pw_mx4_rows_kernel(PwArgs p, PwRowsArg
             for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
         }
         const bool done = q + 1 == Kq;
-        const int nmt = done ? mt + 8 : mt, nq = done ? 0 : q + 1;
-        fetch(min(nmt, Mt - 1), nq);
-        uint32_t sb[NT];
-#pragma unroll
-        for (int j = 0; j < NT; j++) sb[j] = *reinterpret_cast<const uint32_t *>(scales_s + ((q * 2 + half) * PAD + j * 32 + lane % 32) * 4);
+        const int next = done ? unit + 4 : unit, nq = done ? 0 : q + 1;
+        fetch(min(next / NT * 2, Mt - 1), nq);
+        const uint32_t sb[1] = {*reinterpret_cast<const uint32_t *>(scales_s + ((q * 2 + half) * PAD + at + lane % 32) * 4)};
 #pragma unroll
         for (int s = 0; s < 4; s++) {
             if (q * 4 + s < Ks) {
-                u32x4 xb[NT];
-#pragma unroll
-                for (int j = 0; j < NT; j++) xb[j] = *reinterpret_cast<const u32x4 *>(codes_s + ((8 * q + 2 * s + half) * PAD + j * 32 + lane % 32) * 16);
-                step_mx4<2, NT>(s, wa[s], xb, acc, sa, sb);
+                const u32x4 xb[1] = {*reinterpret_cast<const u32x4 *>(codes_s + ((8 * q + 2 * s + half) * PAD + at + lane % 32) * 16)};
+                step_mx4<2, 1>(s, wa[s], xb, acc, sa, sb);
             }
         }
         if (done) {
-            pw_store<DT, 2, NT>(p, acc, mt, row0, lane);
-#pragma unroll
-            for (int i = 0; i < 2; i++)
-#pragma unroll
-                for (int j = 0; j < NT; j++) acc[i][j] = f32x16{};
+            pw_store<DT, 2, 1>(p, acc, mt, row0 + at, lane);
+            acc[0][0] = acc[1][0] = f32x16{};
         }
-        mt = nmt;
+        unit = next;
         q = nq;
     }
 }
