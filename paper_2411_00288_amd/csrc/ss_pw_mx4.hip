@@ -32,27 +32,33 @@ __device__ __forceinline__ f32x16 mma_mx4(const u32x4 &a, const u32x4 &b, const 
 
 constexpr int kChunk = 8;                                  // blocks of a reduction chunk: 256 channels, four steps, one scale word
 
-// The bias of a lane's 16 channels of the tile from channel o0 on; ALL: the tile ends within the matrix.
-template <bool ALL>
-__device__ __forceinline__ void tile_bias(const PwArgs &p, int o0, int half, float (&bias)[16])
+// What the sums of a 32 x 32 tile from channel o0 on start from: the bias.  (Loaded where zeros would be: no instruction for it.)
+__device__ __forceinline__ f32x16 tile_start(const PwArgs &p, int o0, int half)
 {
+    f32x16 s;
+    if (p.bias == nullptr) return f32x16{};
+    if (o0 + 32 <= p.cout) {                               // uniform
 #pragma unroll
-    for (int q = 0; q < 4; q++)
+        for (int v = 0; v < 16; v++) s[v] = p.bias[o0 + 8 * (v / 4) + 4 * half + v % 4];
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int o = o0 + 8 * q + 4 * half + e;
-            bias[4 * q + e] = p.bias != nullptr && (ALL || o < p.cout) ? p.bias[o] : 0.f;
+        for (int v = 0; v < 16; v++) {
+            const int o = o0 + 8 * (v / 4) + 4 * half + v % 4;
+            s[v] = o < p.cout ? p.bias[o] : 0.f;
         }
+    }
+    return s;
 }
 
-// A 32 x 32 tile of sums, finished and stored: bias, residual, activation, rounding, and whole 16-byte runs where the channels allow it.
+// A 32 x 32 tile of sums, finished and stored: residual, activation, rounding, and whole 16-byte runs where the channels allow it.  ALL: the tile ends
+// within the matrix.
 template <int DT, bool ALL>
-__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, const float (&bias)[16], int o0, long long px, int half)
+__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, int o0, long long px, int half)
 {
     const bool in = ALL || px < p.P;
     float z[16];
 #pragma unroll
-    for (int v = 0; v < 16; v++) z[v] = acc[v] + bias[v];
+    for (int v = 0; v < 16; v++) z[v] = acc[v];
     if (p.residual != nullptr && in) {
 #pragma unroll
         for (int q = 0; q < 4; q++) {
@@ -121,12 +127,10 @@ __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI
         for (int i = 0; i < MI; i++) {
             const int o0 = (mt0 + i) * 32;
             if (!ALL && o0 >= p.cout) return;
-            float bias[16];
-            tile_bias<ALL>(p, o0, half, bias);
 #pragma unroll
             for (int j = 0; j < NI; j++) {
                 __builtin_amdgcn_sched_barrier(0);
-                store_tile<DT, ALL>(p, acc[i][j], bias, o0, px0 + j * 32 + lane % 32, half);
+                store_tile<DT, ALL>(p, acc[i][j], o0, px0 + j * 32 + lane % 32, half);
             }
         }
     };
@@ -197,7 +201,14 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         for (int i = 0; i < MI; i++)
             to[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (min(mt0 + i, Mt - 1) * Kq + min(q, Kq - 1)) * 256, 0);
     };
-    f32x16 acc[MI][NI] = {};
+    f32x16 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; i++) {
+        acc[i][0] = tile_start(p, (mt0 + i) * 32, lane / 32);
+#pragma unroll
+        for (int j = 1; j < NI; j++) acc[i][j] = acc[i][0];
+    }
+    __builtin_amdgcn_sched_barrier(0);
     fetch(0);
     weight_scales(0, sa);
 #pragma unroll
@@ -266,20 +277,22 @@ __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, 
 {
     const int runs = 8 * Ks, total = count * runs;
     for (int base = 0; base < total; base += THREADS * U) {
-        float v[U][8];
+        Run<DT> raw[U];
         int row[U], run[U];
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int i = base + u * THREADS + (int)threadIdx.x;
             row[u] = (int)(((unsigned long long)(unsigned)i * mul) >> sh);
             run[u] = i - row[u] * runs;
-            load8<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0, v[u]);
+            raw[u] = load_run<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0);
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int b = run[u] / 4;
-            const uint32_t byte = mx4_scale(quad_max(magnitude8(v[u])));
-            const uint32_t c = mx4_codes8(v[u], byte);
+            float v[8];
+            widen_run<DT>(raw[u], v);
+            const uint32_t byte = mx4_scale(quad_max(magnitude8(v)));
+            const uint32_t c = mx4_codes8(v, byte);
             if (base + u * THREADS + (int)threadIdx.x >= total) continue;
             *reinterpret_cast<uint32_t *>(codes_s + (b * pad + row[u]) * 16 + run[u] % 4 * 4) = c;
             if (run[u] % 4 == 0) scales_s[((b / 8 * 2 + b % 2) * pad + row[u]) * 4 + b % 8 / 2] = (uint8_t)byte;
@@ -294,47 +307,33 @@ struct PwRowsArgs {
 };
 
 // Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves take units of 64 output channels and 32 rows
-// in turn (the units of one 64 channels side by side, so that their weights are in the L1), the next chunk of weights on its way from the L2 while the
-// current one is multiplied.  The input is read once, whatever the number of channels.
-template <int DT, int NT>
-__global__ __launch_bounds__(256, 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
+// in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels.  The next
+// weights are on their way from the L2 while the current ones are multiplied or, with a reduction of one chunk (SHORT), while the sums are finished: that
+// is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
+template <int DT, int NT, bool SHORT>
+__global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     constexpr int PX = 32 * NT, PAD = PX + 1;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32, units = (Mt + 1) / 2 * NT;
+    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = SHORT ? 1 : (Ks + 3) / 4, Mt = (p.cout + 31) / 32, units = (Mt + 1) / 2 * NT;
     const long long row0 = (long long)blockIdx.x * PX;
     uint8_t *const codes_s = smem, *const scales_s = smem + 2 * Ks * PAD * 16;
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 256, 0x00020000);
     u32x4 wa[4][2], wn[4][2];
     uint32_t sa[2], sn[2];
-    auto fetch = [&](int mt, int q) {
+    auto fetch = [&](int mt, int q, u32x4 (&w)[4][2], uint32_t (&sc)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             const int m = min(mt + i, Mt - 1);
-            sn[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (m * Kq + q) * 256, 0);
+            sc[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (m * Kq + q) * 256, 0);
 #pragma unroll
             for (int s = 0; s < 4; s++)
-                wn[s][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (m * Ks + min(q * 4 + s, Ks - 1)) * 1024, 0));
+                w[s][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (m * Ks + min(q * 4 + s, Ks - 1)) * 1024, 0));
         }
     };
-    int unit = wave, q = 0;
-    fetch(min(unit / NT * 2, Mt - 1), 0);
-    quantise_rows<DT, 256, 4>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
-    __syncthreads();
-    f32x16 acc[2][1] = {};
-    while (unit < units) {
-        const int mt = unit / NT * 2, at = unit % NT * 32;
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            sa[i] = sn[i];
-#pragma unroll
-            for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
-        }
-        const bool done = q + 1 == Kq;
-        const int next = done ? unit + 4 : unit, nq = done ? 0 : q + 1;
-        fetch(min(next / NT * 2, Mt - 1), nq);
+    auto multiply = [&](int at, int q, f32x16 (&acc)[2][1]) {
         const uint32_t sb[1] = {*reinterpret_cast<const uint32_t *>(scales_s + ((q * 2 + half) * PAD + at + lane % 32) * 4)};
 #pragma unroll
         for (int s = 0; s < 4; s++) {
@@ -343,77 +342,111 @@ __global__ __launch_bounds__(256, 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArg
                 step_mx4<2, 1>(s, wa[s], xb, acc, sa, sb);
             }
         }
-        if (done) {
+    };
+    auto start = [&](int mt, f32x16 (&acc)[2][1]) {
+        acc[0][0] = tile_start(p, mt * 32, half);
+        acc[1][0] = tile_start(p, mt * 32 + 32, half);
+    };
+    if constexpr (SHORT)
+        fetch(min(wave / NT * 2, Mt - 1), 0, wa, sa);
+    else
+        fetch(min(wave / NT * 2, Mt - 1), 0, wn, sn);
+    f32x16 acc[2][1];
+    start(wave / NT * 2, acc);
+    quantise_rows<DT, 256, SHORT ? 4 : 8>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
+    __syncthreads();
+    int unit = wave, q = 0;
+    while (unit < units) {
+        const int mt = unit / NT * 2, at = unit % NT * 32;
+        if constexpr (SHORT) {
+            multiply(at, 0, acc);
+            unit += 4;
+            fetch(min(unit / NT * 2, Mt - 1), 0, wa, sa);
             pw_store<DT, 2, 1>(p, acc, mt, row0 + at, lane);
-            acc[0][0] = acc[1][0] = f32x16{};
+            start(unit / NT * 2, acc);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                sa[i] = sn[i];
+#pragma unroll
+                for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
+            }
+            const bool done = q + 1 == Kq;
+            const int next = done ? unit + 4 : unit, nq = done ? 0 : q + 1;
+            fetch(min(next / NT * 2, Mt - 1), nq, wn, sn);
+            multiply(at, q, acc);
+            if (done) {
+                pw_store<DT, 2, 1>(p, acc, mt, row0 + at, lane);
+                start(next / NT * 2, acc);
+            }
+            unit = next;
+            q = nq;
         }
-        unit = next;
-        q = nq;
     }
 }
 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
-// the reduction and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first weights are on their way.
+// the reduction, a chunk each in turn, and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first
+// weights are on their way.
 template <int DT, int NW, int NI, bool QUANT>
 __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     static_assert(!QUANT || NI == 1, "rows in LDS");
-    constexpr int U = NI == 4 ? 2 : 4;                     // steps whose operands are in flight together
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const int KB = (p.K + 31) / 32, S = (KB + 3) / 4 * 4, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
     const int mt = blockIdx.x % Mt;
     const long long row0 = (long long)(blockIdx.x / Mt) * (32 * NI);
     const int rows = (int)min((long long)(32 * NI), p.P - row0), pad = rows | 1;
-    const int per = (Ks + NW - 1) / NW, k0 = min(wave * per, Ks), k1 = min(k0 + per, Ks);
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w) + (size_t)mt * Ks * 1024, 0, Ks * 1024, 0x00020000);
-    const uint8_t *const ws = p.w_scales + (size_t)mt * Kq * 256 + lane * 4;
-    auto weights = [&](int k, u32x4 (&wa)[U], uint32_t (&sa)[U]) {
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales) + (size_t)mt * Kq * 256, 0, Kq * 256, 0x00020000);
+    // (the offsets are the lanes' own: only those are held against the buffer's end, which a step past the last reads zeros behind)
+    auto weights = [&](int q, u32x4 (&wa)[4][1], uint32_t (&sa)[1]) {
+        sa[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, q * 256 + lane * 4, 0, 0);
 #pragma unroll
-        for (int u = 0; u < U; u++) {                      // (past the wave's share: past the buffer's end)
-            wa[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, k + u < k1 ? (k + u) * 1024 + lane * 16 : -16, 0, 0));
-            sa[u] = ws[(size_t)(min(k + u, Ks - 1) / 4) * 256 + min(k + u, Ks - 1) % 4];
-        }
+        for (int s = 0; s < 4; s++) wa[s][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (q * 4 + s) * 1024 + lane * 16, 0, 0));
     };
-    u32x4 wa[U];
-    uint32_t sa[U];
-    weights(k0, wa, sa);
+    u32x4 wa[4][1], wn[4][1];
+    uint32_t sa[1], sn[1];
+    weights(wave, wa, sa);
+    weights(wave + NW, wn, sn);
     uint8_t *const scales_s = smem + 2 * Ks * pad * 16;
     if constexpr (QUANT) {
-        quantise_rows<DT, NW * 64, 4>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
+        quantise_rows<DT, NW * 64, 8>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
         __syncthreads();
     }
     f32x16 acc[1][NI] = {};
     int px[NI];
 #pragma unroll
     for (int j = 0; j < NI; j++) px[j] = min(j * 32 + lane % 32, rows - 1);     // (lanes past the last row repeat it)
-    for (int k = k0; k < k1; k += U) {
-        u32x4 xb[U][NI], wn[U];
-        uint32_t sb[U][NI], sn[U];
+    for (int q = wave; q < Kq; q += NW) {
+        u32x4 xb[4][NI];
+        uint32_t sb[NI];
 #pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int j = 0; j < NI; j++) {
-                const int b = 2 * min(k + u, Ks - 1) + half;
-                if constexpr (QUANT) {
-                    xb[u][j] = *reinterpret_cast<const u32x4 *>(smem + (b * pad + px[j]) * 16);
-                    sb[u][j] = scales_s[((b / 8 * 2 + half) * pad + px[j]) * 4 + b % 8 / 2];
-                } else {
-                    const long long row = row0 + px[j];
-                    xb[u][j] = *reinterpret_cast<const u32x4 *>(p.codes + (row * KB + min(b, KB - 1)) * 16);
-                    sb[u][j] = b < KB ? p.scales[row * S + b] : 0u;
-                }
+        for (int j = 0; j < NI; j++) {
+            if constexpr (QUANT) {
+                sb[j] = *reinterpret_cast<const uint32_t *>(scales_s + ((q * 2 + half) * pad + px[j]) * 4);
+            } else {
+                const uint32_t *const s = reinterpret_cast<const uint32_t *>(p.scales + (row0 + px[j]) * S) + 2 * q;
+                sb[j] = __builtin_amdgcn_perm(8 * q + 4 < S ? s[1] : 0u, s[0], half ? 0x07050301u : 0x06040200u);
             }
-        weights(k + U, wn, sn);
 #pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int j = 0; j < NI; j++) acc[0][j] = mma_mx4<0>(wa[u], xb[u][j], acc[0][j], k + u < k1 ? sa[u] : 0u, k + u < k1 ? sb[u][j] : 0u);
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            wa[u] = wn[u];
-            sa[u] = sn[u];
+            for (int s = 0; s < 4; s++) {
+                const int b = 8 * q + 2 * s + half;
+                if constexpr (QUANT)
+                    xb[s][j] = *reinterpret_cast<const u32x4 *>(smem + (min(b, 2 * Ks - 1) * pad + px[j]) * 16);
+                else
+                    xb[s][j] = *reinterpret_cast<const u32x4 *>(p.codes + ((row0 + px[j]) * KB + min(b, KB - 1)) * 16);
+            }
         }
+        // (steps past the last: zero weights and zero scales; of QUANT's rows the scales of such steps were never written)
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+            if (q * 4 + s < Ks) step_mx4<1, NI>(s, wa[s], xb[s], acc, sa, sb);
+#pragma unroll
+        for (int s = 0; s < 4; s++) wa[s][0] = wn[s][0];
+        sa[0] = sn[0];
+        weights(q + 2 * NW, wn, sn);
     }
     // the waves' sums, 32 rows at a time: register v of lane l at (wave * 16 + v) * 65 + l, so that 32 channels of a row are 32 banks
     float *const sums = reinterpret_cast<float *>(smem);
@@ -545,12 +578,12 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
     if (tiles(1, 1) >= cus / 2) return go(One{}, One{});
     const long long px = ((long long)a.P + 31) / 32;
     const PwRowsArgs none{};
-    if (px * t.Mt <= cus || px == 1) {
-        if (t.Ks <= 16) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, false>>(px * t.Mt, 256, few_lds(t, 4, 0), s, a, none);
-        return launch_lds<pw_mx4_few_kernel<DT, 16, 1, false>>(px * t.Mt, 1024, few_lds(t, 16, 0), s, a, none);
-    }
-    if (t.Ks <= 16) return launch_lds<pw_mx4_few_kernel<DT, 4, 2, false>>((px + 1) / 2 * t.Mt, 256, few_lds(t, 4, 0), s, a, none);
-    return launch_lds<pw_mx4_few_kernel<DT, 16, 2, false>>((px + 1) / 2 * t.Mt, 1024, few_lds(t, 16, 0), s, a, none);
+    const auto few = [&](auto nw, auto ni) -> int {
+        constexpr int NW = decltype(nw)::value, NI = decltype(ni)::value;
+        return launch_lds<pw_mx4_few_kernel<DT, NW, NI, false>>((px + NI - 1) / NI * t.Mt, NW * 64, few_lds(t, NW, 0), s, a, none);
+    };
+    const auto waves = [&](auto ni) -> int { return t.Kq > 8 ? few(std::integral_constant<int, 16>{}, ni) : t.Kq > 4 ? few(std::integral_constant<int, 8>{}, ni) : few(Four{}, ni); };
+    return px * t.Mt <= cus || px == 1 ? waves(One{}) : waves(Two{});
 }
 
 template <int DT>
@@ -559,12 +592,16 @@ int product16(const PwArgs &a, const Mx4Dims &t, const PwPlan &plan, const void 
     PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0};
     fast_div_setup((unsigned)t.Ks * 8u, &r.mul, &r.sh);
     if (plan.kind == KIND_FEW) {
-        if (t.Ks <= 16) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
+        if (t.Kq <= 4) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
+        if (t.Kq <= 8) return launch_lds<pw_mx4_few_kernel<DT, 8, 1, true>>(t.Mt, 512, few_lds(t, 8, a.P), s, a, r);
         return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
     }
     const long long blocks = ((long long)a.P + plan.px - 1) / plan.px;
-    return plan.px == 64 ? launch_lds<pw_mx4_rows_kernel<DT, 2>>(blocks, 256, rows_lds(t, 64), s, a, r)
-                         : launch_lds<pw_mx4_rows_kernel<DT, 1>>(blocks, 256, rows_lds(t, 32), s, a, r);
+    if (t.Kq == 1)
+        return plan.px == 64 ? launch_lds<pw_mx4_rows_kernel<DT, 2, true>>(blocks, 256, rows_lds(t, 64), s, a, r)
+                             : launch_lds<pw_mx4_rows_kernel<DT, 1, true>>(blocks, 256, rows_lds(t, 32), s, a, r);
+    return plan.px == 64 ? launch_lds<pw_mx4_rows_kernel<DT, 2, false>>(blocks, 256, rows_lds(t, 64), s, a, r)
+                         : launch_lds<pw_mx4_rows_kernel<DT, 1, false>>(blocks, 256, rows_lds(t, 32), s, a, r);
 }
 
 int product(const ss_weight_desc *d, PwArgs a, const uint8_t *codes, const uint8_t *scales, hipStream_t s)

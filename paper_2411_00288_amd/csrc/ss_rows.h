@@ -35,30 +35,53 @@ __device__ __forceinline__ void store1(void *p, float v)
         *static_cast<uint16_t *>(p) = (uint16_t)cvt_pack2<DT>(v, 0.f);
 }
 
-// v[0..n) = p[0..n), the others `fill`; n <= 0: nothing is read.
+// A run as it lies in memory (32-bit: two vectors).
+template <int DT> struct Run { u32x4 v[DT == SS_F32 ? 2 : 1]; };
+
+// p[0..n), the others zero; n <= 0: nothing is read.
 template <int DT>
-__device__ __forceinline__ void load8(const void *p, int n, float (&v)[8], float fill = 0.f)
+__device__ __forceinline__ Run<DT> load_run(const void *p, int n)
 {
+    Run<DT> r = {};
     if (n >= 8) {
         if constexpr (DT == SS_F32) {
-            const u32x4 a = static_cast<const Vec32 *>(p)[0].v, b = static_cast<const Vec32 *>(p)[1].v;
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                v[e] = as_float(a[e]);
-                v[4 + e] = as_float(b[e]);
-            }
+            r.v[0] = static_cast<const Vec32 *>(p)[0].v;
+            r.v[1] = static_cast<const Vec32 *>(p)[1].v;
         } else {
-            const u32x4 a = static_cast<const Vec16 *>(p)->v;
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                v[2 * e] = widen<DT>((uint16_t)a[e]);
-                v[2 * e + 1] = DT == SS_BF16 ? as_float(a[e] & 0xFFFF0000u) : widen<DT>((uint16_t)(a[e] >> 16));
-            }
+            r.v[0] = static_cast<const Vec16 *>(p)->v;
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = e < n ? load1<DT>(static_cast<const char *>(p) + e * item_bytes<DT>()) : fill;
+        for (int e = 0; e < 7; e++)
+            if (e < n) {
+                if constexpr (DT == SS_F32)
+                    r.v[e / 4][e % 4] = static_cast<const uint32_t *>(p)[e];
+                else
+                    r.v[0][e / 2] |= (uint32_t) static_cast<const uint16_t *>(p)[e] << (16 * (e % 2));
+            }
     }
+    return r;
+}
+
+template <int DT>
+__device__ __forceinline__ void widen_run(const Run<DT> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        if constexpr (DT == SS_F32)
+            v[e] = as_float(r.v[e / 4][e % 4]);
+        else if constexpr (DT == SS_BF16)
+            v[e] = as_float(e % 2 ? r.v[0][e / 2] & 0xFFFF0000u : r.v[0][e / 2] << 16);
+        else
+            v[e] = widen<DT>((uint16_t)(r.v[0][e / 2] >> (16 * (e % 2))));
+    }
+}
+
+// v[0..n) = p[0..n), the others zero; n <= 0: nothing is read.
+template <int DT>
+__device__ __forceinline__ void load8(const void *p, int n, float (&v)[8])
+{
+    widen_run<DT>(load_run<DT>(p, n), v);
 }
 
 // p[0..n) = v[0..n), rounded to nearest even.
