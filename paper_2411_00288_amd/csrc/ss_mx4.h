@@ -42,6 +42,27 @@ __device__ __forceinline__ uint32_t magnitude8(const float (&v)[8])
     return m;
 }
 
+// The same of a run as it lies in memory, as an fp32 pattern: 16-bit patterns are compared in pairs.
+template <int DT>
+__device__ __forceinline__ uint32_t magnitude(const Run<DT> &r)
+{
+    if constexpr (DT == SS_F32) {
+        float v[8];
+        widen_run<DT>(r, v);
+        return magnitude8(v);
+    } else {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t word = r.v[0][e] & 0x7FFF7FFFu;
+            m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, word));
+        }
+        const uint16_t low = m[0], high = m[1];
+        return as_bits(widen<DT>(low > high ? low : high));
+    }
+}
+
 // The maximum over the four lanes of a quad, which hold a block.
 __device__ __forceinline__ uint32_t quad_max(uint32_t m)
 {
@@ -66,6 +87,35 @@ __device__ __forceinline__ uint32_t mx4_codes8(const float (&v)[8], uint32_t byt
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+}
+
+// The same for a run as it lies in memory; 16-bit values are converted as they are.
+template <int DT>
+__device__ __forceinline__ uint32_t mx4_codes(const Run<DT> &r, uint32_t byte)
+{
+    if constexpr (DT == SS_F32) {
+        float v[8];
+        widen_run<DT>(r, v);
+        return mx4_codes8(v, byte);
+    } else {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        if (byte == 0xFFu) return 0;
+        const float scale = as_float(byte == 0 ? 0x00400000u : byte << 23);
+        const uint32_t w0 = r.v[0][0], w1 = r.v[0][1], w2 = r.v[0][2], w3 = r.v[0][3];
+        uint32_t c = 0;
+        if constexpr (DT == SS_F16) {
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, w0), scale, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, w1), scale, 1);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, w2), scale, 2);
+            return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, w3), scale, 3);
+        } else {
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w0), scale, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w1), scale, 1);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w2), scale, 2);
+            return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w3), scale, 3);
+        }
+    }
 }
 
 // What eight codes stand for.

@@ -13,7 +13,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char *__restric
 {
     const int KB = (cols + 31) / 32, S = (int)runs / 4;
     const long long first = (long long)blockIdx.x * 1024 + threadIdx.x;
-    float v[4][8];
+    Run<DT> v[4];
     long long row[4];
     int run[4];
 #pragma unroll
@@ -25,13 +25,13 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char *__restric
             row[u] = i / runs;
         run[u] = (int)(i - row[u] * runs);
         const int n = i < total ? cols - run[u] * 8 : 0;
-        load8<DT>(x + (row[u] * ldx + run[u] * 8) * item_bytes<DT>(), n, v[u]);
+        v[u] = load_run<DT>(x + (row[u] * ldx + run[u] * 8) * item_bytes<DT>(), n);
     }
 #pragma unroll
     for (int u = 0; u < 4; u++) {
         if (first + u * 256 >= total) return;
-        const uint32_t byte = mx4_scale(quad_max(magnitude8(v[u])));
-        if (run[u] < 4 * KB) *reinterpret_cast<uint32_t *>(codes + (row[u] * KB * 4 + run[u]) * 4) = mx4_codes8(v[u], byte);
+        const uint32_t byte = mx4_scale(quad_max(magnitude<DT>(v[u])));
+        if (run[u] < 4 * KB) *reinterpret_cast<uint32_t *>(codes + (row[u] * KB * 4 + run[u]) * 4) = mx4_codes<DT>(v[u], byte);
         if (run[u] % 4 == 0) scales[row[u] * S + run[u] / 4] = (uint8_t)byte;
     }
 }

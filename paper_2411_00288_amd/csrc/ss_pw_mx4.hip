@@ -289,10 +289,8 @@ __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, 
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int b = run[u] / 4;
-            float v[8];
-            widen_run<DT>(raw[u], v);
-            const uint32_t byte = mx4_scale(quad_max(magnitude8(v)));
-            const uint32_t c = mx4_codes8(v, byte);
+            const uint32_t byte = mx4_scale(quad_max(magnitude<DT>(raw[u])));
+            const uint32_t c = mx4_codes<DT>(raw[u], byte);
             if (base + u * THREADS + (int)threadIdx.x >= total) continue;
             *reinterpret_cast<uint32_t *>(codes_s + (b * pad + row[u]) * 16 + run[u] % 4 * 4) = c;
             if (run[u] % 4 == 0) scales_s[((b / 8 * 2 + b % 2) * pad + row[u]) * 4 + b % 8 / 2] = (uint8_t)byte;
