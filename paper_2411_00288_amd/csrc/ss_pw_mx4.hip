@@ -53,8 +53,9 @@ __device__ __forceinline__ f32x16 tile_start(const PwArgs &p, int o0, int half)
 // A 32 x 32 tile of sums, finished and stored: residual, activation, rounding, and whole 16-byte runs where the channels allow it.  ALL: the tile ends
 // within the matrix.
 template <int DT, bool ALL>
-__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, int o0, long long px, int half)
+__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, int o0, long long px0, int half)
 {
+    const long long px = px0 + threadIdx.x % 32;
     const bool in = ALL || px < p.P;
     float z[16];
 #pragma unroll
@@ -84,7 +85,9 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, i
 #pragma unroll
         for (int v = 0; v < 16; v++) z[v] = gelu_cdf<DT>(z[v]);
     }
-    // the two lanes of a pixel trade runs of four channels, so that each holds 16 in a row
+    // A lane holds runs of four channels of one pixel, and a store of those would write 8 bytes here and there.  Its partner's runs come in first (16
+    // bytes of a pixel to the lane, 32 to the two of them), then pixel 16 to 31's places in the first half of the channels are traded for pixel 0 to
+    // 15's in the second: a store instruction then writes all 64 bytes of 16 pixels.
     uint32_t d[4][2];
 #pragma unroll
     for (int q = 0; q < 4; q++) {
@@ -96,15 +99,23 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, i
     for (int q = 0; q < 2; q++)
 #pragma unroll
         for (int e = 0; e < 2; e++) {
-            const auto s = __builtin_amdgcn_permlane32_swap(d[q][e], d[q + 2][e], false, false);
+            const auto s = __builtin_amdgcn_permlane32_swap(d[2 * q][e], d[2 * q + 1][e], false, false);
             run[q][e] = s[0];
             run[q][2 + e] = s[1];
         }
-    if (!in) return;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const uint32_t a = run[0][e], b = run[1][e];
+        const auto s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+        run[0][e] = s[0];
+        run[1][e] = s[1];
+    }
+    const int lane = threadIdx.x % 64, o = o0 + lane / 16 % 2 * 16 + half * 8;
 #pragma unroll
     for (int q = 0; q < 2; q++) {
-        const int o = o0 + 16 * half + 8 * q;
-        uint16_t *dst = p.y + px * p.ldy + o;
+        const long long to = px0 + 16 * q + lane % 16;
+        if (!ALL && to >= p.P) continue;
+        uint16_t *dst = p.y + to * p.ldy + o;
         if (ALL || o + 8 <= p.cout) {
             reinterpret_cast<Vec16 *>(dst)->v = run[q];
         } else {
@@ -116,25 +127,19 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, i
 }
 
 // A wave's MI x NI tiles, from row tile mt0 and pixel px0 on.
-template <int DT, int MI, int NI>
+template <int DT, int MI, int NI, bool ALL>
 __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI][NI], int mt0, long long px0, int lane)
 {
-    const int half = lane / 32;
-    const bool all = (mt0 + MI) * 32 <= p.cout && px0 + NI * 32 <= p.P;       // uniform
-    const auto put = [&](auto whole) {
-        constexpr bool ALL = decltype(whole)::value;
 #pragma unroll
-        for (int i = 0; i < MI; i++) {
-            const int o0 = (mt0 + i) * 32;
-            if (!ALL && o0 >= p.cout) return;
+    for (int i = 0; i < MI; i++) {
+        const int o0 = (mt0 + i) * 32;
+        if (!ALL && o0 >= p.cout) return;
 #pragma unroll
-            for (int j = 0; j < NI; j++) {
-                __builtin_amdgcn_sched_barrier(0);
-                store_tile<DT, ALL>(p, acc[i][j], o0, px0 + j * 32 + lane % 32, half);
-            }
+        for (int j = 0; j < NI; j++) {
+            __builtin_amdgcn_sched_barrier(0);
+            store_tile<DT, ALL>(p, acc[i][j], o0, px0 + j * 32, lane / 32);
         }
-    };
-    all ? put(std::true_type{}) : put(std::false_type{});
+    }
 }
 
 // Large products: four waves, MI x NI tiles of 32 x 32 each, make 64 MI output channels and 64 NI pixels.
@@ -250,7 +255,10 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         for (int i = 0; i < MI; i++) sa[i] = na[i];
         lds_barrier();
     }
-    pw_store<DT, MI, NI>(p, acc, mt0, row0 + px0, lane);
+    if ((mt0 + MI) * 32 <= p.cout && row0 + px0 + NI * 32 <= p.P)              // uniform
+        pw_store<DT, MI, NI, true>(p, acc, mt0, row0 + px0, lane);
+    else
+        pw_store<DT, MI, NI, false>(p, acc, mt0, row0 + px0, lane);
 }
 
 // The product of step s of a scale word.
@@ -269,9 +277,9 @@ __device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x
 }
 
 // 16-bit input rows of a workgroup, quantised into LDS.  Block b of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
-// pieces, and with an odd `pad` the quads of a row's neighbouring blocks write to different banks.  The scale of b = 8 q + 2 s + half is byte s of word
+// pieces, and with an odd `pad` the quads of a row's neighbouring blocks write to different banks.  WHOLE: K is a multiple of 8.  The scale of b = 8 q + 2 s + half is byte s of word
 // (q * 2 + half) * pad + r, the four steps of a lane.  Blocks 0 .. 2 Ks - 1, rows 0 .. count - 1; what is past the matrix is zero.
-template <int DT, int THREADS, int U>
+template <int DT, int THREADS, int U, bool WHOLE>
 __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, int rows, int count, int K, int Ks, int pad, unsigned mul, unsigned sh, uint8_t *codes_s,
                                               uint8_t *scales_s)
 {
@@ -284,7 +292,12 @@ __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, 
             const int i = base + u * THREADS + (int)threadIdx.x;
             row[u] = (int)(((unsigned long long)(unsigned)i * mul) >> sh);
             run[u] = i - row[u] * runs;
-            raw[u] = load_run<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0);
+            if constexpr (WHOLE) {                         // (one load, from inside the matrix, whatever the lane: no branches between the loads)
+                raw[u].v[0] = reinterpret_cast<const Vec16 *>(x + min(row[u], rows - 1) * ldx + min(run[u] * 8, K - 8))->v;
+                if (row[u] >= rows || run[u] * 8 >= K) raw[u].v[0] = u32x4{};
+            } else {
+                raw[u] = load_run<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0);
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
@@ -308,7 +321,7 @@ struct PwRowsArgs {
 // in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels.  The next
 // weights are on their way from the L2 while the current ones are multiplied or, with a reduction of one chunk (SHORT), while the sums are finished: that
 // is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
-template <int DT, int NT, bool SHORT>
+template <int DT, int NT, bool SHORT, bool WHOLE>
 __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -341,52 +354,69 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
             }
         }
     };
+    // The sums start from the bias, which waits in LDS: a load behind the last unit's stores would wait for those, too.
+    float *const bias_s = reinterpret_cast<float *>(scales_s + (Kq * 2 * PAD * 4 + 15) / 16 * 16);
     auto start = [&](int mt, f32x16 (&acc)[2][1]) {
-        acc[0][0] = tile_start(p, mt * 32, half);
-        acc[1][0] = tile_start(p, mt * 32 + 32, half);
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(bias_s + min(mt + i, Mt - 1) * 32 + 8 * g + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; e++) acc[i][0][4 * g + e] = b[e];
+            }
     };
+    for (int o = threadIdx.x; o < Mt * 32; o += 256) bias_s[o] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
     if constexpr (SHORT)
         fetch(min(wave / NT * 2, Mt - 1), 0, wa, sa);
     else
         fetch(min(wave / NT * 2, Mt - 1), 0, wn, sn);
-    f32x16 acc[2][1];
-    start(wave / NT * 2, acc);
-    quantise_rows<DT, 256, SHORT ? 4 : 8>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
+    quantise_rows<DT, 256, SHORT ? 4 : 8, WHOLE>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
     __syncthreads();
-    int unit = wave, q = 0;
-    while (unit < units) {
-        const int mt = unit / NT * 2, at = unit % NT * 32;
-        if constexpr (SHORT) {
-            multiply(at, 0, acc);
-            unit += 4;
-            fetch(min(unit / NT * 2, Mt - 1), 0, wa, sa);
-            pw_store<DT, 2, 1>(p, acc, mt, row0 + at, lane);
-            start(unit / NT * 2, acc);
-        } else {
+    // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
+    // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us).
+    __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt 0, the first weights: so that the loop is entered with none on their way)
+    const auto walk = [&](auto whole) {
+        constexpr bool ALL = decltype(whole)::value;
+        f32x16 acc[2][1];
+        start(wave / NT * 2, acc);
+        int unit = wave, q = 0;
+        while (unit < units) {
+            const int mt = unit / NT * 2, at = unit % NT * 32;
+            if constexpr (SHORT) {
+                multiply(at, 0, acc);
+                unit += 4;
+                fetch(min(unit / NT * 2, Mt - 1), 0, wa, sa);
+                pw_store<DT, 2, 1, ALL>(p, acc, mt, row0 + at, lane);
+                __builtin_amdgcn_sched_barrier(0);
+                start(unit / NT * 2, acc);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                sa[i] = sn[i];
+                for (int i = 0; i < 2; i++) {
+                    sa[i] = sn[i];
 #pragma unroll
-                for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
+                    for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
+                }
+                const bool done = q + 1 == Kq;
+                const int next = done ? unit + 4 : unit, nq = done ? 0 : q + 1;
+                fetch(min(next / NT * 2, Mt - 1), nq, wn, sn);
+                multiply(at, q, acc);
+                if (done) {
+                    pw_store<DT, 2, 1, ALL>(p, acc, mt, row0 + at, lane);
+                    start(next / NT * 2, acc);
+                }
+                unit = next;
+                q = nq;
             }
-            const bool done = q + 1 == Kq;
-            const int next = done ? unit + 4 : unit, nq = done ? 0 : q + 1;
-            fetch(min(next / NT * 2, Mt - 1), nq, wn, sn);
-            multiply(at, q, acc);
-            if (done) {
-                pw_store<DT, 2, 1>(p, acc, mt, row0 + at, lane);
-                start(next / NT * 2, acc);
-            }
-            unit = next;
-            q = nq;
         }
-    }
+    };
+    p.cout % 64 == 0 && row0 + PX <= p.P ? walk(std::true_type{}) : walk(std::false_type{});
 }
 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
 // the reduction, a chunk each in turn, and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first
 // weights are on their way.
-template <int DT, int NW, int NI, bool QUANT>
+template <int DT, int NW, int NI, bool QUANT, bool WHOLE>
 __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -410,7 +440,7 @@ __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArg
     weights(wave + NW, wn, sn);
     uint8_t *const scales_s = smem + 2 * Ks * pad * 16;
     if constexpr (QUANT) {
-        quantise_rows<DT, NW * 64, 8>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
+        quantise_rows<DT, NW * 64, 8, WHOLE>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
         __syncthreads();
     }
     f32x16 acc[1][NI] = {};
@@ -540,7 +570,11 @@ size_t few_lds(const Mx4Dims &t, int waves, int quantised_rows)
     return std::max(rows, (size_t)waves * 16 * 65 * 4);
 }
 
-size_t rows_lds(const Mx4Dims &t, int px) { return (size_t)2 * t.Ks * (px + 1) * 16 + (size_t)t.Kq * 2 * (px + 1) * 4; }
+// LDS of the kernel for reductions that fit it: quantised rows, their scales, the bias.
+size_t rows_lds(const Mx4Dims &t, int px)
+{
+    return (size_t)2 * t.Ks * (px + 1) * 16 + ((size_t)t.Kq * 2 * (px + 1) * 4 + 15) / 16 * 16 + (size_t)t.Mt * 128;
+}
 
 enum { KIND_TILE = 0, KIND_FEW, KIND_ROWS };
 
@@ -578,7 +612,7 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
     const PwRowsArgs none{};
     const auto few = [&](auto nw, auto ni) -> int {
         constexpr int NW = decltype(nw)::value, NI = decltype(ni)::value;
-        return launch_lds<pw_mx4_few_kernel<DT, NW, NI, false>>((px + NI - 1) / NI * t.Mt, NW * 64, few_lds(t, NW, 0), s, a, none);
+        return launch_lds<pw_mx4_few_kernel<DT, NW, NI, false, false>>((px + NI - 1) / NI * t.Mt, NW * 64, few_lds(t, NW, 0), s, a, none);
     };
     const auto waves = [&](auto ni) -> int { return t.Kq > 8 ? few(std::integral_constant<int, 16>{}, ni) : t.Kq > 4 ? few(std::integral_constant<int, 8>{}, ni) : few(Four{}, ni); };
     return px * t.Mt <= cus || px == 1 ? waves(One{}) : waves(Two{});
@@ -589,17 +623,24 @@ int product16(const PwArgs &a, const Mx4Dims &t, const PwPlan &plan, const void 
 {
     PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0};
     fast_div_setup((unsigned)t.Ks * 8u, &r.mul, &r.sh);
-    if (plan.kind == KIND_FEW) {
-        if (t.Kq <= 4) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
-        if (t.Kq <= 8) return launch_lds<pw_mx4_few_kernel<DT, 8, 1, true>>(t.Mt, 512, few_lds(t, 8, a.P), s, a, r);
-        return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
-    }
-    const long long blocks = ((long long)a.P + plan.px - 1) / plan.px;
-    if (t.Kq == 1)
-        return plan.px == 64 ? launch_lds<pw_mx4_rows_kernel<DT, 2, true>>(blocks, 256, rows_lds(t, 64), s, a, r)
-                             : launch_lds<pw_mx4_rows_kernel<DT, 1, true>>(blocks, 256, rows_lds(t, 32), s, a, r);
-    return plan.px == 64 ? launch_lds<pw_mx4_rows_kernel<DT, 2, false>>(blocks, 256, rows_lds(t, 64), s, a, r)
-                         : launch_lds<pw_mx4_rows_kernel<DT, 1, false>>(blocks, 256, rows_lds(t, 32), s, a, r);
+    const auto go = [&](auto whole) -> int {
+        constexpr bool WHOLE = decltype(whole)::value;
+        if (plan.kind == KIND_FEW) {
+            if (t.Kq <= 4) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true, WHOLE>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
+            if (t.Kq <= 8) return launch_lds<pw_mx4_few_kernel<DT, 8, 1, true, WHOLE>>(t.Mt, 512, few_lds(t, 8, a.P), s, a, r);
+            return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true, WHOLE>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
+        }
+        const long long blocks = ((long long)a.P + plan.px - 1) / plan.px;
+        const auto rows = [&](auto nt, auto brief) -> int {
+            constexpr int NT = decltype(nt)::value;
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WHOLE>>(blocks, 256, rows_lds(t, 32 * NT), s, a, r);
+        };
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        if (t.Kq == 1) return plan.px == 64 ? rows(Two{}, std::true_type{}) : rows(One{}, std::true_type{});
+        return plan.px == 64 ? rows(Two{}, std::false_type{}) : rows(One{}, std::false_type{});
+    };
+    return a.K % 8 == 0 ? go(std::true_type{}) : go(std::false_type{});
 }
 
 int product(const ss_weight_desc *d, PwArgs a, const uint8_t *codes, const uint8_t *scales, hipStream_t s)
