@@ -19,6 +19,7 @@ struct PwArgs {
     uint16_t *y;
     long long ldr, ldy;
     int P, cout, K, act;
+    bool stream;                           // the output passes the caches by
 };
 
 // One product of 32 output channels and 32 pixels over 64 reduction indices: lane l gives the 32 values of block l/32 of weight row l%32 and of
@@ -32,34 +33,30 @@ __device__ __forceinline__ f32x16 mma_mx4(const u32x4 &a, const u32x4 &b, const 
 
 constexpr int kChunk = 8;                                  // blocks of a reduction chunk: 256 channels, four steps, one scale word
 
-// What the sums of a 32 x 32 tile from channel o0 on start from: the bias.  (Loaded where zeros would be: no instruction for it.)
-__device__ __forceinline__ f32x16 tile_start(const PwArgs &p, int o0, int half)
+// The bias of a lane's 16 channels of the tile from channel o0 on; ALL: the tile ends within the matrix.
+template <bool ALL>
+__device__ __forceinline__ f32x16 tile_bias(const PwArgs &p, int o0, int half)
 {
-    f32x16 s;
-    if (p.bias == nullptr) return f32x16{};
-    if (o0 + 32 <= p.cout) {                               // uniform
+    f32x16 s = {};
+    if (p.bias == nullptr) return s;
 #pragma unroll
-        for (int v = 0; v < 16; v++) s[v] = p.bias[o0 + 8 * (v / 4) + 4 * half + v % 4];
-    } else {
-#pragma unroll
-        for (int v = 0; v < 16; v++) {
-            const int o = o0 + 8 * (v / 4) + 4 * half + v % 4;
-            s[v] = o < p.cout ? p.bias[o] : 0.f;
-        }
+    for (int v = 0; v < 16; v++) {
+        const int o = o0 + 8 * (v / 4) + 4 * half + v % 4;
+        s[v] = ALL || o < p.cout ? p.bias[o] : 0.f;
     }
     return s;
 }
 
 // A 32 x 32 tile of sums, finished and stored: residual, activation, rounding, and whole 16-byte runs where the channels allow it.  ALL: the tile ends
-// within the matrix.
-template <int DT, bool ALL>
-__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, int o0, long long px0, int half)
+// within the matrix.  BIAS: it is not in the sums yet.  STREAM: the output's lines are not kept in the caches.
+template <int DT, bool ALL, bool BIAS, bool STREAM>
+__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, const f32x16 &bias, int o0, long long px0, int half)
 {
     const long long px = px0 + threadIdx.x % 32;
     const bool in = ALL || px < p.P;
     float z[16];
 #pragma unroll
-    for (int v = 0; v < 16; v++) z[v] = acc[v];
+    for (int v = 0; v < 16; v++) z[v] = BIAS ? acc[v] + bias[v] : acc[v];
     if (p.residual != nullptr && in) {
 #pragma unroll
         for (int q = 0; q < 4; q++) {
@@ -117,7 +114,10 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, i
         if (!ALL && to >= p.P) continue;
         uint16_t *dst = p.y + to * p.ldy + o;
         if (ALL || o + 8 <= p.cout) {
-            reinterpret_cast<Vec16 *>(dst)->v = run[q];
+            if constexpr (STREAM)
+                __builtin_nontemporal_store(run[q], &reinterpret_cast<Vec16 *>(dst)->v);
+            else
+                reinterpret_cast<Vec16 *>(dst)->v = run[q];
         } else {
 #pragma unroll
             for (int e = 0; e < 8; e++)
@@ -126,18 +126,20 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, i
     }
 }
 
-// A wave's MI x NI tiles, from row tile mt0 and pixel px0 on.
-template <int DT, int MI, int NI, bool ALL>
+// A wave's MI x NI tiles, from row tile mt0 and pixel px0 on.  BIAS: it is not in the sums yet.
+template <int DT, int MI, int NI, bool ALL, bool BIAS, bool STREAM>
 __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI][NI], int mt0, long long px0, int lane)
 {
 #pragma unroll
     for (int i = 0; i < MI; i++) {
         const int o0 = (mt0 + i) * 32;
         if (!ALL && o0 >= p.cout) return;
+        f32x16 bias = {};
+        if constexpr (BIAS) bias = tile_bias<ALL>(p, o0, lane / 32);
 #pragma unroll
         for (int j = 0; j < NI; j++) {
             __builtin_amdgcn_sched_barrier(0);
-            store_tile<DT, ALL>(p, acc[i][j], o0, px0 + j * 32, lane / 32);
+            store_tile<DT, ALL, BIAS, STREAM>(p, acc[i][j], bias, o0, px0 + j * 32, lane / 32);
         }
     }
 }
@@ -206,14 +208,7 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         for (int i = 0; i < MI; i++)
             to[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (min(mt0 + i, Mt - 1) * Kq + min(q, Kq - 1)) * 256, 0);
     };
-    f32x16 acc[MI][NI];
-#pragma unroll
-    for (int i = 0; i < MI; i++) {
-        acc[i][0] = tile_start(p, (mt0 + i) * 32, lane / 32);
-#pragma unroll
-        for (int j = 1; j < NI; j++) acc[i][j] = acc[i][0];
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    f32x16 acc[MI][NI] = {};
     fetch(0);
     weight_scales(0, sa);
 #pragma unroll
@@ -256,9 +251,9 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         lds_barrier();
     }
     if ((mt0 + MI) * 32 <= p.cout && row0 + px0 + NI * 32 <= p.P)              // uniform
-        pw_store<DT, MI, NI, true>(p, acc, mt0, row0 + px0, lane);
+        pw_store<DT, MI, NI, true, true, false>(p, acc, mt0, row0 + px0, lane);
     else
-        pw_store<DT, MI, NI, false>(p, acc, mt0, row0 + px0, lane);
+        pw_store<DT, MI, NI, false, true, false>(p, acc, mt0, row0 + px0, lane);
 }
 
 // The product of step s of a scale word.
@@ -376,8 +371,8 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
     // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us).
     __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt 0, the first weights: so that the loop is entered with none on their way)
-    const auto walk = [&](auto whole) {
-        constexpr bool ALL = decltype(whole)::value;
+    const auto walk = [&](auto whole, auto stream) {
+        constexpr bool ALL = decltype(whole)::value, STREAM = decltype(stream)::value;
         f32x16 acc[2][1];
         start(wave / NT * 2, acc);
         int unit = wave, q = 0;
@@ -387,7 +382,7 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
                 multiply(at, 0, acc);
                 unit += 4;
                 fetch(min(unit / NT * 2, Mt - 1), 0, wa, sa);
-                pw_store<DT, 2, 1, ALL>(p, acc, mt, row0 + at, lane);
+                pw_store<DT, 2, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
                 __builtin_amdgcn_sched_barrier(0);
                 start(unit / NT * 2, acc);
             } else {
@@ -402,7 +397,7 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
                 fetch(min(next / NT * 2, Mt - 1), nq, wn, sn);
                 multiply(at, q, acc);
                 if (done) {
-                    pw_store<DT, 2, 1, ALL>(p, acc, mt, row0 + at, lane);
+                    pw_store<DT, 2, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
                     start(next / NT * 2, acc);
                 }
                 unit = next;
@@ -410,7 +405,10 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
             }
         }
     };
-    p.cout % 64 == 0 && row0 + PX <= p.P ? walk(std::true_type{}) : walk(std::false_type{});
+    if (p.cout % 64 != 0 || row0 + PX > p.P)
+        walk(std::false_type{}, std::false_type{});
+    else
+        p.stream ? walk(std::true_type{}, std::true_type{}) : walk(std::true_type{}, std::false_type{});
 }
 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
@@ -560,6 +558,9 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
+    // An output of more than half the last-level cache is gone from it before anyone reads it, and its lines leave in the order of their rows only if they are not
+    // kept: 401408 x 96 -> 384 (308 MB) 138 -> 101 us, 192 channels (154 MB) 50.0 -> 49.1, 96 (77 MB) 33.5 -> 32.8 on its own.
+    a.stream = (long long)rows * d->cout * 2 > 128ll << 20;
     return a;
 }
 
@@ -586,7 +587,7 @@ struct PwPlan {
 PwPlan plan16(const Mx4Dims &t, int64_t rows)
 {
     if (rows <= 32 && few_lds(t, 16, (int)rows) <= 160 * 1024) return {KIND_FEW, 32};
-    if (rows_lds(t, 32) <= 80 * 1024) return {KIND_ROWS, rows >= 64 * 512 && rows_lds(t, 64) <= 40 * 1024 ? 64 : 32};
+    if (rows_lds(t, 32) <= 80 * 1024) return {KIND_ROWS, rows >= 64 * 512 && rows_lds(t, 64) <= 40 * 1024 ? (t.Kq == 1 ? 128 : 64) : 32};
     return {KIND_TILE, 0};
 }
 
@@ -637,7 +638,7 @@ int product16(const PwArgs &a, const Mx4Dims &t, const PwPlan &plan, const void 
         };
         using One = std::integral_constant<int, 1>;
         using Two = std::integral_constant<int, 2>;
-        if (t.Kq == 1) return plan.px == 64 ? rows(Two{}, std::true_type{}) : rows(One{}, std::true_type{});
+        if (t.Kq == 1) return plan.px == 128 ? rows(std::integral_constant<int, 4>{}, std::true_type{}) : rows(One{}, std::true_type{});
         return plan.px == 64 ? rows(Two{}, std::false_type{}) : rows(One{}, std::false_type{});
     };
     return a.K % 8 == 0 ? go(std::true_type{}) : go(std::false_type{});
