@@ -1,13 +1,15 @@
 // Quantisation to MXFP4 and back, and the packing of weights for the pointwise layer on such operands.
 #include "ss_mx4.h"
 #include "ss_conv_params.h"
+#include <type_traits>
 
 namespace ss {
 
 // One thread per run of 8 values, four runs a thread; the quad of lanes that holds a block finds its scale among itself.  Bound by memory: 2 bytes
 // read and 0.53 written for a 16-bit value.  `runs` = 16 * ceil(blocks / 4) to the row, so that a quad is never split between rows and the
 // scales' surplus bytes are written too.
-template <int DT>
+// WIDE: rows of at least 8.
+template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char *__restrict__ x, long long ldx, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
                                                            long long total, int cols, unsigned runs, unsigned mul, unsigned sh)
 {
@@ -24,12 +26,15 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char *__restric
         else
             row[u] = i / runs;
         run[u] = (int)(i - row[u] * runs);
-        const int n = i < total ? cols - run[u] * 8 : 0;
-        v[u] = load_run<DT>(x + (row[u] * ldx + run[u] * 8) * item_bytes<DT>(), n);
+        if constexpr (WIDE)                              // (past the last run: the first row)
+            v[u] = load_wide<DT>(x + (i < total ? row[u] * ldx : 0ll) * item_bytes<DT>(), run[u] * 8, cols);
+        else
+            v[u] = load_run<DT>(x + (row[u] * ldx + run[u] * 8) * item_bytes<DT>(), i < total ? cols - run[u] * 8 : 0);
     }
 #pragma unroll
     for (int u = 0; u < 4; u++) {
         if (first + u * 256 >= total) return;
+        if constexpr (WIDE) place_wide<DT>(v[u], run[u] * 8, cols, true);
         const uint32_t byte = mx4_scale(quad_max(magnitude<DT>(v[u])));
         if (run[u] < 4 * KB) *reinterpret_cast<uint32_t *>(codes + (row[u] * KB * 4 + run[u]) * 4) = mx4_codes<DT>(v[u], byte);
         if (run[u] % 4 == 0) scales[row[u] * S + run[u] / 4] = (uint8_t)byte;
@@ -128,7 +133,11 @@ int mx4_quantize(const void *x, int64_t rows, int cols, int64_t ldx, int dtype, 
     const auto go = [&](auto kern) {
         kern<<<dim3((unsigned)blocks), dim3(256), 0, s>>>(static_cast<const char *>(x), (long long)ldx, codes, scales, total, cols, runs, mul, sh);
     };
-    dtype == SS_F16 ? go(mx4_quantize_kernel<SS_F16>) : dtype == SS_BF16 ? go(mx4_quantize_kernel<SS_BF16>) : go(mx4_quantize_kernel<SS_F32>);
+    const auto pick = [&](auto wide) {
+        constexpr bool WIDE = decltype(wide)::value;
+        dtype == SS_F16 ? go(mx4_quantize_kernel<SS_F16, WIDE>) : dtype == SS_BF16 ? go(mx4_quantize_kernel<SS_BF16, WIDE>) : go(mx4_quantize_kernel<SS_F32, WIDE>);
+    };
+    cols >= 8 ? pick(std::true_type{}) : pick(std::false_type{});
     return launched();
 }
 

@@ -1,0 +1,607 @@
+// Norms before and after a block, fused with its gate, its residual scale and the residual sum; and their gradient.
+//
+//     u = post(h)            x_out = x + scale * gate * u            y = norm(x_out) * w + b
+//
+// post and norm: none, LayerNorm or RMS over the channels of a row.  A row lives in the registers of `LPR` lanes, 8 channels to the lane (NV runs of
+// 8 in the widest rows), from its only read to its only write; means and sums of squares are fp32, the variance is the mean square of the
+// differences from the mean.  Bound by memory.
+#ifndef SS_NORM_KERNEL_H_
+#define SS_NORM_KERNEL_H_
+#include "ss_mx4.h"
+#include <algorithm>
+#include <type_traits>
+
+namespace ss {
+
+struct NormArgs {
+    const char *x, *h, *gate;
+    const float *w, *b, *scale, *post_w, *post_b;
+    char *x_out, *y;
+    uint8_t *codes, *scales;
+    long long ldx, ldh, ldx_out, ldy;
+    int rows, cols, gate_cols, norm, post;
+    float eps, post_eps;
+    unsigned g_mul, g_sh;                  // a row's gate: row * g_mul >> g_sh
+};
+
+struct NormGradArgs {
+    const char *dy, *x_out, *dx_out, *h, *gate;
+    const float *w, *scale, *post_w, *post_b;
+    char *dx, *dh, *dgate;
+    float *part, *gate_part;               // [accumulator][workgroup][cols], [group][strip][gate_cols]
+    long long lddy, ldx_out, lddx_out, ldh, lddx, lddh;
+    int rows, cols, gate_cols, norm, post;
+    float eps, post_eps;
+    int groups, per_group, strips, per_strip;
+    bool grouped;                          // a gate of several rows: its gradient is a sum over them
+};
+
+// ---------------------------------------------------------------------------------------------
+// sums over the LPR lanes of a row; every lane gets the sum
+// ---------------------------------------------------------------------------------------------
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)as_bits(v), CTRL, 0xF, 0xF, true));
+}
+
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v += dpp<0xB1>(v);                     // lane ^ 1
+    v += dpp<0x4E>(v);                     // lane ^ 2
+    v += dpp<0x141>(v);                    // the mirror image in 8 lanes
+    v += dpp<0x140>(v);                    // the mirror image in 16
+    if constexpr (LANES >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(as_bits(v), as_bits(v), false, false);
+        v = as_float(p[0]) + as_float(p[1]);
+    }
+    if constexpr (LANES >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(as_bits(v), as_bits(v), false, false);
+        v = as_float(p[0]) + as_float(p[1]);
+    }
+    return v;
+}
+
+// N sums at once.  Rows of several waves join theirs in LDS: `turn` alternates between two places, and a wave that writes one again has
+// passed the barrier of the other, behind everyone's reads of the first.
+template <int LPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*shared)[2][LPR / 64 > 0 ? LPR / 64 : 1], int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = lanes_sum < (LPR < 64 ? LPR : 64) > (v[i]);
+    if constexpr (LPR > 64) {
+        constexpr int WAVES = LPR / 64;
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int i = 0; i < N; i++) shared[turn][i][threadIdx.x % LPR / 64] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            v[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < WAVES; k++) v[i] += shared[turn][i][k];
+        }
+        turn ^= 1;
+    }
+}
+
+// v becomes its normalised row; the factor is returned.  Places past the row stay zero.
+template <int LPR, int NV>
+__device__ __forceinline__ float normalise(float (&v)[NV][8], const int (&n)[NV], int cols, bool layer, float eps, float (*shared)[2][LPR / 64 > 0 ? LPR / 64 : 1],
+                                           int &turn)
+{
+    if (layer) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) s[0] += v[j][e];
+        row_sums<LPR>(s, shared, turn);
+        const float mean = s[0] / (float)cols;
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[j][e] = e < n[j] ? v[j][e] - mean : 0.f;
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) s[0] = __builtin_fmaf(v[j][e], v[j][e], s[0]);
+    row_sums<LPR>(s, shared, turn);
+    const float r = 1.f / sqrtf(s[0] / (float)cols + eps);
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[j][e] = e < n[j] ? v[j][e] * r : 0.f;
+    return r;
+}
+
+// A vector of the channels, or `fill` where there is none.
+template <int NV>
+__device__ __forceinline__ void channel_vector(const float *p, const int (&c)[NV], int cols, float fill, float (&v)[NV][8])
+{
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        if (p != nullptr)
+            load8<SS_F32>(p + c[j], cols - c[j], v[j]);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[j][e] = fill;
+    }
+}
+
+// A run of a row, the way its width allows (WIDE: rows of at least 8 channels).
+template <int DT, bool WIDE>
+__device__ __forceinline__ Run<DT> row_run(const char *row, int c, int n, int cols)
+{
+    if constexpr (WIDE)
+        return load_wide<DT>(row, c, cols);
+    else
+        return load_run<DT>(row + (long long)c * item_bytes<DT>(), n);
+}
+
+template <int DT, bool WIDE>
+__device__ __forceinline__ void row_values(Run<DT> r, int c, int n, int cols, float (&v)[8])
+{
+    if constexpr (WIDE) place_wide<DT>(r, c, cols, n > 0);
+    widen_run<DT>(r, v);
+}
+
+// The next rows are loaded while the current ones are worked on.
+template <int DT, int LPR, int NV, bool MX4, bool POST, bool WIDE>
+__global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
+{
+    constexpr int THREADS = LPR < 256 ? 256 : LPR, R = THREADS / LPR;
+    constexpr int B = item_bytes<DT>();
+    // (rows of 128 lanes: two to the workgroup, each with its own half of the waves)
+    __shared__ float shared_all[R][2][2][LPR / 64 > 0 ? LPR / 64 : 1];
+    auto *shared = shared_all[threadIdx.x / LPR];
+    int turn = 0;
+    const int lane = threadIdx.x % LPR;
+    int c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; j++) c[j] = (j * LPR + lane) * 8;
+    const bool vector_gate = p.gate_cols > 1 || p.cols == 1;
+    Run<DT> nx[NV], nh[NV], ng[NV];
+    float one = 1.f;
+    auto fetch = [&](long long row) {
+        const long long at = min(row, (long long)p.rows - 1);
+        const bool in = row < p.rows;
+#pragma unroll
+        for (int j = 0; j < NV; j++) nx[j] = row_run<DT, WIDE>(p.x + at * p.ldx * B, c[j], in ? p.cols - c[j] : 0, p.cols);
+        if (p.h == nullptr) return;
+#pragma unroll
+        for (int j = 0; j < NV; j++) nh[j] = row_run<DT, WIDE>(p.h + at * p.ldh * B, c[j], in ? p.cols - c[j] : 0, p.cols);
+        if (p.gate == nullptr) return;
+        const long long g = (long long)(((unsigned long long)(unsigned)at * p.g_mul) >> p.g_sh);
+        if (vector_gate) {
+#pragma unroll
+            for (int j = 0; j < NV; j++) ng[j] = row_run<DT, WIDE>(p.gate + g * p.gate_cols * B, c[j], in ? p.cols - c[j] : 0, p.cols);
+        } else {
+            one = load1<DT>(p.gate + g * B);
+        }
+    };
+    fetch((long long)blockIdx.x * R + threadIdx.x / LPR);
+    float w[NV][8], b[NV][8], scale[NV][8], post_w[NV][8], post_b[NV][8];
+    channel_vector<NV>(p.w, c, p.cols, 1.f, w);
+    channel_vector<NV>(p.b, c, p.cols, 0.f, b);
+    channel_vector<NV>(p.scale, c, p.cols, 1.f, scale);
+    if constexpr (POST) {
+        channel_vector<NV>(p.post_w, c, p.cols, 1.f, post_w);
+        channel_vector<NV>(p.post_b, c, p.cols, 0.f, post_b);
+    }
+    for (long long base = (long long)blockIdx.x * R; base < p.rows; base += (long long)gridDim.x * R) {
+        const long long row = base + threadIdx.x / LPR;
+        int n[NV];
+        float v[NV][8], u[NV][8], gate[NV][8];
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            n[j] = row < p.rows ? p.cols - c[j] : 0;
+            row_values<DT, WIDE>(nx[j], c[j], n[j], p.cols, v[j]);
+            if (p.h != nullptr) row_values<DT, WIDE>(nh[j], c[j], n[j], p.cols, u[j]);
+            if (p.gate != nullptr) {
+                if (vector_gate)
+                    row_values<DT, WIDE>(ng[j], c[j], n[j], p.cols, gate[j]);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; e++) gate[j][e] = one;
+            }
+        }
+        fetch(row + (long long)gridDim.x * R);
+        if (p.h != nullptr) {
+            if constexpr (POST) {
+                normalise<LPR, NV>(u, n, p.cols, p.post == SS_NORM_LAYER, p.post_eps, shared, turn);
+#pragma unroll
+                for (int j = 0; j < NV; j++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) u[j][e] = __builtin_fmaf(u[j][e], post_w[j][e], post_b[j][e]);
+            }
+#pragma unroll
+            for (int j = 0; j < NV; j++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    float s = u[j][e] * scale[j][e];
+                    if (p.gate != nullptr) s *= gate[j][e];
+                    v[j][e] = e < n[j] ? v[j][e] + s : 0.f;
+                }
+#pragma unroll
+            for (int j = 0; j < NV; j++) store8<DT>(p.x_out + (row * p.ldx_out + c[j]) * B, n[j], v[j]);
+        }
+        if (p.norm == SS_NORM_NONE) continue;
+        normalise<LPR, NV>(v, n, p.cols, p.norm == SS_NORM_LAYER, p.eps, shared, turn);
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[j][e] = __builtin_fmaf(v[j][e], w[j][e], b[j][e]);
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            if constexpr (MX4) {
+                // four lanes hold a block
+                const int KB = (p.cols + 31) / 32, S = (KB + 3) / 4 * 4, run = c[j] / 8;
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[j][e] = e < n[j] ? v[j][e] : 0.f;
+                const uint32_t byte = mx4_scale(quad_max(magnitude8(v[j])));
+                if (row < p.rows && run < 4 * KB) *reinterpret_cast<uint32_t *>(p.codes + (row * KB * 4 + run) * 4) = mx4_codes8(v[j], byte);
+                if (row < p.rows && run < 4 * S && run % 4 == 0) p.scales[row * S + run / 4] = (uint8_t)byte;
+            } else {
+                store8<DT>(p.y + (row * p.ldy + c[j]) * B, n[j], v[j]);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// gradient
+// ---------------------------------------------------------------------------------------------
+// With xh the normalised row, r its factor and g = dy * w:
+//     t = dx_out + r (g - mean(g) - xh mean(g xh))          (RMS: without mean(g))
+//     dx = t,  dw = sum dy xh,  db = sum dy,  dscale = sum t gate u,  dgate = sum t scale u,  du = t scale gate,  and the same through post.
+// Statistics are found again from the rows, which have to be read anyway.  Sums over rows: a workgroup's own rows in registers, in their order,
+// then its partial sums in the workspace, which norm_grad_sum_kernel adds in a fixed order: the same bits every time.
+enum { ACC_W = 0, ACC_B, ACC_SCALE, ACC_POST_W, ACC_POST_B, ACC_COUNT };
+
+constexpr int grad_threads(int lpr, bool post) { return lpr >= 512 ? lpr : post ? 512 : 256; }
+
+template <int DT, int LPR, int NV, bool POST, bool WIDE>
+__global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3) void norm_grad_kernel(NormGradArgs p)
+{
+    constexpr int THREADS = grad_threads(LPR, POST), R = THREADS / LPR;
+    constexpr int B = item_bytes<DT>();
+    __shared__ float shared_all[R][2][2][LPR / 64 > 0 ? LPR / 64 : 1];
+    __shared__ float joined[R > 1 ? THREADS * 8 : 1];
+    __shared__ float waves[THREADS / 64];
+    auto *shared = shared_all[threadIdx.x / LPR];
+    int turn = 0;
+    const int lane = threadIdx.x % LPR, rg = threadIdx.x / LPR;
+    int c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; j++) c[j] = (j * LPR + lane) * 8;
+    float acc[POST ? ACC_COUNT : ACC_SCALE + 1][NV][8] = {};
+    const float inv = 1.f / (float)p.cols;
+    const bool vector_gate = p.gate != nullptr && (p.gate_cols > 1 || p.cols == 1);
+
+    // sums of the row groups' registers, to dst[0 .. cols)
+    auto join = [&](const float (&v)[NV][8], auto &&put) {
+        if constexpr (R == 1) {
+#pragma unroll
+            for (int j = 0; j < NV; j++)
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (c[j] + e < p.cols) put(c[j] + e, v[j][e]);
+        } else {
+            static_assert(NV == 1, "one run to the lane");
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; e++) joined[rg * LPR * 8 + c[0] + e] = v[0][e];
+            __syncthreads();
+            for (int col = threadIdx.x; col < p.cols; col += THREADS) {
+                float s = 0.f;
+#pragma unroll
+                for (int k = 0; k < R; k++) s += joined[k * LPR * 8 + col];
+                put(col, s);
+            }
+        }
+    };
+
+    // The channels' vectors stay in registers where there is room for them.
+    constexpr bool KEEP = LPR <= 512 && NV == 1;
+    float w[NV][8], scale[NV][8], post_w[NV][8], post_b[NV][8];
+    auto vectors = [&] {
+        channel_vector<NV>(p.w, c, p.cols, 1.f, w);
+        channel_vector<NV>(p.scale, c, p.cols, 1.f, scale);
+        if constexpr (POST) {
+            channel_vector<NV>(p.post_w, c, p.cols, 1.f, post_w);
+            channel_vector<NV>(p.post_b, c, p.cols, 0.f, post_b);
+        }
+    };
+    if constexpr (KEEP) vectors();
+
+    const long long units = (long long)p.groups * p.strips;
+    const long long u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
+    for (long long unit = u0; unit < u1; unit++) {
+        const long long group = unit / p.strips, strip = unit - group * p.strips;
+        const long long first = group * p.per_group + strip * p.per_strip;
+        const long long last = group * p.per_group + min((long long)p.per_group, (strip + 1) * p.per_strip);
+        float gate_acc[NV][8] = {}, gate_one = 0.f;
+        Run<DT> nv[NV], nt[NV], nd[NV], nh[NV], ng[NV];
+        float next_one = 1.f;
+        // the rows from `base` on, which are loaded while the ones before them are worked on
+        auto fetch = [&](long long base) {
+            const long long row = base + rg, at = min(row, last - 1);
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                const int n = row < last ? p.cols - c[j] : 0;
+                if (p.norm != SS_NORM_NONE) {
+                    nv[j] = row_run<DT, WIDE>(p.x_out + at * p.ldx_out * B, c[j], n, p.cols);
+                    nt[j] = row_run<DT, WIDE>(p.dy + at * p.lddy * B, c[j], n, p.cols);
+                }
+                if (p.dx_out != nullptr) nd[j] = row_run<DT, WIDE>(p.dx_out + at * p.lddx_out * B, c[j], n, p.cols);
+                if (p.h != nullptr) nh[j] = row_run<DT, WIDE>(p.h + at * p.ldh * B, c[j], n, p.cols);
+                if (vector_gate) ng[j] = row_run<DT, WIDE>(p.gate + (p.grouped ? group : at) * p.gate_cols * B, c[j], n, p.cols);
+            }
+            if (p.gate != nullptr && !vector_gate) next_one = load1<DT>(p.gate + (p.grouped ? group : at) * B);
+        };
+        if (first < last) fetch(first);
+        for (long long base = first; base < last; base += R) {
+            const long long row = base + rg;
+            const bool in = row < last;
+            if constexpr (!KEEP) vectors();
+            int n[NV];
+            float t[NV][8] = {}, d[NV][8] = {}, hh[NV][8] = {}, v[NV][8], gate[NV][8];
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                n[j] = in ? p.cols - c[j] : 0;
+                if (p.norm != SS_NORM_NONE) {
+                    row_values<DT, WIDE>(nv[j], c[j], n[j], p.cols, v[j]);
+                    row_values<DT, WIDE>(nt[j], c[j], n[j], p.cols, t[j]);
+                }
+                if (p.dx_out != nullptr) row_values<DT, WIDE>(nd[j], c[j], n[j], p.cols, d[j]);
+                if (p.h != nullptr) row_values<DT, WIDE>(nh[j], c[j], n[j], p.cols, hh[j]);
+                if (vector_gate)
+                    row_values<DT, WIDE>(ng[j], c[j], n[j], p.cols, gate[j]);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; e++) gate[j][e] = next_one;
+            }
+            if constexpr (KEEP) fetch(base + R);           // (past the last: the last row again)
+            if (p.norm != SS_NORM_NONE) {
+                const bool layer = p.norm == SS_NORM_LAYER;
+                const float r = normalise<LPR, NV>(v, n, p.cols, layer, p.eps, shared, turn);
+                float s[2] = {0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < NV; j++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        // (values past a row's end are zero, in all of its tensors and in w)
+                        acc[ACC_W][j][e] = __builtin_fmaf(t[j][e], v[j][e], acc[ACC_W][j][e]);
+                        acc[ACC_B][j][e] += t[j][e];
+                        const float g = t[j][e] * w[j][e];
+                        t[j][e] = g;
+                        s[0] += g;
+                        s[1] = __builtin_fmaf(g, v[j][e], s[1]);
+                    }
+                row_sums<LPR>(s, shared, turn);
+                const float m0 = layer ? s[0] * inv : 0.f, m1 = s[1] * inv;
+#pragma unroll
+                for (int j = 0; j < NV; j++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) t[j][e] = e < n[j] ? r * (t[j][e] - m0 - v[j][e] * m1) : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < NV; j++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) t[j][e] += d[j][e];
+#pragma unroll
+            for (int j = 0; j < NV; j++) store8<DT>(p.dx + (row * p.lddx + c[j]) * B, n[j], t[j]);
+            if (p.h != nullptr) {
+                float hr = 0.f;
+                if constexpr (POST) hr = normalise<LPR, NV>(hh, n, p.cols, p.post == SS_NORM_LAYER, p.post_eps, shared, turn);
+                float dg[NV][8], s[2] = {0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < NV; j++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const float u = POST ? __builtin_fmaf(hh[j][e], post_w[j][e], post_b[j][e]) : hh[j][e];
+                        const float tu = t[j][e] * u;
+                        acc[ACC_SCALE][j][e] = __builtin_fmaf(tu, gate[j][e], acc[ACC_SCALE][j][e]);
+                        dg[j][e] = tu * scale[j][e];
+                        const float du = t[j][e] * scale[j][e] * gate[j][e];
+                        if constexpr (POST) {
+                            acc[ACC_POST_W][j][e] = __builtin_fmaf(du, hh[j][e], acc[ACC_POST_W][j][e]);
+                            acc[ACC_POST_B][j][e] += du;
+                            const float gg = du * post_w[j][e];
+                            t[j][e] = gg;
+                            s[0] += gg;
+                            s[1] = __builtin_fmaf(gg, hh[j][e], s[1]);
+                        } else {
+                            t[j][e] = du;
+                        }
+                    }
+                if constexpr (POST) {
+                    row_sums<LPR>(s, shared, turn);
+                    const float m0 = p.post == SS_NORM_LAYER ? s[0] * inv : 0.f, m1 = s[1] * inv;
+#pragma unroll
+                    for (int j = 0; j < NV; j++)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) t[j][e] = hr * (t[j][e] - m0 - hh[j][e] * m1);
+                }
+#pragma unroll
+                for (int j = 0; j < NV; j++) store8<DT>(p.dh + (row * p.lddh + c[j]) * B, n[j], t[j]);
+                if (p.gate != nullptr) {
+                    if (p.grouped) {
+#pragma unroll
+                        for (int j = 0; j < NV; j++)
+#pragma unroll
+                            for (int e = 0; e < 8; e++) {
+                                if (vector_gate) gate_acc[j][e] += dg[j][e];
+                                else gate_one += dg[j][e];
+                            }
+                    } else if (vector_gate) {
+#pragma unroll
+                        for (int j = 0; j < NV; j++) store8<DT>(p.dgate + (row * p.gate_cols + c[j]) * B, n[j], dg[j]);
+                    } else {
+                        float one[1] = {0.f};
+#pragma unroll
+                        for (int j = 0; j < NV; j++)
+#pragma unroll
+                            for (int e = 0; e < 8; e++) one[0] += dg[j][e];
+                        row_sums<LPR>(one, shared, turn);
+                        if (in && lane == 0) store1<DT>(p.dgate + row * B, one[0]);
+                    }
+                }
+            }
+            if constexpr (!KEEP)
+                if (base + R < last) fetch(base + R);
+        }
+        if (p.grouped && p.gate != nullptr) {
+            auto put = [&](int col, float v) {
+                if (p.strips > 1)
+                    p.gate_part[unit * p.gate_cols + col] = v;
+                else
+                    store1<DT>(p.dgate + (group * p.gate_cols + col) * B, v);
+            };
+            if (vector_gate) {
+                join(gate_acc, put);
+            } else {
+                gate_one = lanes_sum<64>(gate_one);
+                __syncthreads();
+                if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = gate_one;
+                __syncthreads();
+                float s = 0.f;
+                for (int k = 0; k < THREADS / 64; k++) s += waves[k];
+                if (threadIdx.x == 0) put(0, s);
+            }
+        }
+    }
+    const size_t at = (size_t)blockIdx.x * p.cols, step = (size_t)gridDim.x * p.cols;
+    auto part = [&](int a, const float (&v)[NV][8]) { join(v, [&](int col, float s) { p.part[a * step + at + col] = s; }); };
+    if (p.norm != SS_NORM_NONE) {
+        part(ACC_W, acc[ACC_W]);
+        part(ACC_B, acc[ACC_B]);
+    }
+    if (p.h != nullptr) part(ACC_SCALE, acc[ACC_SCALE]);
+    if constexpr (POST) {
+        part(ACC_POST_W, acc[ACC_POST_W]);
+        part(ACC_POST_B, acc[ACC_POST_B]);
+    }
+}
+
+struct NormSumArgs {
+    const float *part, *gate_part;
+    float *out[ACC_COUNT];
+    char *dgate;
+    int cols, parts, strips, column_tiles;
+    long long gates;                       // elements of the gate's gradient that are still in `strips` parts, or 0
+    int gate_cols;
+};
+
+// 16 columns to the workgroup, 64 slices of the partial sums; behind those workgroups, one thread for an element of the gate's gradient.
+template <int DT>
+__global__ __launch_bounds__(1024) void norm_grad_sum_kernel(NormSumArgs p)
+{
+    __shared__ float s[64][17];
+    const int tiles = p.column_tiles * ACC_COUNT;
+    if ((int)blockIdx.x < tiles) {
+        const int a = blockIdx.x / p.column_tiles, col = (blockIdx.x - a * p.column_tiles) * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
+        if (p.out[a] == nullptr) return;                 // uniform
+        float v = 0.f;
+        if (col < p.cols) {
+            const float *src = p.part + (size_t)a * p.parts * p.cols + col;
+#pragma unroll 8
+            for (int i = slice; i < p.parts; i += 64) v += src[(size_t)i * p.cols];
+        }
+        s[slice][threadIdx.x % 16] = v;
+        __syncthreads();
+        for (int half = 32; half > 0; half >>= 1) {
+            if (slice < half) s[slice][threadIdx.x % 16] += s[slice + half][threadIdx.x % 16];
+            __syncthreads();
+        }
+        if (slice == 0 && col < p.cols) p.out[a][col] = s[0][threadIdx.x];
+        return;
+    }
+    const long long i = (long long)(blockIdx.x - tiles) * 1024 + threadIdx.x;
+    if (i >= p.gates) return;
+    const long long group = i / p.gate_cols, col = i - group * p.gate_cols;
+    const float *src = p.gate_part + group * p.strips * p.gate_cols + col;
+    float v = 0.f;
+    for (int k = 0; k < p.strips; k++) v += src[(long long)k * p.gate_cols];
+    store1<DT>(p.dgate + i * item_bytes<DT>(), v);
+}
+
+// Lanes of a row (8 channels each), and with 1024 of them two runs to the lane.
+struct RowShape {
+    int lanes, runs;
+};
+inline RowShape row_shape(int cols)
+{
+    int lanes = 16;
+    while (lanes < 1024 && lanes * 8 < cols) lanes *= 2;
+    return {lanes, lanes * 8 < cols ? 2 : 1};
+}
+
+template <int DT>
+void launch_norm(const NormArgs &a, bool mx4, bool post, hipStream_t s)
+{
+    const RowShape shape = row_shape(a.cols);
+    const int threads = shape.lanes < 256 ? 256 : shape.lanes, r = threads / shape.lanes;
+    const int cus = std::max(compute_units(), 1);
+    // (as many workgroups as run at once: four waves to the SIMD with a post norm, five without)
+    const unsigned grid = (unsigned)std::min<long long>(((long long)a.rows + r - 1) / r, (long long)cus * ((post ? 1024 : 1280) / threads));
+    const auto go = [&](auto kern) { kern<<<dim3(grid), dim3(threads), 0, s>>>(a); };
+    const auto pick = [&](auto m, auto ps, auto wd) {
+        constexpr bool MX4 = decltype(m)::value, POST = decltype(ps)::value, WIDE = decltype(wd)::value;
+        switch (shape.lanes) {
+            case 16: go(norm_kernel<DT, 16, 1, MX4, POST, WIDE>); break;
+            case 32: if constexpr (WIDE) go(norm_kernel<DT, 32, 1, MX4, POST, WIDE>); break;
+            case 64: if constexpr (WIDE) go(norm_kernel<DT, 64, 1, MX4, POST, WIDE>); break;
+            case 128: if constexpr (WIDE) go(norm_kernel<DT, 128, 1, MX4, POST, WIDE>); break;
+            case 256: if constexpr (WIDE) go(norm_kernel<DT, 256, 1, MX4, POST, WIDE>); break;
+            case 512: if constexpr (WIDE) go(norm_kernel<DT, 512, 1, MX4, POST, WIDE>); break;
+            default:
+                if constexpr (WIDE) shape.runs == 1 ? go(norm_kernel<DT, 1024, 1, MX4, POST, WIDE>) : go(norm_kernel<DT, 1024, 2, MX4, POST, WIDE>);
+        }
+    };
+    const auto wide = [&](auto m, auto ps) { a.cols >= 8 ? pick(m, ps, std::true_type{}) : pick(m, ps, std::false_type{}); };
+    const auto posts = [&](auto m) { post ? wide(m, std::true_type{}) : wide(m, std::false_type{}); };
+    mx4 ? posts(std::true_type{}) : posts(std::false_type{});
+}
+
+template <int DT>
+void launch_norm_grad(const NormGradArgs &a, bool post, int workgroups, hipStream_t s)
+{
+    const RowShape shape = row_shape(a.cols);
+    const auto go = [&](auto kern) { kern<<<dim3(workgroups), dim3(grad_threads(shape.lanes, post)), 0, s>>>(a); };
+    const auto pick = [&](auto ps, auto wd) {
+        constexpr bool POST = decltype(ps)::value, WIDE = decltype(wd)::value;
+        switch (shape.lanes) {
+            case 16: go(norm_grad_kernel<DT, 16, 1, POST, WIDE>); break;
+            case 32: if constexpr (WIDE) go(norm_grad_kernel<DT, 32, 1, POST, WIDE>); break;
+            case 64: if constexpr (WIDE) go(norm_grad_kernel<DT, 64, 1, POST, WIDE>); break;
+            case 128: if constexpr (WIDE) go(norm_grad_kernel<DT, 128, 1, POST, WIDE>); break;
+            case 256: if constexpr (WIDE) go(norm_grad_kernel<DT, 256, 1, POST, WIDE>); break;
+            case 512: if constexpr (WIDE) go(norm_grad_kernel<DT, 512, 1, POST, WIDE>); break;
+            default: if constexpr (WIDE) shape.runs == 1 ? go(norm_grad_kernel<DT, 1024, 1, POST, WIDE>) : go(norm_grad_kernel<DT, 1024, 2, POST, WIDE>);
+        }
+    };
+    const auto wide = [&](auto ps) { a.cols >= 8 ? pick(ps, std::true_type{}) : pick(ps, std::false_type{}); };
+    post ? wide(std::true_type{}) : wide(std::false_type{});
+}
+
+template <int DT>
+void launch_norm_sum(const NormSumArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.column_tiles * ACC_COUNT + (a.gates + 1023) / 1024)), block(1024);
+    norm_grad_sum_kernel<DT><<<grid, block, 0, s>>>(a);
+}
+
+// (one translation unit to the type, ss_norm_*.hip, instantiates these)
+#define SS_NORM_LAUNCHES(X, DT)                                                  \
+    X template void launch_norm<DT>(const NormArgs &, bool, bool, hipStream_t);  \
+    X template void launch_norm_grad<DT>(const NormGradArgs &, bool, int, hipStream_t); \
+    X template void launch_norm_sum<DT>(const NormSumArgs &, hipStream_t);
+
+}  // namespace ss
+
+#endif

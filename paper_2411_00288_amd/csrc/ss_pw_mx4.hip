@@ -272,9 +272,9 @@ __device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x
 }
 
 // 16-bit input rows of a workgroup, quantised into LDS.  Block b of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
-// pieces, and with an odd `pad` the quads of a row's neighbouring blocks write to different banks.  WHOLE: K is a multiple of 8.  The scale of b = 8 q + 2 s + half is byte s of word
+// pieces, and with an odd `pad` the quads of a row's neighbouring blocks write to different banks.  WIDE: K is at least 8.  The scale of b = 8 q + 2 s + half is byte s of word
 // (q * 2 + half) * pad + r, the four steps of a lane.  Blocks 0 .. 2 Ks - 1, rows 0 .. count - 1; what is past the matrix is zero.
-template <int DT, int THREADS, int U, bool WHOLE>
+template <int DT, int THREADS, int U, bool WIDE>
 __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, int rows, int count, int K, int Ks, int pad, unsigned mul, unsigned sh, uint8_t *codes_s,
                                               uint8_t *scales_s)
 {
@@ -287,9 +287,8 @@ __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, 
             const int i = base + u * THREADS + (int)threadIdx.x;
             row[u] = (int)(((unsigned long long)(unsigned)i * mul) >> sh);
             run[u] = i - row[u] * runs;
-            if constexpr (WHOLE) {                         // (one load, from inside the matrix, whatever the lane: no branches between the loads)
-                raw[u].v[0] = reinterpret_cast<const Vec16 *>(x + min(row[u], rows - 1) * ldx + min(run[u] * 8, K - 8))->v;
-                if (row[u] >= rows || run[u] * 8 >= K) raw[u].v[0] = u32x4{};
+            if constexpr (WIDE) {
+                raw[u] = load_wide<DT>(x + min(row[u], rows - 1) * ldx, run[u] * 8, K);
             } else {
                 raw[u] = load_run<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0);
             }
@@ -297,6 +296,7 @@ __device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, 
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int b = run[u] / 4;
+            if constexpr (WIDE) place_wide<DT>(raw[u], run[u] * 8, K, row[u] < rows);
             const uint32_t byte = mx4_scale(quad_max(magnitude<DT>(raw[u])));
             const uint32_t c = mx4_codes<DT>(raw[u], byte);
             if (base + u * THREADS + (int)threadIdx.x >= total) continue;
@@ -316,7 +316,7 @@ struct PwRowsArgs {
 // in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels.  The next
 // weights are on their way from the L2 while the current ones are multiplied or, with a reduction of one chunk (SHORT), while the sums are finished: that
 // is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
-template <int DT, int NT, bool SHORT, bool WHOLE>
+template <int DT, int NT, bool SHORT, bool WIDE>
 __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
         fetch(min(wave / NT * 2, Mt - 1), 0, wa, sa);
     else
         fetch(min(wave / NT * 2, Mt - 1), 0, wn, sn);
-    quantise_rows<DT, 256, SHORT ? 4 : 8, WHOLE>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
+    quantise_rows<DT, 256, SHORT ? 4 : 8, WIDE>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
     __syncthreads();
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
     // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us).
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
 // the reduction, a chunk each in turn, and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first
 // weights are on their way.
-template <int DT, int NW, int NI, bool QUANT, bool WHOLE>
+template <int DT, int NW, int NI, bool QUANT, bool WIDE>
 __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArg
     weights(wave + NW, wn, sn);
     uint8_t *const scales_s = smem + 2 * Ks * pad * 16;
     if constexpr (QUANT) {
-        quantise_rows<DT, NW * 64, 8, WHOLE>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
+        quantise_rows<DT, NW * 64, 8, WIDE>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
         __syncthreads();
     }
     f32x16 acc[1][NI] = {};
@@ -624,24 +624,24 @@ int product16(const PwArgs &a, const Mx4Dims &t, const PwPlan &plan, const void 
 {
     PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0};
     fast_div_setup((unsigned)t.Ks * 8u, &r.mul, &r.sh);
-    const auto go = [&](auto whole) -> int {
-        constexpr bool WHOLE = decltype(whole)::value;
+    const auto go = [&](auto wide) -> int {
+        constexpr bool WIDE = decltype(wide)::value;
         if (plan.kind == KIND_FEW) {
-            if (t.Kq <= 4) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true, WHOLE>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
-            if (t.Kq <= 8) return launch_lds<pw_mx4_few_kernel<DT, 8, 1, true, WHOLE>>(t.Mt, 512, few_lds(t, 8, a.P), s, a, r);
-            return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true, WHOLE>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
+            if (t.Kq <= 4) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true, WIDE>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
+            if (t.Kq <= 8) return launch_lds<pw_mx4_few_kernel<DT, 8, 1, true, WIDE>>(t.Mt, 512, few_lds(t, 8, a.P), s, a, r);
+            return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true, WIDE>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
         }
         const long long blocks = ((long long)a.P + plan.px - 1) / plan.px;
         const auto rows = [&](auto nt, auto brief) -> int {
             constexpr int NT = decltype(nt)::value;
-            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WHOLE>>(blocks, 256, rows_lds(t, 32 * NT), s, a, r);
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(blocks, 256, rows_lds(t, 32 * NT), s, a, r);
         };
         using One = std::integral_constant<int, 1>;
         using Two = std::integral_constant<int, 2>;
         if (t.Kq == 1) return plan.px == 128 ? rows(std::integral_constant<int, 4>{}, std::true_type{}) : rows(One{}, std::true_type{});
         return plan.px == 64 ? rows(Two{}, std::false_type{}) : rows(One{}, std::false_type{});
     };
-    return a.K % 8 == 0 ? go(std::true_type{}) : go(std::false_type{});
+    return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
 }
 
 int product(const ss_weight_desc *d, PwArgs a, const uint8_t *codes, const uint8_t *scales, hipStream_t s)

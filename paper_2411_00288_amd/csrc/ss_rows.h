@@ -63,6 +63,49 @@ __device__ __forceinline__ Run<DT> load_run(const void *p, int n)
     return r;
 }
 
+// Channels c .. c + 7 of a row of at least 8: one load from inside the row whatever the lane, so that loads follow each other without a branch between them.
+// place_wide then moves what a lane at the row's end got into place.
+template <int DT>
+__device__ __forceinline__ Run<DT> load_wide(const void *row, int c, int cols)
+{
+    const char *const p = static_cast<const char *>(row) + (long long)min(c, cols - 8) * item_bytes<DT>();
+    Run<DT> r;
+    if constexpr (DT == SS_F32) {
+        r.v[0] = reinterpret_cast<const Vec32 *>(p)[0].v;
+        r.v[1] = reinterpret_cast<const Vec32 *>(p)[1].v;
+    } else {
+        r.v[0] = reinterpret_cast<const Vec16 *>(p)->v;
+    }
+    return r;
+}
+
+// What load_wide read, with zeros past the row's end, and everywhere where the row is not `active`.
+template <int DT>
+__device__ __forceinline__ void place_wide(Run<DT> &r, int c, int cols, bool active)
+{
+    constexpr int N = DT == SS_F32 ? 2 : 1;
+    if (c + 8 <= cols && active) return;
+    const int by = c + 8 - cols;                           // (8 and more: nothing is left)
+    uint32_t w[4 * N + 4];
+#pragma unroll
+    for (int e = 0; e < 4 * N; e++) w[e] = r.v[e / 4][e % 4];
+#pragma unroll
+    for (int e = 4 * N; e < 4 * N + 4; e++) w[e] = 0;
+    constexpr int UNIT = DT == SS_F32 ? 1 : 2;             // elements of a word
+#pragma unroll
+    for (int step = 4; step >= UNIT; step /= 2)
+        if (by & step) {
+#pragma unroll
+            for (int e = 0; e < 4 * N; e++) w[e] = w[e + step / UNIT];
+        }
+    if (UNIT == 2 && (by & 1)) {
+#pragma unroll
+        for (int e = 0; e < 4 * N; e++) w[e] = (w[e] >> 16) | (w[e + 1] << 16);
+    }
+#pragma unroll
+    for (int e = 0; e < 4 * N; e++) r.v[e / 4][e % 4] = active && by < 8 ? w[e] : 0u;
+}
+
 template <int DT>
 __device__ __forceinline__ void widen_run(const Run<DT> &r, float (&v)[8])
 {
