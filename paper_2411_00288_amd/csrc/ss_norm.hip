@@ -28,7 +28,9 @@ GradPlan grad_plan(const ss_norm_desc &d, long long rows, long long groups, int 
     const RowShape shape = row_shape(d.cols);
     const int threads = grad_threads(shape.lanes, d.post != SS_NORM_NONE), r = threads / shape.lanes;
     const long long cus = std::max(compute_units(), 1);
-    const long long most = std::min(std::max(64ll, rows / 8), cus * std::max(1, 768 / threads));
+    const bool post = d.post != SS_NORM_NONE;
+    const int resident = post ? 512 : 256 * grad_waves(d.dtype, gate_cols > 1);          // threads of a compute unit
+    const long long most = std::min(std::max(64ll, rows / 8), cus * std::max(1, resident / threads));
     const long long target = std::max(1ll, std::min((rows + r - 1) / r, most));
     g.grouped = gate_cols > 0 && groups < rows;
     g.groups = g.grouped ? (int)groups : 1;

@@ -86,10 +86,34 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*shared)[2][LPR /
     }
 }
 
-// v becomes its normalised row; the factor is returned.  Places past the row stay zero.
-template <int LPR, int NV>
-__device__ __forceinline__ float normalise(float (&v)[NV][8], const int (&n)[NV], int cols, bool layer, float eps, float (*shared)[2][LPR / 64 > 0 ? LPR / 64 : 1],
-                                           int &turn)
+// How a row's width meets the lanes' runs of 8: narrower than one, with a last run that is cut, or even.
+enum { NARROW = 0, CUT = 1, EVEN = 2 };
+
+// One for a channel of the row, zero past its end.  (As a factor: values past the end are loaded as zeros, and what is subtracted from them is multiplied by
+// this, so that they stay zeros without a comparison.)
+template <int NV, int MODE>
+struct Inside {
+    float v[NV][MODE == EVEN ? 1 : 8];
+    __device__ __forceinline__ Inside(const int (&c)[NV], int cols)
+    {
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int e = 0; e < (MODE == EVEN ? 1 : 8); e++) v[j][e] = c[j] + e < cols ? 1.f : 0.f;
+    }
+    __device__ __forceinline__ float at(int j, int e) const { return v[j][MODE == EVEN ? 0 : e]; }
+};
+
+// 1 / sqrt(q), within two units in the last place.  (The instruction alone takes no denormal numbers.)
+__device__ __forceinline__ float reciprocal_root(float q)
+{
+    return q > 1e-36f ? __builtin_amdgcn_rsqf(q) : 1.f / sqrtf(q);
+}
+
+// v becomes its normalised row; the factor is returned.  `in`: the row is one; otherwise its values are zero and so is the factor.
+template <int LPR, int NV, int MODE>
+__device__ __forceinline__ float normalise(float (&v)[NV][8], const Inside<NV, MODE> &inside, float inv, bool layer, float eps, bool in,
+                                           float (*shared)[2][LPR / 64 > 0 ? LPR / 64 : 1], int &turn)
 {
     if (layer) {
         float s[1] = {0.f};
@@ -98,11 +122,20 @@ __device__ __forceinline__ float normalise(float (&v)[NV][8], const int (&n)[NV]
 #pragma unroll
             for (int e = 0; e < 8; e++) s[0] += v[j][e];
         row_sums<LPR>(s, shared, turn);
-        const float mean = s[0] / (float)cols;
+        const float mean = s[0] * inv;
+        if constexpr (MODE == EVEN) {
 #pragma unroll
-        for (int j = 0; j < NV; j++)
+            for (int j = 0; j < NV; j++) {
+                const float m = mean * inside.at(j, 0);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[j][e] = e < n[j] ? v[j][e] - mean : 0.f;
+                for (int e = 0; e < 8; e++) v[j][e] -= m;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; j++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[j][e] = __builtin_fmaf(-mean, inside.at(j, e), v[j][e]);
+        }
     }
     float s[1] = {0.f};
 #pragma unroll
@@ -110,15 +143,15 @@ __device__ __forceinline__ float normalise(float (&v)[NV][8], const int (&n)[NV]
 #pragma unroll
         for (int e = 0; e < 8; e++) s[0] = __builtin_fmaf(v[j][e], v[j][e], s[0]);
     row_sums<LPR>(s, shared, turn);
-    const float r = 1.f / sqrtf(s[0] / (float)cols + eps);
+    const float r = in ? reciprocal_root(__builtin_fmaf(s[0], inv, eps)) : 0.f;
 #pragma unroll
     for (int j = 0; j < NV; j++)
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[j][e] = e < n[j] ? v[j][e] * r : 0.f;
+        for (int e = 0; e < 8; e++) v[j][e] *= r;
     return r;
 }
 
-// A vector of the channels, or `fill` where there is none.
+// A vector of the channels, or `fill` where there is none; zero past the row's end.
 template <int NV>
 __device__ __forceinline__ void channel_vector(const float *p, const int (&c)[NV], int cols, float fill, float (&v)[NV][8])
 {
@@ -128,29 +161,33 @@ __device__ __forceinline__ void channel_vector(const float *p, const int (&c)[NV
             load8<SS_F32>(p + c[j], cols - c[j], v[j]);
         else
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[j][e] = fill;
+            for (int e = 0; e < 8; e++) v[j][e] = c[j] + e < cols ? fill : 0.f;
     }
 }
 
-// A run of a row, the way its width allows (WIDE: rows of at least 8 channels).
-template <int DT, bool WIDE>
+// A run of a row, the way its width allows.
+template <int DT, int MODE>
 __device__ __forceinline__ Run<DT> row_run(const char *row, int c, int n, int cols)
 {
-    if constexpr (WIDE)
+    if constexpr (MODE != NARROW)
         return load_wide<DT>(row, c, cols);
     else
         return load_run<DT>(row + (long long)c * item_bytes<DT>(), n);
 }
 
-template <int DT, bool WIDE>
+template <int DT, int MODE>
 __device__ __forceinline__ void row_values(Run<DT> r, int c, int n, int cols, float (&v)[8])
 {
-    if constexpr (WIDE) place_wide<DT>(r, c, cols, n > 0);
+    if constexpr (MODE == CUT) place_wide<DT>(r, c, cols, n > 0);
+    if constexpr (MODE == EVEN) {
+#pragma unroll
+        for (int k = 0; k < (DT == SS_F32 ? 2 : 1); k++) r.v[k] = n > 0 ? r.v[k] : u32x4{};
+    }
     widen_run<DT>(r, v);
 }
 
 // The next rows are loaded while the current ones are worked on.
-template <int DT, int LPR, int NV, bool MX4, bool POST, bool WIDE>
+template <int DT, int LPR, int NV, bool MX4, bool POST, int MODE>
 __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
 {
     constexpr int THREADS = LPR < 256 ? 256 : LPR, R = THREADS / LPR;
@@ -164,21 +201,23 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
 #pragma unroll
     for (int j = 0; j < NV; j++) c[j] = (j * LPR + lane) * 8;
     const bool vector_gate = p.gate_cols > 1 || p.cols == 1;
+    const Inside<NV, MODE> inside(c, p.cols);
+    const float inv = 1.f / (float)p.cols;
     Run<DT> nx[NV], nh[NV], ng[NV];
     float one = 1.f;
     auto fetch = [&](long long row) {
         const long long at = min(row, (long long)p.rows - 1);
         const bool in = row < p.rows;
 #pragma unroll
-        for (int j = 0; j < NV; j++) nx[j] = row_run<DT, WIDE>(p.x + at * p.ldx * B, c[j], in ? p.cols - c[j] : 0, p.cols);
+        for (int j = 0; j < NV; j++) nx[j] = row_run<DT, MODE>(p.x + at * p.ldx * B, c[j], in ? p.cols - c[j] : 0, p.cols);
         if (p.h == nullptr) return;
 #pragma unroll
-        for (int j = 0; j < NV; j++) nh[j] = row_run<DT, WIDE>(p.h + at * p.ldh * B, c[j], in ? p.cols - c[j] : 0, p.cols);
+        for (int j = 0; j < NV; j++) nh[j] = row_run<DT, MODE>(p.h + at * p.ldh * B, c[j], in ? p.cols - c[j] : 0, p.cols);
         if (p.gate == nullptr) return;
         const long long g = (long long)(((unsigned long long)(unsigned)at * p.g_mul) >> p.g_sh);
         if (vector_gate) {
 #pragma unroll
-            for (int j = 0; j < NV; j++) ng[j] = row_run<DT, WIDE>(p.gate + g * p.gate_cols * B, c[j], in ? p.cols - c[j] : 0, p.cols);
+            for (int j = 0; j < NV; j++) ng[j] = row_run<DT, MODE>(p.gate + g * p.gate_cols * B, c[j], in ? p.cols - c[j] : 0, p.cols);
         } else {
             one = load1<DT>(p.gate + g * B);
         }
@@ -199,11 +238,11 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             n[j] = row < p.rows ? p.cols - c[j] : 0;
-            row_values<DT, WIDE>(nx[j], c[j], n[j], p.cols, v[j]);
-            if (p.h != nullptr) row_values<DT, WIDE>(nh[j], c[j], n[j], p.cols, u[j]);
+            row_values<DT, MODE>(nx[j], c[j], n[j], p.cols, v[j]);
+            if (p.h != nullptr) row_values<DT, MODE>(nh[j], c[j], n[j], p.cols, u[j]);
             if (p.gate != nullptr) {
                 if (vector_gate)
-                    row_values<DT, WIDE>(ng[j], c[j], n[j], p.cols, gate[j]);
+                    row_values<DT, MODE>(ng[j], c[j], n[j], p.cols, gate[j]);
                 else
 #pragma unroll
                     for (int e = 0; e < 8; e++) gate[j][e] = one;
@@ -212,7 +251,7 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
         fetch(row + (long long)gridDim.x * R);
         if (p.h != nullptr) {
             if constexpr (POST) {
-                normalise<LPR, NV>(u, n, p.cols, p.post == SS_NORM_LAYER, p.post_eps, shared, turn);
+                normalise<LPR, NV, MODE>(u, inside, inv, p.post == SS_NORM_LAYER, p.post_eps, row < p.rows, shared, turn);
 #pragma unroll
                 for (int j = 0; j < NV; j++)
 #pragma unroll
@@ -222,15 +261,16 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
             for (int j = 0; j < NV; j++)
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
+                    // (past the row's end u is zero: post_w and post_b are)
                     float s = u[j][e] * scale[j][e];
                     if (p.gate != nullptr) s *= gate[j][e];
-                    v[j][e] = e < n[j] ? v[j][e] + s : 0.f;
+                    v[j][e] += s;
                 }
 #pragma unroll
             for (int j = 0; j < NV; j++) store8<DT>(p.x_out + (row * p.ldx_out + c[j]) * B, n[j], v[j]);
         }
         if (p.norm == SS_NORM_NONE) continue;
-        normalise<LPR, NV>(v, n, p.cols, p.norm == SS_NORM_LAYER, p.eps, shared, turn);
+        normalise<LPR, NV, MODE>(v, inside, inv, p.norm == SS_NORM_LAYER, p.eps, row < p.rows, shared, turn);
 #pragma unroll
         for (int j = 0; j < NV; j++)
 #pragma unroll
@@ -262,10 +302,12 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
 // then its partial sums in the workspace, which norm_grad_sum_kernel adds in a fixed order: the same bits every time.
 enum { ACC_W = 0, ACC_B, ACC_SCALE, ACC_POST_W, ACC_POST_B, ACC_COUNT };
 
+// Waves to the SIMD: what the registers of a kernel without post norm leave.
+constexpr int grad_waves(int dt, bool vector_gate) { return dt == SS_F32 || vector_gate ? 3 : 4; }
 constexpr int grad_threads(int lpr, bool post) { return lpr >= 512 ? lpr : post ? 512 : 256; }
 
-template <int DT, int LPR, int NV, bool POST, bool WIDE>
-__global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3) void norm_grad_kernel(NormGradArgs p)
+template <int DT, int LPR, int NV, bool POST, bool VECTOR_GATE, int MODE>
+__global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : grad_waves(DT, VECTOR_GATE)) void norm_grad_kernel(NormGradArgs p)
 {
     constexpr int THREADS = grad_threads(LPR, POST), R = THREADS / LPR;
     constexpr int B = item_bytes<DT>();
@@ -280,7 +322,7 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3
     for (int j = 0; j < NV; j++) c[j] = (j * LPR + lane) * 8;
     float acc[POST ? ACC_COUNT : ACC_SCALE + 1][NV][8] = {};
     const float inv = 1.f / (float)p.cols;
-    const bool vector_gate = p.gate != nullptr && (p.gate_cols > 1 || p.cols == 1);
+    const Inside<NV, MODE> inside(c, p.cols);
 
     // sums of the row groups' registers, to dst[0 .. cols)
     auto join = [&](const float (&v)[NV][8], auto &&put) {
@@ -324,24 +366,19 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3
         const long long group = unit / p.strips, strip = unit - group * p.strips;
         const long long first = group * p.per_group + strip * p.per_strip;
         const long long last = group * p.per_group + min((long long)p.per_group, (strip + 1) * p.per_strip);
-        float gate_acc[NV][8] = {}, gate_one = 0.f;
-        Run<DT> nv[NV], nt[NV], nd[NV], nh[NV], ng[NV];
-        float next_one = 1.f;
-        // the rows from `base` on, which are loaded while the ones before them are worked on
+        float gate_acc[VECTOR_GATE ? NV : 1][8] = {}, gate_one = 0.f;
+        Run<DT> nv[NV], nt[NV];
+        // What the sums begin with is loaded while the rows before are worked on; what comes behind them, at their start.  (All of it ahead took more registers
+        // than four waves have: 134 -> 156 us.)
         auto fetch = [&](long long base) {
             const long long row = base + rg, at = min(row, last - 1);
+            if (p.norm != SS_NORM_NONE)
 #pragma unroll
-            for (int j = 0; j < NV; j++) {
-                const int n = row < last ? p.cols - c[j] : 0;
-                if (p.norm != SS_NORM_NONE) {
-                    nv[j] = row_run<DT, WIDE>(p.x_out + at * p.ldx_out * B, c[j], n, p.cols);
-                    nt[j] = row_run<DT, WIDE>(p.dy + at * p.lddy * B, c[j], n, p.cols);
+                for (int j = 0; j < NV; j++) {
+                    const int n = row < last ? p.cols - c[j] : 0;
+                    nv[j] = row_run<DT, MODE>(p.x_out + at * p.ldx_out * B, c[j], n, p.cols);
+                    nt[j] = row_run<DT, MODE>(p.dy + at * p.lddy * B, c[j], n, p.cols);
                 }
-                if (p.dx_out != nullptr) nd[j] = row_run<DT, WIDE>(p.dx_out + at * p.lddx_out * B, c[j], n, p.cols);
-                if (p.h != nullptr) nh[j] = row_run<DT, WIDE>(p.h + at * p.ldh * B, c[j], n, p.cols);
-                if (vector_gate) ng[j] = row_run<DT, WIDE>(p.gate + (p.grouped ? group : at) * p.gate_cols * B, c[j], n, p.cols);
-            }
-            if (p.gate != nullptr && !vector_gate) next_one = load1<DT>(p.gate + (p.grouped ? group : at) * B);
         };
         if (first < last) fetch(first);
         for (long long base = first; base < last; base += R) {
@@ -349,26 +386,26 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3
             const bool in = row < last;
             if constexpr (!KEEP) vectors();
             int n[NV];
-            float t[NV][8] = {}, d[NV][8] = {}, hh[NV][8] = {}, v[NV][8], gate[NV][8];
+            float t[NV][8] = {}, v[NV][8], one = 1.f;
+            Run<DT> rd[NV], rh[NV], rgate[VECTOR_GATE ? NV : 1];
+            const long long at = min(row, last - 1), g = p.grouped ? group : at;
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 n[j] = in ? p.cols - c[j] : 0;
+                rd[j] = rh[j] = Run<DT>{};
                 if (p.norm != SS_NORM_NONE) {
-                    row_values<DT, WIDE>(nv[j], c[j], n[j], p.cols, v[j]);
-                    row_values<DT, WIDE>(nt[j], c[j], n[j], p.cols, t[j]);
+                    row_values<DT, MODE>(nv[j], c[j], n[j], p.cols, v[j]);
+                    row_values<DT, MODE>(nt[j], c[j], n[j], p.cols, t[j]);
                 }
-                if (p.dx_out != nullptr) row_values<DT, WIDE>(nd[j], c[j], n[j], p.cols, d[j]);
-                if (p.h != nullptr) row_values<DT, WIDE>(nh[j], c[j], n[j], p.cols, hh[j]);
-                if (vector_gate)
-                    row_values<DT, WIDE>(ng[j], c[j], n[j], p.cols, gate[j]);
-                else
-#pragma unroll
-                    for (int e = 0; e < 8; e++) gate[j][e] = next_one;
+                if (p.dx_out != nullptr) rd[j] = row_run<DT, MODE>(p.dx_out + at * p.lddx_out * B, c[j], n[j], p.cols);
+                if (p.h != nullptr) rh[j] = row_run<DT, MODE>(p.h + at * p.ldh * B, c[j], n[j], p.cols);
+                if constexpr (VECTOR_GATE) rgate[j] = row_run<DT, MODE>(p.gate + g * p.gate_cols * B, c[j], n[j], p.cols);
             }
+            if (!VECTOR_GATE && p.gate != nullptr) one = load1<DT>(p.gate + g * B);
             if constexpr (KEEP) fetch(base + R);           // (past the last: the last row again)
             if (p.norm != SS_NORM_NONE) {
                 const bool layer = p.norm == SS_NORM_LAYER;
-                const float r = normalise<LPR, NV>(v, n, p.cols, layer, p.eps, shared, turn);
+                const float r = normalise<LPR, NV, MODE>(v, inside, inv, layer, p.eps, in, shared, turn);
                 float s[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < NV; j++)
@@ -387,27 +424,41 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3
 #pragma unroll
                 for (int j = 0; j < NV; j++)
 #pragma unroll
-                    for (int e = 0; e < 8; e++) t[j][e] = e < n[j] ? r * (t[j][e] - m0 - v[j][e] * m1) : 0.f;
+                    for (int e = 0; e < 8; e++) t[j][e] = r * __builtin_fmaf(-v[j][e], m1, __builtin_fmaf(-m0, inside.at(j, e), t[j][e]));
             }
+            if (p.dx_out != nullptr) {
 #pragma unroll
-            for (int j = 0; j < NV; j++)
+                for (int j = 0; j < NV; j++) {
+                    float d[8];
+                    row_values<DT, MODE>(rd[j], c[j], n[j], p.cols, d);
 #pragma unroll
-                for (int e = 0; e < 8; e++) t[j][e] += d[j][e];
+                    for (int e = 0; e < 8; e++) t[j][e] += d[e];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < NV; j++) store8<DT>(p.dx + (row * p.lddx + c[j]) * B, n[j], t[j]);
             if (p.h != nullptr) {
-                float hr = 0.f;
-                if constexpr (POST) hr = normalise<LPR, NV>(hh, n, p.cols, p.post == SS_NORM_LAYER, p.post_eps, shared, turn);
-                float dg[NV][8], s[2] = {0.f, 0.f};
+                float hr = 0.f, hh[NV][8], gate[VECTOR_GATE ? NV : 1][8];
+#pragma unroll
+                for (int j = 0; j < NV; j++) {
+                    row_values<DT, MODE>(rh[j], c[j], n[j], p.cols, hh[j]);
+                    if constexpr (VECTOR_GATE) row_values<DT, MODE>(rgate[j], c[j], n[j], p.cols, gate[j]);
+                }
+                if constexpr (POST) hr = normalise<LPR, NV, MODE>(hh, inside, inv, p.post == SS_NORM_LAYER, p.post_eps, in, shared, turn);
+                float dg[VECTOR_GATE ? NV : 1][8], dg_one = 0.f, s[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < NV; j++)
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
                         const float u = POST ? __builtin_fmaf(hh[j][e], post_w[j][e], post_b[j][e]) : hh[j][e];
-                        const float tu = t[j][e] * u;
-                        acc[ACC_SCALE][j][e] = __builtin_fmaf(tu, gate[j][e], acc[ACC_SCALE][j][e]);
-                        dg[j][e] = tu * scale[j][e];
-                        const float du = t[j][e] * scale[j][e] * gate[j][e];
+                        const float tu = t[j][e] * u, ts = t[j][e] * scale[j][e];
+                        const float g = VECTOR_GATE ? gate[VECTOR_GATE ? j : 0][e] : one;
+                        acc[ACC_SCALE][j][e] = __builtin_fmaf(tu, g, acc[ACC_SCALE][j][e]);
+                        if constexpr (VECTOR_GATE)
+                            dg[j][e] = ts * u;
+                        else
+                            dg_one = __builtin_fmaf(ts, u, dg_one);
+                        const float du = ts * g;
                         if constexpr (POST) {
                             acc[ACC_POST_W][j][e] = __builtin_fmaf(du, hh[j][e], acc[ACC_POST_W][j][e]);
                             acc[ACC_POST_B][j][e] += du;
@@ -425,30 +476,27 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3
 #pragma unroll
                     for (int j = 0; j < NV; j++)
 #pragma unroll
-                        for (int e = 0; e < 8; e++) t[j][e] = hr * (t[j][e] - m0 - hh[j][e] * m1);
+                        for (int e = 0; e < 8; e++) t[j][e] = hr * __builtin_fmaf(-hh[j][e], m1, __builtin_fmaf(-m0, inside.at(j, e), t[j][e]));
                 }
 #pragma unroll
                 for (int j = 0; j < NV; j++) store8<DT>(p.dh + (row * p.lddh + c[j]) * B, n[j], t[j]);
-                if (p.gate != nullptr) {
+                if constexpr (VECTOR_GATE) {
+#pragma unroll
+                    for (int j = 0; j < NV; j++) {
+                        if (p.grouped) {
+#pragma unroll
+                            for (int e = 0; e < 8; e++) gate_acc[j][e] += dg[j][e];
+                        } else {
+                            store8<DT>(p.dgate + (row * p.gate_cols + c[j]) * B, n[j], dg[j]);
+                        }
+                    }
+                } else if (p.gate != nullptr) {
                     if (p.grouped) {
-#pragma unroll
-                        for (int j = 0; j < NV; j++)
-#pragma unroll
-                            for (int e = 0; e < 8; e++) {
-                                if (vector_gate) gate_acc[j][e] += dg[j][e];
-                                else gate_one += dg[j][e];
-                            }
-                    } else if (vector_gate) {
-#pragma unroll
-                        for (int j = 0; j < NV; j++) store8<DT>(p.dgate + (row * p.gate_cols + c[j]) * B, n[j], dg[j]);
+                        gate_one += dg_one;
                     } else {
-                        float one[1] = {0.f};
-#pragma unroll
-                        for (int j = 0; j < NV; j++)
-#pragma unroll
-                            for (int e = 0; e < 8; e++) one[0] += dg[j][e];
-                        row_sums<LPR>(one, shared, turn);
-                        if (in && lane == 0) store1<DT>(p.dgate + row * B, one[0]);
+                        float sum[1] = {dg_one};
+                        row_sums<LPR>(sum, shared, turn);
+                        if (in && lane == 0) store1<DT>(p.dgate + row * B, sum[0]);
                     }
                 }
             }
@@ -462,7 +510,7 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : 3
                 else
                     store1<DT>(p.dgate + (group * p.gate_cols + col) * B, v);
             };
-            if (vector_gate) {
+            if constexpr (VECTOR_GATE) {
                 join(gate_acc, put);
             } else {
                 gate_one = lanes_sum<64>(gate_one);
@@ -541,6 +589,8 @@ inline RowShape row_shape(int cols)
     return {lanes, lanes * 8 < cols ? 2 : 1};
 }
 
+template <int M> using Mode = std::integral_constant<int, M>;
+
 template <int DT>
 void launch_norm(const NormArgs &a, bool mx4, bool post, hipStream_t s)
 {
@@ -550,21 +600,24 @@ void launch_norm(const NormArgs &a, bool mx4, bool post, hipStream_t s)
     // (as many workgroups as run at once: four waves to the SIMD with a post norm, five without)
     const unsigned grid = (unsigned)std::min<long long>(((long long)a.rows + r - 1) / r, (long long)cus * ((post ? 1024 : 1280) / threads));
     const auto go = [&](auto kern) { kern<<<dim3(grid), dim3(threads), 0, s>>>(a); };
-    const auto pick = [&](auto m, auto ps, auto wd) {
-        constexpr bool MX4 = decltype(m)::value, POST = decltype(ps)::value, WIDE = decltype(wd)::value;
+    const auto pick = [&](auto m, auto ps, auto md) {
+        constexpr bool MX4 = decltype(m)::value, POST = decltype(ps)::value;
+        constexpr int MODE = decltype(md)::value;
         switch (shape.lanes) {
-            case 16: go(norm_kernel<DT, 16, 1, MX4, POST, WIDE>); break;
-            case 32: if constexpr (WIDE) go(norm_kernel<DT, 32, 1, MX4, POST, WIDE>); break;
-            case 64: if constexpr (WIDE) go(norm_kernel<DT, 64, 1, MX4, POST, WIDE>); break;
-            case 128: if constexpr (WIDE) go(norm_kernel<DT, 128, 1, MX4, POST, WIDE>); break;
-            case 256: if constexpr (WIDE) go(norm_kernel<DT, 256, 1, MX4, POST, WIDE>); break;
-            case 512: if constexpr (WIDE) go(norm_kernel<DT, 512, 1, MX4, POST, WIDE>); break;
+            case 16: go(norm_kernel<DT, 16, 1, MX4, POST, MODE>); break;
+            case 32: if constexpr (MODE != NARROW) go(norm_kernel<DT, 32, 1, MX4, POST, MODE>); break;
+            case 64: if constexpr (MODE != NARROW) go(norm_kernel<DT, 64, 1, MX4, POST, MODE>); break;
+            case 128: if constexpr (MODE != NARROW) go(norm_kernel<DT, 128, 1, MX4, POST, MODE>); break;
+            case 256: if constexpr (MODE != NARROW) go(norm_kernel<DT, 256, 1, MX4, POST, MODE>); break;
+            case 512: if constexpr (MODE != NARROW) go(norm_kernel<DT, 512, 1, MX4, POST, MODE>); break;
             default:
-                if constexpr (WIDE) shape.runs == 1 ? go(norm_kernel<DT, 1024, 1, MX4, POST, WIDE>) : go(norm_kernel<DT, 1024, 2, MX4, POST, WIDE>);
+                if constexpr (MODE != NARROW) shape.runs == 1 ? go(norm_kernel<DT, 1024, 1, MX4, POST, MODE>) : go(norm_kernel<DT, 1024, 2, MX4, POST, MODE>);
         }
     };
-    const auto wide = [&](auto m, auto ps) { a.cols >= 8 ? pick(m, ps, std::true_type{}) : pick(m, ps, std::false_type{}); };
-    const auto posts = [&](auto m) { post ? wide(m, std::true_type{}) : wide(m, std::false_type{}); };
+    const auto widths = [&](auto m, auto ps) {
+        a.cols < 8 ? pick(m, ps, Mode<NARROW>{}) : a.cols % 8 ? pick(m, ps, Mode<CUT>{}) : pick(m, ps, Mode<EVEN>{});
+    };
+    const auto posts = [&](auto m) { post ? widths(m, std::true_type{}) : widths(m, std::false_type{}); };
     mx4 ? posts(std::true_type{}) : posts(std::false_type{});
 }
 
@@ -573,20 +626,24 @@ void launch_norm_grad(const NormGradArgs &a, bool post, int workgroups, hipStrea
 {
     const RowShape shape = row_shape(a.cols);
     const auto go = [&](auto kern) { kern<<<dim3(workgroups), dim3(grad_threads(shape.lanes, post)), 0, s>>>(a); };
-    const auto pick = [&](auto ps, auto wd) {
-        constexpr bool POST = decltype(ps)::value, WIDE = decltype(wd)::value;
+    const auto pick = [&](auto ps, auto vg, auto md) {
+        constexpr bool POST = decltype(ps)::value, VG = decltype(vg)::value;
+        constexpr int MODE = decltype(md)::value;
         switch (shape.lanes) {
-            case 16: go(norm_grad_kernel<DT, 16, 1, POST, WIDE>); break;
-            case 32: if constexpr (WIDE) go(norm_grad_kernel<DT, 32, 1, POST, WIDE>); break;
-            case 64: if constexpr (WIDE) go(norm_grad_kernel<DT, 64, 1, POST, WIDE>); break;
-            case 128: if constexpr (WIDE) go(norm_grad_kernel<DT, 128, 1, POST, WIDE>); break;
-            case 256: if constexpr (WIDE) go(norm_grad_kernel<DT, 256, 1, POST, WIDE>); break;
-            case 512: if constexpr (WIDE) go(norm_grad_kernel<DT, 512, 1, POST, WIDE>); break;
-            default: if constexpr (WIDE) shape.runs == 1 ? go(norm_grad_kernel<DT, 1024, 1, POST, WIDE>) : go(norm_grad_kernel<DT, 1024, 2, POST, WIDE>);
+            case 16: go(norm_grad_kernel<DT, 16, 1, POST, VG, MODE>); break;
+            case 32: if constexpr (MODE != NARROW) go(norm_grad_kernel<DT, 32, 1, POST, VG, MODE>); break;
+            case 64: if constexpr (MODE != NARROW) go(norm_grad_kernel<DT, 64, 1, POST, VG, MODE>); break;
+            case 128: if constexpr (MODE != NARROW) go(norm_grad_kernel<DT, 128, 1, POST, VG, MODE>); break;
+            case 256: if constexpr (MODE != NARROW) go(norm_grad_kernel<DT, 256, 1, POST, VG, MODE>); break;
+            case 512: if constexpr (MODE != NARROW) go(norm_grad_kernel<DT, 512, 1, POST, VG, MODE>); break;
+            default: if constexpr (MODE != NARROW) shape.runs == 1 ? go(norm_grad_kernel<DT, 1024, 1, POST, VG, MODE>) : go(norm_grad_kernel<DT, 1024, 2, POST, VG, MODE>);
         }
     };
-    const auto wide = [&](auto ps) { a.cols >= 8 ? pick(ps, std::true_type{}) : pick(ps, std::false_type{}); };
-    post ? wide(std::true_type{}) : wide(std::false_type{});
+    const auto widths = [&](auto ps, auto vg) {
+        a.cols < 8 ? pick(ps, vg, Mode<NARROW>{}) : a.cols % 8 ? pick(ps, vg, Mode<CUT>{}) : pick(ps, vg, Mode<EVEN>{});
+    };
+    const auto gates = [&](auto ps) { a.gate != nullptr && (a.gate_cols > 1 || a.cols == 1) ? widths(ps, std::true_type{}) : widths(ps, std::false_type{}); };
+    post ? gates(std::true_type{}) : gates(std::false_type{});
 }
 
 template <int DT>
