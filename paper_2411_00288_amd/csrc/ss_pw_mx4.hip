@@ -274,43 +274,54 @@ __device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x
 // 16-bit input rows of a workgroup, quantised into LDS.  Block b of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
 // pieces, and with an odd `pad` the quads of a row's neighbouring blocks write to different banks.  WIDE: K is at least 8.  The scale of b = 8 q + 2 s + half is byte s of word
 // (q * 2 + half) * pad + r, the four steps of a lane.  Blocks 0 .. 2 Ks - 1, rows 0 .. count - 1; what is past the matrix is zero.
-template <int DT, int THREADS, int U, bool WIDE>
-__device__ __forceinline__ void quantise_rows(const uint16_t *x, long long ldx, int rows, int count, int K, int Ks, int pad, unsigned mul, unsigned sh, uint8_t *codes_s,
-                                              uint8_t *scales_s)
-{
-    const int runs = 8 * Ks, total = count * runs;
-    for (int base = 0; base < total; base += THREADS * U) {
-        Run<DT> raw[U];
-        int row[U], run[U];
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int i = base + u * THREADS + (int)threadIdx.x;
-            row[u] = (int)(((unsigned long long)(unsigned)i * mul) >> sh);
-            run[u] = i - row[u] * runs;
-            if constexpr (WIDE) {
-                raw[u] = load_wide<DT>(x + min(row[u], rows - 1) * ldx, run[u] * 8, K);
-            } else {
-                raw[u] = load_run<DT>(x + row[u] * ldx + run[u] * 8, i < total && row[u] < rows ? K - run[u] * 8 : 0);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int b = run[u] / 4;
-            if constexpr (WIDE) place_wide<DT>(raw[u], run[u] * 8, K, row[u] < rows);
-            const uint32_t byte = mx4_scale(quad_max(magnitude<DT>(raw[u])));
-            const uint32_t c = mx4_codes<DT>(raw[u], byte);
-            if (base + u * THREADS + (int)threadIdx.x >= total) continue;
-            *reinterpret_cast<uint32_t *>(codes_s + (b * pad + row[u]) * 16 + run[u] % 4 * 4) = c;
-            if (run[u] % 4 == 0) scales_s[((b / 8 * 2 + b % 2) * pad + row[u]) * 4 + b % 8 / 2] = (uint8_t)byte;
-        }
-    }
-}
-
+//
+// A thread's runs are THREADS apart: `step_row` rows and `step_run` runs, or one row more and a row's runs less, so that only the first takes a division.
 struct PwRowsArgs {
     const uint16_t *x;
     long long ldx;
     unsigned mul, sh;                      // division by a row's runs, 8 Ks
+    int step_row, step_run;                // the kernel's threads over and modulo the runs
 };
+
+template <int DT, int THREADS, int U, bool WIDE>
+__device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row0, int rows, int count, int K, int Ks, int pad, uint8_t *codes_s, uint8_t *scales_s)
+{
+    const int runs = 8 * Ks, total = count * runs;
+    const uint16_t *const x = r.x + row0 * r.ldx;
+    int row = (int)(((unsigned long long)threadIdx.x * r.mul) >> r.sh), run = (int)threadIdx.x - row * runs;
+    for (int base = 0; base < total; base += THREADS * U) {
+        Run<DT> raw[U];
+        int rw[U], rn[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            rw[u] = row;
+            rn[u] = run;
+            if (base + u * THREADS < total) {              // uniform
+                if constexpr (WIDE)
+                    raw[u] = load_wide<DT>(x + (long long)min(row, rows - 1) * (int)r.ldx, run * 8, K);
+                else
+                    raw[u] = load_run<DT>(x + (long long)row * (int)r.ldx + run * 8, row < rows ? K - run * 8 : 0);
+            }
+            row += r.step_row;
+            run += r.step_run;
+            if (run >= runs) {
+                run -= runs;
+                row++;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (base + u * THREADS >= total) break;        // uniform
+            const int b = rn[u] / 4;
+            if constexpr (WIDE) place_wide<DT>(raw[u], rn[u] * 8, K, rw[u] < rows);
+            const uint32_t byte = mx4_scale(quad_max(magnitude<DT>(raw[u])));
+            const uint32_t c = mx4_codes<DT>(raw[u], byte);
+            if (rw[u] >= count) continue;
+            *reinterpret_cast<uint32_t *>(codes_s + (__umul24(b, pad) + rw[u]) * 16 + rn[u] % 4 * 4) = c;
+            if (rn[u] % 4 == 0) scales_s[(__umul24(b / 8 * 2 + b % 2, pad) + rw[u]) * 4 + b % 8 / 2] = (uint8_t)byte;
+        }
+    }
+}
 
 // Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves take units of 64 output channels and 32 rows
 // in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels.  The next
@@ -366,7 +377,7 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
         fetch(min(wave / NT * 2, Mt - 1), 0, wa, sa);
     else
         fetch(min(wave / NT * 2, Mt - 1), 0, wn, sn);
-    quantise_rows<DT, 256, SHORT ? 4 : 8, WIDE>(r.x + row0 * r.ldx, r.ldx, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, r.mul, r.sh, codes_s, scales_s);
+    quantise_rows<DT, 256, SHORT ? 4 : 8, WIDE>(r, row0, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, codes_s, scales_s);
     __syncthreads();
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
     // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us).
@@ -438,7 +449,7 @@ __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArg
     weights(wave + NW, wn, sn);
     uint8_t *const scales_s = smem + 2 * Ks * pad * 16;
     if constexpr (QUANT) {
-        quantise_rows<DT, NW * 64, 8, WIDE>(r.x + row0 * r.ldx, r.ldx, rows, rows, p.K, Ks, pad, r.mul, r.sh, smem, scales_s);
+        quantise_rows<DT, NW * 64, 8, WIDE>(r, row0, rows, rows, p.K, Ks, pad, smem, scales_s);
         __syncthreads();
     }
     f32x16 acc[1][NI] = {};
@@ -577,69 +588,95 @@ size_t rows_lds(const Mx4Dims &t, int px)
     return (size_t)2 * t.Ks * (px + 1) * 16 + ((size_t)t.Kq * 2 * (px + 1) * 4 + 15) / 16 * 16 + (size_t)t.Mt * 128;
 }
 
-enum { KIND_TILE = 0, KIND_FEW, KIND_ROWS };
+// The kernels, by the ids of the test hook.  On codes: tiles of 64 x 64, 128 x 128 and 256 x 256, few rows 32 and 64 at a time.  On 16-bit input: few rows,
+// reductions that fit LDS with 32 rows to the workgroup and with more, and a quantisation of its own with the product on its codes.
+enum PwKernel { PW_TILE_64 = 70, PW_TILE_128, PW_TILE_256, PW_FEW_32, PW_FEW_64, PW16_FEW, PW16_ROWS, PW16_ROWS_MORE, PW16_CODES };
 
-// Which kernel takes a layer on 16-bit input: KIND_TILE stands for a quantisation of its own and the product on its codes.
-struct PwPlan {
-    int kind, px;
-};
+long long pw_tiles(const Mx4Dims &t, long long rows, int m, int n) { return ((t.Mt * 32ll + m - 1) / m) * ((rows + n - 1) / n); }
 
-PwPlan plan16(const Mx4Dims &t, int64_t rows)
+PwKernel choose_codes(const Mx4Dims &t, long long rows, long long cus)
 {
-    if (rows <= 32 && few_lds(t, 16, (int)rows) <= 160 * 1024) return {KIND_FEW, 32};
-    if (rows_lds(t, 32) <= 80 * 1024) return {KIND_ROWS, rows >= 64 * 512 && rows_lds(t, 64) <= 40 * 1024 ? (t.Kq == 1 ? 128 : 64) : 32};
-    return {KIND_TILE, 0};
+    const int forced = forced_tile();                      // test hook
+    if (forced >= PW_TILE_64 && forced <= PW_FEW_64) return (PwKernel)forced;
+    if (pw_tiles(t, rows, 256, 256) >= cus) return PW_TILE_256;
+    if (pw_tiles(t, rows, 128, 128) >= cus) return PW_TILE_128;
+    if (rows > 64 && pw_tiles(t, rows, 64, 64) >= cus / 2) return PW_TILE_64;
+    return rows <= 32 || pw_tiles(t, rows, 32, 32) <= cus ? PW_FEW_32 : PW_FEW_64;
 }
+
+int more_rows(const Mx4Dims &t) { return t.Kq == 1 ? 128 : 64; }
+
+bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
+{
+    switch (k) {
+        case PW16_FEW: return rows <= 32 && few_lds(t, 16, (int)rows) <= 160 * 1024;
+        case PW16_ROWS: return rows_lds(t, 32) <= 160 * 1024;
+        case PW16_ROWS_MORE: return rows_lds(t, more_rows(t)) <= 160 * 1024;
+        default: return true;
+    }
+}
+
+PwKernel choose16(const Mx4Dims &t, long long rows)
+{
+    const int forced = forced_tile();                      // test hook
+    if (forced >= PW16_FEW && forced <= PW16_CODES && fits16(t, rows, (PwKernel)forced)) return (PwKernel)forced;
+    if (!fits16(t, rows, PW16_ROWS)) return PW16_CODES;
+    if (fits16(t, rows, PW16_FEW)) return PW16_FEW;
+    if (rows_lds(t, 32) > 80 * 1024) return PW16_CODES;
+    return rows >= 64 * 512 && rows_lds(t, 64) <= 40 * 1024 ? PW16_ROWS_MORE : PW16_ROWS;
+}
+
+template <int N> using Int = std::integral_constant<int, N>;
 
 template <int DT>
 int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
 {
-    const auto go = [&](auto mi, auto ni) -> int {
-        constexpr int MI = decltype(mi)::value, NI = decltype(ni)::value;
-        const long long tm = (t.Mt + 2 * MI - 1) / (2 * MI), tn = ((long long)a.P + 64 * NI - 1) / (64 * NI);
+    const auto tile = [&](auto ni) -> int {
+        constexpr int NI = decltype(ni)::value;
+        const long long tm = (t.Mt + 2 * NI - 1) / (2 * NI), tn = ((long long)a.P + 64 * NI - 1) / (64 * NI);
         if (tm * tn > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
-        pw_mx4_tile_kernel<DT, MI, NI><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
+        pw_mx4_tile_kernel<DT, NI, NI><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
         return launched();
     };
-    using One = std::integral_constant<int, 1>;
-    using Two = std::integral_constant<int, 2>;
-    using Four = std::integral_constant<int, 4>;
-    const long long cus = std::max(compute_units(), 1);
-    const auto tiles = [&](int mi, int ni) { return (long long)((t.Mt + 2 * mi - 1) / (2 * mi)) * (((long long)a.P + 64 * ni - 1) / (64 * ni)); };
-    if (tiles(4, 4) >= cus) return go(Four{}, Four{});
-    if (tiles(2, 2) >= cus) return go(Two{}, Two{});
-    if (tiles(1, 1) >= cus / 2) return go(One{}, One{});
-    const long long px = ((long long)a.P + 31) / 32;
-    const PwRowsArgs none{};
-    const auto few = [&](auto nw, auto ni) -> int {
-        constexpr int NW = decltype(nw)::value, NI = decltype(ni)::value;
-        return launch_lds<pw_mx4_few_kernel<DT, NW, NI, false, false>>((px + NI - 1) / NI * t.Mt, NW * 64, few_lds(t, NW, 0), s, a, none);
+    const auto few = [&](auto ni) -> int {
+        constexpr int NI = decltype(ni)::value;
+        const long long blocks = ((long long)a.P + 32 * NI - 1) / (32 * NI) * t.Mt;
+        if (t.Kq > 8) return launch_lds<pw_mx4_few_kernel<DT, 16, NI, false, false>>(blocks, 1024, few_lds(t, 16, 0), s, a, PwRowsArgs{});
+        if (t.Kq > 4) return launch_lds<pw_mx4_few_kernel<DT, 8, NI, false, false>>(blocks, 512, few_lds(t, 8, 0), s, a, PwRowsArgs{});
+        return launch_lds<pw_mx4_few_kernel<DT, 4, NI, false, false>>(blocks, 256, few_lds(t, 4, 0), s, a, PwRowsArgs{});
     };
-    const auto waves = [&](auto ni) -> int { return t.Kq > 8 ? few(std::integral_constant<int, 16>{}, ni) : t.Kq > 4 ? few(std::integral_constant<int, 8>{}, ni) : few(Four{}, ni); };
-    return px * t.Mt <= cus || px == 1 ? waves(One{}) : waves(Two{});
+    switch (choose_codes(t, a.P, std::max(compute_units(), 1))) {
+        case PW_TILE_64: return tile(Int<1>{});
+        case PW_TILE_128: return tile(Int<2>{});
+        case PW_TILE_256: return tile(Int<4>{});
+        case PW_FEW_32: return few(Int<1>{});
+        default: return few(Int<2>{});
+    }
 }
 
 template <int DT>
-int product16(const PwArgs &a, const Mx4Dims &t, const PwPlan &plan, const void *x, int64_t ldx, hipStream_t s)
+int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x, int64_t ldx, hipStream_t s)
 {
-    PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0};
-    fast_div_setup((unsigned)t.Ks * 8u, &r.mul, &r.sh);
+    PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0, 0, 0};
+    const int runs = t.Ks * 8;
+    fast_div_setup((unsigned)runs, &r.mul, &r.sh);
     const auto go = [&](auto wide) -> int {
         constexpr bool WIDE = decltype(wide)::value;
-        if (plan.kind == KIND_FEW) {
-            if (t.Kq <= 4) return launch_lds<pw_mx4_few_kernel<DT, 4, 1, true, WIDE>>(t.Mt, 256, few_lds(t, 4, a.P), s, a, r);
-            if (t.Kq <= 8) return launch_lds<pw_mx4_few_kernel<DT, 8, 1, true, WIDE>>(t.Mt, 512, few_lds(t, 8, a.P), s, a, r);
-            return launch_lds<pw_mx4_few_kernel<DT, 16, 1, true, WIDE>>(t.Mt, 1024, few_lds(t, 16, a.P), s, a, r);
-        }
-        const long long blocks = ((long long)a.P + plan.px - 1) / plan.px;
+        const auto few = [&](auto nw) -> int {
+            constexpr int NW = decltype(nw)::value;
+            r.step_row = NW * 64 / runs;
+            r.step_run = NW * 64 % runs;
+            return launch_lds<pw_mx4_few_kernel<DT, NW, 1, true, WIDE>>(t.Mt, NW * 64, few_lds(t, NW, a.P), s, a, r);
+        };
         const auto rows = [&](auto nt, auto brief) -> int {
             constexpr int NT = decltype(nt)::value;
-            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(blocks, 256, rows_lds(t, 32 * NT), s, a, r);
+            r.step_row = 256 / runs;
+            r.step_run = 256 % runs;
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(((long long)a.P + 32 * NT - 1) / (32 * NT), 256, rows_lds(t, 32 * NT), s, a, r);
         };
-        using One = std::integral_constant<int, 1>;
-        using Two = std::integral_constant<int, 2>;
-        if (t.Kq == 1) return plan.px == 128 ? rows(std::integral_constant<int, 4>{}, std::true_type{}) : rows(One{}, std::true_type{});
-        return plan.px == 64 ? rows(Two{}, std::false_type{}) : rows(One{}, std::false_type{});
+        if (kernel == PW16_FEW) return t.Kq > 8 ? few(Int<16>{}) : t.Kq > 4 ? few(Int<8>{}) : few(Int<4>{});
+        if (t.Kq == 1) return kernel == PW16_ROWS_MORE ? rows(Int<4>{}, std::true_type{}) : rows(Int<1>{}, std::true_type{});
+        return kernel == PW16_ROWS_MORE ? rows(Int<2>{}, std::false_type{}) : rows(Int<1>{}, std::false_type{});
     };
     return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
 }
@@ -676,7 +713,7 @@ extern "C" int ss_pw_mx4_workspace_bytes(const ss_weight_desc *desc, int64_t row
     if (!bytes || rows < 0) return SS_ERR_INVALID_ARG;
     if (rows > INT32_MAX) return SS_ERR_UNSUPPORTED;
     const Mx4Dims t = mx4_dims(desc->cout, desc->cin);
-    *bytes = plan16(t, rows).kind == KIND_TILE ? codes_bytes(t, rows) + (size_t)rows * t.S : 0;
+    *bytes = rows > 0 && choose16(t, rows) == PW16_CODES ? codes_bytes(t, rows) + (size_t)rows * t.S : 0;
     return SS_OK;
 }
 
@@ -689,15 +726,12 @@ extern "C" int ss_pw_mx4_fwd(const ss_weight_desc *desc, const void *x, int64_t 
     if (ldx > INT32_MAX) return SS_ERR_UNSUPPORTED;
     if (rows == 0) return SS_OK;
     if (!x || !aligned(x, 2)) return SS_ERR_INVALID_ARG;
-    size_t need = 0;
-    st = ss_pw_mx4_workspace_bytes(desc, rows, &need);
-    if (st != SS_OK) return st;
-    if (need > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < need)) return SS_ERR_WORKSPACE;
     const Mx4Dims t = mx4_dims(desc->cout, desc->cin);
+    const PwKernel kernel = choose16(t, rows);
+    if (kernel == PW16_CODES && (!workspace || !aligned(workspace, 16) || ws_bytes < codes_bytes(t, rows) + (size_t)rows * t.S)) return SS_ERR_WORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const PwArgs a = pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy);
-    const PwPlan plan = plan16(t, rows);
-    if (plan.kind != KIND_TILE) return desc->dtype == SS_F16 ? product16<SS_F16>(a, t, plan, x, ldx, s) : product16<SS_BF16>(a, t, plan, x, ldx, s);
+    if (kernel != PW16_CODES) return desc->dtype == SS_F16 ? product16<SS_F16>(a, t, kernel, x, ldx, s) : product16<SS_BF16>(a, t, kernel, x, ldx, s);
     uint8_t *codes = static_cast<uint8_t *>(workspace), *scales = codes + codes_bytes(t, rows);
     st = mx4_quantize(x, rows, desc->cin, ldx, desc->dtype, codes, scales, s);
     if (st != SS_OK) return st;
