@@ -7,29 +7,11 @@
 #ifndef SS_MX4_H_
 #define SS_MX4_H_
 #include "ss_rows.h"
+#include "ss_pw_choice.h"
 
 namespace ss {
 
 constexpr uint32_t kMagicMx4 = 0x344D5353u;      // "SSM4"
-
-// Row sizes of a quantised activation and tile counts of quantised weights.
-struct Mx4Dims {
-    int KB;        // blocks of a row
-    int S;         // scale bytes of a row: KB rounded up to 4, the surplus zero
-    int Mt, Ks;    // 32-row tiles, reduction steps of 64
-    int Kq;        // scale words of a tile and lane: 4 steps each
-};
-
-inline Mx4Dims mx4_dims(int rows, int K)
-{
-    Mx4Dims t;
-    t.KB = (K + 31) / 32;
-    t.S = (t.KB + 3) / 4 * 4;
-    t.Mt = (rows + 31) / 32;
-    t.Ks = (t.KB + 1) / 2;
-    t.Kq = (t.Ks + 3) / 4;
-    return t;
-}
 
 inline size_t mx4_packed_size(const Mx4Dims &t) { return (size_t)kHeaderBytes + (size_t)t.Mt * t.Ks * 1024 + (size_t)t.Mt * t.Kq * 256; }
 

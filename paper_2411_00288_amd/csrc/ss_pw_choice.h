@@ -1,0 +1,122 @@
+// Which kernel a pointwise MXFP4 layer takes (host code, no device calls; kernels: ss_pw_mx4.hip).
+#ifndef SS_PW_CHOICE_H_
+#define SS_PW_CHOICE_H_
+#include "ss_internal.h"
+#include <algorithm>
+
+namespace ss {
+
+// Row sizes of a quantised activation and tile counts of quantised weights.
+struct Mx4Dims {
+    int KB;        // blocks of a row
+    int S;         // scale bytes of a row: KB rounded up to 4, the surplus zero
+    int Mt, Ks;    // 32-row tiles, reduction steps of 64
+    int Kq;        // scale words of a tile and lane: 4 steps each
+};
+
+inline Mx4Dims mx4_dims(int rows, int K)
+{
+    Mx4Dims t;
+    t.KB = (K + 31) / 32;
+    t.S = (t.KB + 3) / 4 * 4;
+    t.Mt = (rows + 31) / 32;
+    t.Ks = (t.KB + 1) / 2;
+    t.Kq = (t.Ks + 3) / 4;
+    return t;
+}
+
+// The kernels, by the ids of the test hook.  On codes: tiles of 64 x 64, 128 x 128 and 256 x 256, few rows 32 and 64 at a time.  On 16-bit input: few rows,
+// reductions that fit LDS with 32 rows to the workgroup and (one chunk) with 128, and a quantisation of its own with the product on its codes.
+enum PwKernel { PW_TILE_64 = 70, PW_TILE_128, PW_TILE_256, PW_FEW_32, PW_FEW_64, PW16_FEW, PW16_ROWS, PW16_ROWS_128, PW16_CODES };
+
+constexpr size_t kPwLds = 160 * 1024;
+
+// LDS of the few-row kernel: its quantised rows, later the waves' sums.
+inline size_t few_lds(const Mx4Dims &t, int waves, int quantised_rows)
+{
+    const size_t pad = (size_t)(quantised_rows | 1), rows = quantised_rows ? (size_t)2 * t.Ks * pad * 16 + (size_t)t.Kq * 2 * pad * 4 : 0;
+    return std::max(rows, (size_t)waves * 16 * 65 * 4);
+}
+
+// LDS of the kernel for reductions that fit it: quantised rows, their scales, the bias.
+inline size_t rows_lds(const Mx4Dims &t, int px)
+{
+    return (size_t)2 * t.Ks * (px + 1) * 16 + ((size_t)t.Kq * 2 * (px + 1) * 4 + 15) / 16 * 16 + (size_t)t.Mt * 128;
+}
+
+// Estimated time of the tiled kernels in us.  A compute unit's n tiles of m x m take their loads and stores (a) and their steps (b each) one after the other, and
+// those of the last ones beside each other (c): 64 x 64 tiles a = 0.65, b = 0.08, 128 x 128 2.8 and 0.17, 256 x 256 10 and 0.43.  Measured on 14 layers of
+// 64 -> 256 to 8192 -> 8192 channels and 512 to 200704 rows, among them (estimates / measurements of the three):
+//     64 -> 256 on 200704 rows   39 / 40   39 / 36   42 / 42        1024 -> 256 on 12544        11 / 10     8 / 9    17 / 16
+//     8192 -> 1024 on 12544     140 / 132 101 / 95   65 / 65        8192 -> 8192 on 3136       276 / 259  156 / 164 130 / 141
+inline double tile_us(const Mx4Dims &t, long long rows, int m, long long cus)
+{
+    const double tiles = (double)((t.Mt * 32ll + m - 1) / m) * (double)((rows + m - 1) / m) / (double)cus;
+    const double n = m == 256 || tiles < 4 ? (double)(long long)(tiles + 0.999999) : tiles;
+    if (m == 256) return n * (10.0 + 0.43 * t.Ks);
+    if (m == 128) return 2.2 + n * (2.8 + 0.17 * t.Ks);
+    return 3.2 + 0.65 * n + 0.08 * t.Ks * std::max(n, 1.4);
+}
+
+inline PwKernel best_tile(const Mx4Dims &t, long long rows, long long cus)
+{
+    const double small = tile_us(t, rows, 64, cus), middle = tile_us(t, rows, 128, cus), large = tile_us(t, rows, 256, cus);
+    return large < small && large < middle ? PW_TILE_256 : middle < small ? PW_TILE_128 : PW_TILE_64;
+}
+
+// On codes.  Few rows until their workgroups of 32 channels and 32 rows fill the chip (768 -> 2304 on 100 rows, 288 of them: 4.6 us, in tiles 5.1; 4096 -> 4096 on 100, 512
+// of them: 13.3 and 10.5), and of wide layers with long reductions up to 64 rows, two tiles of them to the workgroup (8192 -> 8192 on 33 rows 14.2, in tiles 22.6).
+inline PwKernel choose_codes(const Mx4Dims &t, long long rows, long long cus)
+{
+    if (rows <= 32 || (rows + 31) / 32 * t.Mt <= cus * 5 / 4) return PW_FEW_32;
+    if (rows <= 64 && t.Kq > 8) return PW_FEW_64;
+    return best_tile(t, rows, cus);
+}
+
+inline double tiles_us(const Mx4Dims &t, long long rows, long long cus)
+{
+    const PwKernel k = best_tile(t, rows, cus);
+    return tile_us(t, rows, k == PW_TILE_256 ? 256 : k == PW_TILE_128 ? 128 : 64, cus);
+}
+
+// How many workgroups share the output channels of 32 rows of the kernel for reductions that fit LDS: until there is one to a compute unit, and at least a
+// unit of 64 channels for each of their four waves.
+inline int rows_splits(const Mx4Dims &t, long long rows, long long cus)
+{
+    const long long blocks = (rows + 31) / 32, units = (t.Mt + 1) / 2;
+    return (int)std::max(1ll, std::min((units + 3) / 4, cus / blocks));
+}
+
+// Does the kernel take such a layer at all?
+inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
+{
+    switch (k) {
+        case PW16_FEW: return rows <= 32 && few_lds(t, 16, (int)rows) <= kPwLds;
+        case PW16_ROWS: return rows_lds(t, 32) <= kPwLds;
+        case PW16_ROWS_128: return t.Kq == 1 && rows_lds(t, 128) <= kPwLds;
+        default: return true;
+    }
+}
+
+// On 16-bit input.  Few rows while every workgroup's own quantisation of them is short (1024 -> 4096: 16 rows 4.6 us, and with a quantisation of its own 3.3 + 2.9; 4096 ->
+// 4096: 24 rows 9.1 and 6.3 + 3.0).  Otherwise the shorter estimate: of the kernel that quantises in LDS, whose waves walk down the channels, three workgroups to the compute unit
+// (4 us, 4 for each 1024 channels of the reduction and 0.17 a step and unit; what follows the first three overlaps, with 4.2 TB/s for what is moved), or of a quantisation at
+// 4 TB/s and the tiled product (512 -> 2048 on 12544 rows estimated 32 and 34, measured 30 and 33; 1024 -> 256 on 12544 18 and 18, 15 and 18; 64 -> 256 on 200704 34 and 55, 31
+// and 52).  128 rows to the workgroup, one tile of them to the wave, with
+// short reductions and many rows (64 -> 256 on 200704 rows 47 -> 31 us, on 12544 7.4 and 8.2).
+inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
+{
+    if (rows * t.KB <= 1536 && fits16(t, rows, PW16_FEW)) return PW16_FEW;
+    if (!fits16(t, rows, PW16_ROWS)) return PW16_CODES;
+    const double K = t.KB * 32.0, out = rows * t.Mt * 64.0;
+    const long long blocks = (rows + 31) / 32, splits = rows_splits(t, rows, cus), units = ((t.Mt + 1) / 2 + splits * 4 - 1) / (splits * 4);
+    const double one = 4.0 + 0.004 * K + 0.17 * units * t.Ks, rounds = (double)(blocks * splits) / (3.0 * cus);
+    const double lds = one + std::max((rounds - 1.0) * 0.7 * one, (rows * K * 2 + out) / 4.2e6);
+    const double codes = 2.5 + rows * K * 2.53 / 4e6 + (choose_codes(t, rows, cus) >= PW_FEW_32 ? 4.0 + 0.05 * t.Ks : tiles_us(t, rows, cus));
+    if (codes < lds) return PW16_CODES;
+    return rows >= 128 * cus && fits16(t, rows, PW16_ROWS_128) ? PW16_ROWS_128 : PW16_ROWS;
+}
+
+}  // namespace ss
+
+#endif

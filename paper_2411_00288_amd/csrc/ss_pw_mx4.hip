@@ -1,7 +1,6 @@
 // Pointwise layer on MXFP4 operands: y = act(Wq xq + bias + residual).
 #include "ss_mx4.h"
 #include "ss_conv_params.h"
-#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -281,6 +280,8 @@ struct PwRowsArgs {
     long long ldx;
     unsigned mul, sh;                      // division by a row's runs, 8 Ks
     int step_row, step_run;                // the kernel's threads over and modulo the runs
+    unsigned blocks;                       // workgroups that share the rows (the others take other output channels)
+    int units;                             // units of 64 channels of a workgroup
 };
 
 template <int DT, int THREADS, int U, bool WIDE>
@@ -324,7 +325,8 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
 }
 
 // Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves take units of 64 output channels and 32 rows
-// in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels.  The next
+// in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels, unless there are
+// few rows: then several workgroups share the channels of one's rows.  The next
 // weights are on their way from the L2 while the current ones are multiplied or, with a reduction of one chunk (SHORT), while the sums are finished: that
 // is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
 template <int DT, int NT, bool SHORT, bool WIDE>
@@ -333,8 +335,10 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     constexpr int PX = 32 * NT, PAD = PX + 1;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = SHORT ? 1 : (Ks + 3) / 4, Mt = (p.cout + 31) / 32, units = (Mt + 1) / 2 * NT;
-    const long long row0 = (long long)blockIdx.x * PX;
+    const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = SHORT ? 1 : (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
+    const unsigned part = blockIdx.x / r.blocks;
+    const int first = (int)part * r.units * NT, units = min((Mt + 1) / 2, ((int)part + 1) * r.units) * NT;
+    const long long row0 = (long long)(blockIdx.x - part * r.blocks) * PX;
     uint8_t *const codes_s = smem, *const scales_s = smem + 2 * Ks * PAD * 16;
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 256, 0x00020000);
@@ -374,9 +378,9 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
     };
     for (int o = threadIdx.x; o < Mt * 32; o += 256) bias_s[o] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
     if constexpr (SHORT)
-        fetch(min(wave / NT * 2, Mt - 1), 0, wa, sa);
+        fetch(min((first + wave) / NT * 2, Mt - 1), 0, wa, sa);
     else
-        fetch(min(wave / NT * 2, Mt - 1), 0, wn, sn);
+        fetch(min((first + wave) / NT * 2, Mt - 1), 0, wn, sn);
     quantise_rows<DT, 256, SHORT ? 4 : 8, WIDE>(r, row0, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, codes_s, scales_s);
     __syncthreads();
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
@@ -385,8 +389,8 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
     const auto walk = [&](auto whole, auto stream) {
         constexpr bool ALL = decltype(whole)::value, STREAM = decltype(stream)::value;
         f32x16 acc[2][1];
-        start(wave / NT * 2, acc);
-        int unit = wave, q = 0;
+        int unit = first + wave, q = 0;
+        start(unit / NT * 2, acc);
         while (unit < units) {
             const int mt = unit / NT * 2, at = unit % NT * 32;
             if constexpr (SHORT) {
@@ -575,55 +579,19 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     return a;
 }
 
-// LDS of the few-row kernel: its quantised rows, later the waves' sums.
-size_t few_lds(const Mx4Dims &t, int waves, int quantised_rows)
+// The test hook's kernel where it is one that takes the layer, or the library's choice.
+PwKernel codes_kernel(const Mx4Dims &t, long long rows)
 {
-    const size_t pad = (size_t)(quantised_rows | 1), rows = quantised_rows ? (size_t)2 * t.Ks * pad * 16 + (size_t)t.Kq * 2 * pad * 4 : 0;
-    return std::max(rows, (size_t)waves * 16 * 65 * 4);
-}
-
-// LDS of the kernel for reductions that fit it: quantised rows, their scales, the bias.
-size_t rows_lds(const Mx4Dims &t, int px)
-{
-    return (size_t)2 * t.Ks * (px + 1) * 16 + ((size_t)t.Kq * 2 * (px + 1) * 4 + 15) / 16 * 16 + (size_t)t.Mt * 128;
-}
-
-// The kernels, by the ids of the test hook.  On codes: tiles of 64 x 64, 128 x 128 and 256 x 256, few rows 32 and 64 at a time.  On 16-bit input: few rows,
-// reductions that fit LDS with 32 rows to the workgroup and with more, and a quantisation of its own with the product on its codes.
-enum PwKernel { PW_TILE_64 = 70, PW_TILE_128, PW_TILE_256, PW_FEW_32, PW_FEW_64, PW16_FEW, PW16_ROWS, PW16_ROWS_MORE, PW16_CODES };
-
-long long pw_tiles(const Mx4Dims &t, long long rows, int m, int n) { return ((t.Mt * 32ll + m - 1) / m) * ((rows + n - 1) / n); }
-
-PwKernel choose_codes(const Mx4Dims &t, long long rows, long long cus)
-{
-    const int forced = forced_tile();                      // test hook
+    const int forced = forced_tile();
     if (forced >= PW_TILE_64 && forced <= PW_FEW_64) return (PwKernel)forced;
-    if (pw_tiles(t, rows, 256, 256) >= cus) return PW_TILE_256;
-    if (pw_tiles(t, rows, 128, 128) >= cus) return PW_TILE_128;
-    if (rows > 64 && pw_tiles(t, rows, 64, 64) >= cus / 2) return PW_TILE_64;
-    return rows <= 32 || pw_tiles(t, rows, 32, 32) <= cus ? PW_FEW_32 : PW_FEW_64;
+    return choose_codes(t, rows, std::max(compute_units(), 1));
 }
 
-int more_rows(const Mx4Dims &t) { return t.Kq == 1 ? 128 : 64; }
-
-bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
+PwKernel kernel16(const Mx4Dims &t, long long rows)
 {
-    switch (k) {
-        case PW16_FEW: return rows <= 32 && few_lds(t, 16, (int)rows) <= 160 * 1024;
-        case PW16_ROWS: return rows_lds(t, 32) <= 160 * 1024;
-        case PW16_ROWS_MORE: return rows_lds(t, more_rows(t)) <= 160 * 1024;
-        default: return true;
-    }
-}
-
-PwKernel choose16(const Mx4Dims &t, long long rows)
-{
-    const int forced = forced_tile();                      // test hook
+    const int forced = forced_tile();
     if (forced >= PW16_FEW && forced <= PW16_CODES && fits16(t, rows, (PwKernel)forced)) return (PwKernel)forced;
-    if (!fits16(t, rows, PW16_ROWS)) return PW16_CODES;
-    if (fits16(t, rows, PW16_FEW)) return PW16_FEW;
-    if (rows_lds(t, 32) > 80 * 1024) return PW16_CODES;
-    return rows >= 64 * 512 && rows_lds(t, 64) <= 40 * 1024 ? PW16_ROWS_MORE : PW16_ROWS;
+    return choose16(t, rows, std::max(compute_units(), 1));
 }
 
 template <int N> using Int = std::integral_constant<int, N>;
@@ -645,7 +613,7 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
         if (t.Kq > 4) return launch_lds<pw_mx4_few_kernel<DT, 8, NI, false, false>>(blocks, 512, few_lds(t, 8, 0), s, a, PwRowsArgs{});
         return launch_lds<pw_mx4_few_kernel<DT, 4, NI, false, false>>(blocks, 256, few_lds(t, 4, 0), s, a, PwRowsArgs{});
     };
-    switch (choose_codes(t, a.P, std::max(compute_units(), 1))) {
+    switch (codes_kernel(t, a.P)) {
         case PW_TILE_64: return tile(Int<1>{});
         case PW_TILE_128: return tile(Int<2>{});
         case PW_TILE_256: return tile(Int<4>{});
@@ -657,7 +625,9 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
 template <int DT>
 int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x, int64_t ldx, hipStream_t s)
 {
-    PwRowsArgs r{static_cast<const uint16_t *>(x), ldx, 0, 0, 0, 0};
+    PwRowsArgs r{};
+    r.x = static_cast<const uint16_t *>(x);
+    r.ldx = ldx;
     const int runs = t.Ks * 8;
     fast_div_setup((unsigned)runs, &r.mul, &r.sh);
     const auto go = [&](auto wide) -> int {
@@ -672,11 +642,17 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
             constexpr int NT = decltype(nt)::value;
             r.step_row = 256 / runs;
             r.step_run = 256 % runs;
-            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(((long long)a.P + 32 * NT - 1) / (32 * NT), 256, rows_lds(t, 32 * NT), s, a, r);
+            const long long blocks = ((long long)a.P + 32 * NT - 1) / (32 * NT);
+            const int splits = NT == 1 ? rows_splits(t, a.P, std::max(compute_units(), 1)) : 1;
+            r.blocks = (unsigned)blocks;
+            r.units = ((t.Mt + 1) / 2 + splits - 1) / splits;
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(blocks * splits, 256, rows_lds(t, 32 * NT), s, a, r);
         };
-        if (kernel == PW16_FEW) return t.Kq > 8 ? few(Int<16>{}) : t.Kq > 4 ? few(Int<8>{}) : few(Int<4>{});
-        if (t.Kq == 1) return kernel == PW16_ROWS_MORE ? rows(Int<4>{}, std::true_type{}) : rows(Int<1>{}, std::true_type{});
-        return kernel == PW16_ROWS_MORE ? rows(Int<2>{}, std::false_type{}) : rows(Int<1>{}, std::false_type{});
+        // (as many waves as there are scale words, or as the quantisation keeps busy)
+        const int elements = a.P * a.K;
+        if (kernel == PW16_FEW) return t.Kq > 8 || elements > 16384 ? few(Int<16>{}) : t.Kq > 4 || elements > 8192 ? few(Int<8>{}) : few(Int<4>{});
+        if (kernel == PW16_ROWS_128) return rows(Int<4>{}, std::true_type{});
+        return t.Kq == 1 ? rows(Int<1>{}, std::true_type{}) : rows(Int<1>{}, std::false_type{});
     };
     return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
 }
@@ -713,7 +689,7 @@ extern "C" int ss_pw_mx4_workspace_bytes(const ss_weight_desc *desc, int64_t row
     if (!bytes || rows < 0) return SS_ERR_INVALID_ARG;
     if (rows > INT32_MAX) return SS_ERR_UNSUPPORTED;
     const Mx4Dims t = mx4_dims(desc->cout, desc->cin);
-    *bytes = rows > 0 && choose16(t, rows) == PW16_CODES ? codes_bytes(t, rows) + (size_t)rows * t.S : 0;
+    *bytes = rows > 0 && kernel16(t, rows) == PW16_CODES ? codes_bytes(t, rows) + (size_t)rows * t.S : 0;
     return SS_OK;
 }
 
@@ -727,7 +703,7 @@ extern "C" int ss_pw_mx4_fwd(const ss_weight_desc *desc, const void *x, int64_t 
     if (rows == 0) return SS_OK;
     if (!x || !aligned(x, 2)) return SS_ERR_INVALID_ARG;
     const Mx4Dims t = mx4_dims(desc->cout, desc->cin);
-    const PwKernel kernel = choose16(t, rows);
+    const PwKernel kernel = kernel16(t, rows);
     if (kernel == PW16_CODES && (!workspace || !aligned(workspace, 16) || ws_bytes < codes_bytes(t, rows) + (size_t)rows * t.S)) return SS_ERR_WORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const PwArgs a = pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy);
