@@ -99,18 +99,18 @@ inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
 }
 
 // On 16-bit input.  Few rows while every workgroup's own quantisation of them is short (1024 -> 4096: 16 rows 4.6 us, and with a quantisation of its own 3.3 + 2.9; 4096 ->
-// 4096: 24 rows 9.1 and 6.3 + 3.0).  Otherwise the shorter estimate: of the kernel that quantises in LDS, whose waves walk down the channels, three workgroups to the compute unit
-// (4 us, 4 for each 1024 channels of the reduction and 0.17 a step and unit; what follows the first three overlaps, with 4.2 TB/s for what is moved), or of a quantisation at
-// 4 TB/s and the tiled product (512 -> 2048 on 12544 rows estimated 32 and 34, measured 30 and 33; 1024 -> 256 on 12544 18 and 18, 15 and 18; 64 -> 256 on 200704 34 and 55, 31
-// and 52).  128 rows to the workgroup, one tile of them to the wave, with
-// short reductions and many rows (64 -> 256 on 200704 rows 47 -> 31 us, on 12544 7.4 and 8.2).
+// 4096: 24 rows 9.1 and 6.3 + 3.0).  Otherwise the shorter estimate: of the kernel that quantises in LDS, whose waves walk down the channels, two workgroups to the compute unit
+// (4 us, 2.6 for each 1024 channels of the reduction and 0.11 a step and 32 channels; what follows the first overlaps, with 4.2 TB/s for what is moved), or of a quantisation at
+// 4 TB/s and the tiled product.  Estimated / measured, the former and the latter: 512 -> 2048 on 100 rows 6.2 / 6.4 and 6.9 / 7.1 us, on 12544 28 / 28 and 34 / 32; 4096 -> 4096 on
+// 1024 rows 22 / 33 and 21 / 26; 64 -> 256 on 200704 36 / 32 and 55 / 46.  128 rows to the workgroup, one tile of them to the wave, with short reductions and many rows (64 -> 256 on
+// 200704 rows 47 -> 31 us, on 12544 7.4 and 8.2).
 inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
 {
     if (rows * t.KB <= 1536 && fits16(t, rows, PW16_FEW)) return PW16_FEW;
     if (!fits16(t, rows, PW16_ROWS)) return PW16_CODES;
     const double K = t.KB * 32.0, out = rows * t.Mt * 64.0;
-    const long long blocks = (rows + 31) / 32, splits = rows_splits(t, rows, cus), units = ((t.Mt + 1) / 2 + splits * 4 - 1) / (splits * 4);
-    const double one = 4.0 + 0.004 * K + 0.17 * units * t.Ks, rounds = (double)(blocks * splits) / (3.0 * cus);
+    const long long blocks = (rows + 31) / 32, splits = rows_splits(t, rows, cus), units = (t.Mt + splits * 8 - 1) / (splits * 8);
+    const double one = 4.0 + 0.0025 * K + 0.11 * units * t.Ks, rounds = (double)(blocks * splits) / (2.0 * cus);
     const double lds = one + std::max((rounds - 1.0) * 0.7 * one, (rows * K * 2 + out) / 4.2e6);
     const double codes = 2.5 + rows * K * 2.53 / 4e6 + (choose_codes(t, rows, cus) >= PW_FEW_32 ? 4.0 + 0.05 * t.Ks : tiles_us(t, rows, cus));
     if (codes < lds) return PW16_CODES;

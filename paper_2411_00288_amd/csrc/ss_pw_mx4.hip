@@ -329,24 +329,27 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
 // few rows: then several workgroups share the channels of one's rows.  The next
 // weights are on their way from the L2 while the current ones are multiplied or, with a reduction of one chunk (SHORT), while the sums are finished: that
 // is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
+// (one chunk: four waves, units of 64 channels; longer: eight, of 32, so that the rows are loaded and quantised by twice as many threads)
+constexpr int rows_threads(bool brief) { return brief ? 256 : 512; }
+
 template <int DT, int NT, bool SHORT, bool WIDE>
-__global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
+__global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    constexpr int PX = 32 * NT, PAD = PX + 1;
+    constexpr int PX = 32 * NT, PAD = PX + 1, THREADS = rows_threads(SHORT), WAVES = THREADS / 64, MI = SHORT ? 2 : 1;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = SHORT ? 1 : (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
     const unsigned part = blockIdx.x / r.blocks;
-    const int first = (int)part * r.units * NT, units = min((Mt + 1) / 2, ((int)part + 1) * r.units) * NT;
+    const int first = (int)part * r.units * NT, units = min((Mt + MI - 1) / MI, ((int)part + 1) * r.units) * NT;
     const long long row0 = (long long)(blockIdx.x - part * r.blocks) * PX;
     uint8_t *const codes_s = smem, *const scales_s = smem + 2 * Ks * PAD * 16;
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 256, 0x00020000);
-    u32x4 wa[4][2], wn[4][2];
-    uint32_t sa[2], sn[2];
-    auto fetch = [&](int mt, int q, u32x4 (&w)[4][2], uint32_t (&sc)[2]) {
+    u32x4 wa[4][MI], wn[4][MI];
+    uint32_t sa[MI], sn[MI];
+    auto fetch = [&](int mt, int q, u32x4 (&w)[4][MI], uint32_t (&sc)[MI]) {
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < MI; i++) {
             const int m = min(mt + i, Mt - 1);
             sc[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (m * Kq + q) * 256, 0);
 #pragma unroll
@@ -354,21 +357,21 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
                 w[s][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (m * Ks + min(q * 4 + s, Ks - 1)) * 1024, 0));
         }
     };
-    auto multiply = [&](int at, int q, f32x16 (&acc)[2][1]) {
+    auto multiply = [&](int at, int q, f32x16 (&acc)[MI][1]) {
         const uint32_t sb[1] = {*reinterpret_cast<const uint32_t *>(scales_s + ((q * 2 + half) * PAD + at + lane % 32) * 4)};
 #pragma unroll
         for (int s = 0; s < 4; s++) {
             if (q * 4 + s < Ks) {
                 const u32x4 xb[1] = {*reinterpret_cast<const u32x4 *>(codes_s + ((8 * q + 2 * s + half) * PAD + at + lane % 32) * 16)};
-                step_mx4<2, 1>(s, wa[s], xb, acc, sa, sb);
+                step_mx4<MI, 1>(s, wa[s], xb, acc, sa, sb);
             }
         }
     };
     // The sums start from the bias, which waits in LDS: a load behind the last unit's stores would wait for those, too.
     float *const bias_s = reinterpret_cast<float *>(scales_s + (Kq * 2 * PAD * 4 + 15) / 16 * 16);
-    auto start = [&](int mt, f32x16 (&acc)[2][1]) {
+    auto start = [&](int mt, f32x16 (&acc)[MI][1]) {
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+        for (int i = 0; i < MI; i++)
 #pragma unroll
             for (int g = 0; g < 4; g++) {
                 const f32x4 b = *reinterpret_cast<const f32x4 *>(bias_s + min(mt + i, Mt - 1) * 32 + 8 * g + 4 * half);
@@ -376,44 +379,44 @@ __global__ __launch_bounds__(256, SHORT ? 4 : 3) void pw_mx4_rows_kernel(PwArgs 
                 for (int e = 0; e < 4; e++) acc[i][0][4 * g + e] = b[e];
             }
     };
-    for (int o = threadIdx.x; o < Mt * 32; o += 256) bias_s[o] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
+    for (int o = threadIdx.x; o < Mt * 32; o += THREADS) bias_s[o] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
     if constexpr (SHORT)
-        fetch(min((first + wave) / NT * 2, Mt - 1), 0, wa, sa);
+        fetch(min((first + wave) / NT * MI, Mt - 1), 0, wa, sa);
     else
-        fetch(min((first + wave) / NT * 2, Mt - 1), 0, wn, sn);
-    quantise_rows<DT, 256, SHORT ? 4 : 8, WIDE>(r, row0, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, codes_s, scales_s);
+        fetch(min((first + wave) / NT * MI, Mt - 1), 0, wn, sn);
+    quantise_rows<DT, THREADS, SHORT ? 4 : 8, WIDE>(r, row0, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, codes_s, scales_s);
     __syncthreads();
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
     // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us).
     __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt 0, the first weights: so that the loop is entered with none on their way)
     const auto walk = [&](auto whole, auto stream) {
         constexpr bool ALL = decltype(whole)::value, STREAM = decltype(stream)::value;
-        f32x16 acc[2][1];
+        f32x16 acc[MI][1];
         int unit = first + wave, q = 0;
-        start(unit / NT * 2, acc);
+        start(unit / NT * MI, acc);
         while (unit < units) {
-            const int mt = unit / NT * 2, at = unit % NT * 32;
+            const int mt = unit / NT * MI, at = unit % NT * 32;
             if constexpr (SHORT) {
                 multiply(at, 0, acc);
-                unit += 4;
-                fetch(min(unit / NT * 2, Mt - 1), 0, wa, sa);
-                pw_store<DT, 2, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
+                unit += WAVES;
+                fetch(min(unit / NT * MI, Mt - 1), 0, wa, sa);
+                pw_store<DT, MI, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
                 __builtin_amdgcn_sched_barrier(0);
-                start(unit / NT * 2, acc);
+                start(unit / NT * MI, acc);
             } else {
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
+                for (int i = 0; i < MI; i++) {
                     sa[i] = sn[i];
 #pragma unroll
                     for (int s = 0; s < 4; s++) wa[s][i] = wn[s][i];
                 }
                 const bool done = q + 1 == Kq;
-                const int next = done ? unit + 4 : unit, nq = done ? 0 : q + 1;
-                fetch(min(next / NT * 2, Mt - 1), nq, wn, sn);
+                const int next = done ? unit + WAVES : unit, nq = done ? 0 : q + 1;
+                fetch(min(next / NT * MI, Mt - 1), nq, wn, sn);
                 multiply(at, q, acc);
                 if (done) {
-                    pw_store<DT, 2, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
-                    start(next / NT * 2, acc);
+                    pw_store<DT, MI, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
+                    start(next / NT * MI, acc);
                 }
                 unit = next;
                 q = nq;
@@ -640,13 +643,15 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
         };
         const auto rows = [&](auto nt, auto brief) -> int {
             constexpr int NT = decltype(nt)::value;
-            r.step_row = 256 / runs;
-            r.step_run = 256 % runs;
+            constexpr int THREADS = rows_threads(decltype(brief)::value);
+            r.step_row = THREADS / runs;
+            r.step_run = THREADS % runs;
             const long long blocks = ((long long)a.P + 32 * NT - 1) / (32 * NT);
             const int splits = NT == 1 ? rows_splits(t, a.P, std::max(compute_units(), 1)) : 1;
             r.blocks = (unsigned)blocks;
-            r.units = ((t.Mt + 1) / 2 + splits - 1) / splits;
-            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(blocks * splits, 256, rows_lds(t, 32 * NT), s, a, r);
+            r.units = (decltype(brief)::value ? (t.Mt + 1) / 2 : t.Mt) + splits - 1;
+            r.units /= splits;
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(blocks * splits, THREADS, rows_lds(t, 32 * NT), s, a, r);
         };
         // (as many waves as there are scale words, or as the quantisation keeps busy)
         const int elements = a.P * a.K;
