@@ -143,6 +143,21 @@ __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI
     }
 }
 
+// The product of step s of a scale word.
+template <int MI, int NI>
+__device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x4 (&b)[NI], f32x16 (&acc)[MI][NI], const uint32_t (&sa)[MI], const uint32_t (&sb)[NI])
+{
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+            if (s == 0) acc[i][j] = mma_mx4<0>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+            if (s == 1) acc[i][j] = mma_mx4<1>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+            if (s == 2) acc[i][j] = mma_mx4<2>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+            if (s == 3) acc[i][j] = mma_mx4<3>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+        }
+}
+
 // Large products: four waves, MI x NI tiles of 32 x 32 each, make 64 MI output channels and 64 NI pixels.
 //   weights     straight from memory into registers, in the instruction's own order, three steps (of 64 reduction indices) ahead
 //   activation  256 channels at a time through two LDS buffers, filled from registers that were loaded a chunk earlier; 16-byte pieces trade
@@ -207,67 +222,57 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         for (int i = 0; i < MI; i++)
             to[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (min(mt0 + i, Mt - 1) * Kq + min(q, Kq - 1)) * 256, 0);
     };
+    const int px0 = (wave % 2) * NI * 32, half = lane / 32;
+    u32x4 xb[2][NI];
+    uint32_t sb[NI];
+    auto pixels = [&](int buf, int s, u32x4 (&to)[NI]) {
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+            const int row = px0 + j * 32 + lane % 32, b = 2 * s + half;
+            to[j] = *reinterpret_cast<const u32x4 *>(codes_s[buf] + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16));
+        }
+    };
     f32x16 acc[MI][NI] = {};
     fetch(0);
     weight_scales(0, sa);
 #pragma unroll
     for (int s = 0; s < 3; s++) weights(s, wa[s]);
     fill(0);
+    fetch(1);
     __syncthreads();
-    const int px0 = (wave % 2) * NI * 32, half = lane / 32;
-    // (no branches: the compiler moves matrix instructions behind one, away from their loads; what is fetched behind the last chunk is not used)
+    pixels(0, 0, xb[0]);
+    // One wave to the SIMD has nothing to hide a wait behind but its own matrix instructions, so everything a step needs is asked for a step or more before: the
+    // pixels' next step while the current one is multiplied, the weights three steps ahead, the activation's next chunk written to LDS in step 1, its successor loaded in
+    // step 2, and the barrier stands between step 2 and step 3, in front of the next chunk's first read and behind the last of the current one's.  (With reads at
+    // their step's start and the barrier at the chunk's end 8192^3 took 302 us.)  No branches: the compiler moves matrix instructions behind one, away from
+    // their loads; what is loaded behind the last chunk is not used.
     for (int q = 0; q < Kq; q++) {
         const int buf = q & 1;
-        fetch(q + 1);
-        weight_scales(q + 1, na);
-        uint32_t sb[NI];
 #pragma unroll
         for (int j = 0; j < NI; j++) sb[j] = scales_s[buf][half][px0 + j * 32 + lane % 32];
 #pragma unroll
         for (int s = 0; s < 4; s++) {
             __builtin_amdgcn_sched_barrier(0);              // (loads stay in their step: moved ahead they take more registers than there are)
+            if (s == 3) lds_barrier();
+            pixels(s == 3 ? buf ^ 1 : buf, (s + 1) % 4, xb[(s + 1) % 2]);
             weights(q * 4 + s + 3, wa[(s + 3) % 4]);
-            u32x4 xb[NI];
+            if (s == 0) weight_scales(q + 1, na);
+            if (s == 1) fill(buf ^ 1);
+            if (s == 2) fetch(q + 2);
+            step_mx4<MI, NI>(s, wa[s], xb[s % 2], acc, sa, sb);
 #pragma unroll
-            for (int j = 0; j < NI; j++) {
-                const int row = px0 + j * 32 + lane % 32, b = 2 * s + half;
-                xb[j] = *reinterpret_cast<const u32x4 *>(codes_s[buf] + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16));
+            for (int i = 0; i < MI * NI / 2; i++) {         // between two matrix instructions each, one of the others
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x320, 2, 0);
             }
-#pragma unroll
-            for (int i = 0; i < MI; i++)
-#pragma unroll
-                for (int j = 0; j < NI; j++) {
-                    if (s == 0) acc[i][j] = mma_mx4<0>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
-                    if (s == 1) acc[i][j] = mma_mx4<1>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
-                    if (s == 2) acc[i][j] = mma_mx4<2>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
-                    if (s == 3) acc[i][j] = mma_mx4<3>(wa[s][i], xb[j], acc[i][j], sa[i], sb[j]);
-                }
         }
-        __builtin_amdgcn_sched_barrier(0);
-        fill(buf ^ 1);
 #pragma unroll
         for (int i = 0; i < MI; i++) sa[i] = na[i];
-        lds_barrier();
     }
     if ((mt0 + MI) * 32 <= p.cout && row0 + px0 + NI * 32 <= p.P)              // uniform
         pw_store<DT, MI, NI, true, true, false>(p, acc, mt0, row0 + px0, lane);
     else
         pw_store<DT, MI, NI, false, true, false>(p, acc, mt0, row0 + px0, lane);
-}
-
-// The product of step s of a scale word.
-template <int MI, int NI>
-__device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x4 (&b)[NI], f32x16 (&acc)[MI][NI], const uint32_t (&sa)[MI], const uint32_t (&sb)[NI])
-{
-#pragma unroll
-    for (int i = 0; i < MI; i++)
-#pragma unroll
-        for (int j = 0; j < NI; j++) {
-            if (s == 0) acc[i][j] = mma_mx4<0>(a[i], b[j], acc[i][j], sa[i], sb[j]);
-            if (s == 1) acc[i][j] = mma_mx4<1>(a[i], b[j], acc[i][j], sa[i], sb[j]);
-            if (s == 2) acc[i][j] = mma_mx4<2>(a[i], b[j], acc[i][j], sa[i], sb[j]);
-            if (s == 3) acc[i][j] = mma_mx4<3>(a[i], b[j], acc[i][j], sa[i], sb[j]);
-        }
 }
 
 // 16-bit input rows of a workgroup, quantised into LDS.  Block b of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
