@@ -8,8 +8,9 @@ namespace ss {
 // One thread per run of 8 values, four runs a thread; the quad of lanes that holds a block finds its scale among itself.  Bound by memory: 2 bytes
 // read and 0.53 written for a 16-bit value.  `runs` = 16 * ceil(blocks / 4) to the row, so that a quad is never split between rows and the
 // scales' surplus bytes are written too.
-// WIDE: rows of at least 8.
-template <int DT, bool WIDE>
+// WIDE: rows of at least 8.  LAST: a tensor too large for the caches, whose lines are not kept in them (401408 x 384 to codes and back 151 -> 129 us, 50176 x 768,
+// which fit, 33 -> 36).
+template <int DT, bool WIDE, bool LAST>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char *__restrict__ x, long long ldx, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
                                                            long long total, int cols, unsigned runs, unsigned mul, unsigned sh)
 {
@@ -27,7 +28,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char *__restric
             row[u] = i / runs;
         run[u] = (int)(i - row[u] * runs);
         if constexpr (WIDE)                              // (past the last run: the first row)
-            v[u] = load_wide<DT>(x + (i < total ? row[u] * ldx : 0ll) * item_bytes<DT>(), run[u] * 8, cols);
+            v[u] = load_wide<DT, LAST>(x + (i < total ? row[u] * ldx : 0ll) * item_bytes<DT>(), run[u] * 8, cols);
         else
             v[u] = load_run<DT>(x + (row[u] * ldx + run[u] * 8) * item_bytes<DT>(), i < total ? cols - run[u] * 8 : 0);
     }
@@ -133,11 +134,14 @@ int mx4_quantize(const void *x, int64_t rows, int cols, int64_t ldx, int dtype, 
     const auto go = [&](auto kern) {
         kern<<<dim3((unsigned)blocks), dim3(256), 0, s>>>(static_cast<const char *>(x), (long long)ldx, codes, scales, total, cols, runs, mul, sh);
     };
-    const auto pick = [&](auto wide) {
-        constexpr bool WIDE = decltype(wide)::value;
-        dtype == SS_F16 ? go(mx4_quantize_kernel<SS_F16, WIDE>) : dtype == SS_BF16 ? go(mx4_quantize_kernel<SS_BF16, WIDE>) : go(mx4_quantize_kernel<SS_F32, WIDE>);
+    const auto pick = [&](auto wide, auto last) {
+        constexpr bool WIDE = decltype(wide)::value, LAST = decltype(last)::value;
+        dtype == SS_F16 ? go(mx4_quantize_kernel<SS_F16, WIDE, LAST>) : dtype == SS_BF16 ? go(mx4_quantize_kernel<SS_BF16, WIDE, LAST>) : go(mx4_quantize_kernel<SS_F32, WIDE, LAST>);
     };
-    cols >= 8 ? pick(std::true_type{}) : pick(std::false_type{});
+    if (cols < 8)
+        pick(std::false_type{}, std::false_type{});
+    else
+        rows * (int64_t)cols * (dtype == SS_F32 ? 4 : 2) > 192ll << 20 ? pick(std::true_type{}, std::true_type{}) : pick(std::true_type{}, std::false_type{});
     return launched();
 }
 

@@ -126,17 +126,20 @@ extern "C" int ss_norm_bwd(const ss_norm_desc *d, const ss_norm_grad_io *io, voi
         if (!aligned(v, 4)) return SS_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     NormSumArgs sum{};
-    sum.out[ACC_W] = io->dw; sum.out[ACC_B] = io->db; sum.out[ACC_SCALE] = io->dscale; sum.out[ACC_POST_W] = io->dpost_w; sum.out[ACC_POST_B] = io->dpost_b;
+    float *const outs[ACC_COUNT] = {io->dw, io->db, io->dscale, io->dpost_w, io->dpost_b};       // (in the order of the accumulators)
+    for (int a = 0; a < ACC_COUNT; a++)
+        if (outs[a]) {
+            sum.out[sum.wanted] = outs[a];
+            sum.which[sum.wanted++] = a;
+        }
     sum.cols = d->cols;
-    sum.column_tiles = (d->cols + 15) / 16;
-    bool any = false;
-    for (const float *o : sum.out) any = any || o;
     const auto finish = [&](long long gates) {
         sum.gates = gates;
+        sum.tiles = (d->cols + sum_columns(sum.parts) - 1) / sum_columns(sum.parts);
         d->dtype == SS_F16 ? launch_norm_sum<SS_F16>(sum, s) : d->dtype == SS_BF16 ? launch_norm_sum<SS_BF16>(sum, s) : launch_norm_sum<SS_F32>(sum, s);
         return launched();
     };
-    if (io->rows == 0) return any ? finish(0) : SS_OK;   // sums over no rows
+    if (io->rows == 0) return sum.wanted ? finish(0) : SS_OK;   // sums over no rows
     if (!rows_ok(d, io->dy, io->lddy, norm) || !rows_ok(d, io->x_out, io->ldx_out, norm) || !rows_ok(d, io->dx_out, io->lddx_out, false) ||
         !rows_ok(d, io->h, io->ldh, false) || !rows_ok(d, io->dx, io->lddx, true) || !rows_ok(d, io->dh, io->lddh, io->h != nullptr) ||
         (io->gate && (!aligned(io->gate, d->dtype == SS_F32 ? 4 : 2) || !aligned(io->dgate, d->dtype == SS_F32 ? 4 : 2))))
@@ -159,7 +162,7 @@ extern "C" int ss_norm_bwd(const ss_norm_desc *d, const ss_norm_grad_io *io, voi
     const int started = launched();
     if (started != SS_OK) return started;
     const long long gates = g.gate_part ? (long long)g.groups * a.gate_cols : 0;
-    if (!any && gates == 0) return SS_OK;
+    if (!sum.wanted && gates == 0) return SS_OK;
     sum.part = a.part; sum.gate_part = a.gate_part; sum.dgate = a.dgate;
     sum.parts = g.workgroups; sum.strips = g.strips; sum.gate_cols = a.gate_cols;
     return finish(gates);

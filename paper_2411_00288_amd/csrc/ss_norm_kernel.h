@@ -86,22 +86,24 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*shared)[2][LPR /
     }
 }
 
-// How a row's width meets the lanes' runs of 8: narrower than one, with a last run that is cut, or even.
-enum { NARROW = 0, CUT = 1, EVEN = 2 };
+// How a row's width meets the lanes' runs of 8: narrower than one, with a last run that is cut, or even; and even rows of tensors too large for the caches, whose
+// lines are not kept (401408 x 96, gradient: 104 -> 94 us; of 4096 x 4096, which fit, 57 -> 60).
+enum { NARROW = 0, CUT = 1, EVEN = 2, EVEN_LARGE = 3 };
+constexpr bool even(int mode) { return mode >= EVEN; }
 
 // One for a channel of the row, zero past its end.  (As a factor: values past the end are loaded as zeros, and what is subtracted from them is multiplied by
 // this, so that they stay zeros without a comparison.)
 template <int NV, int MODE>
 struct Inside {
-    float v[NV][MODE == EVEN ? 1 : 8];
+    float v[NV][even(MODE) ? 1 : 8];
     __device__ __forceinline__ Inside(const int (&c)[NV], int cols)
     {
 #pragma unroll
         for (int j = 0; j < NV; j++)
 #pragma unroll
-            for (int e = 0; e < (MODE == EVEN ? 1 : 8); e++) v[j][e] = c[j] + e < cols ? 1.f : 0.f;
+            for (int e = 0; e < (even(MODE) ? 1 : 8); e++) v[j][e] = c[j] + e < cols ? 1.f : 0.f;
     }
-    __device__ __forceinline__ float at(int j, int e) const { return v[j][MODE == EVEN ? 0 : e]; }
+    __device__ __forceinline__ float at(int j, int e) const { return v[j][even(MODE) ? 0 : e]; }
 };
 
 // 1 / sqrt(q), within two units in the last place.  (The instruction alone takes no denormal numbers.)
@@ -123,7 +125,7 @@ __device__ __forceinline__ float normalise(float (&v)[NV][8], const Inside<NV, M
             for (int e = 0; e < 8; e++) s[0] += v[j][e];
         row_sums<LPR>(s, shared, turn);
         const float mean = s[0] * inv;
-        if constexpr (MODE == EVEN) {
+        if constexpr (even(MODE)) {
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const float m = mean * inside.at(j, 0);
@@ -170,7 +172,7 @@ template <int DT, int MODE>
 __device__ __forceinline__ Run<DT> row_run(const char *row, int c, int n, int cols)
 {
     if constexpr (MODE != NARROW)
-        return load_wide<DT>(row, c, cols);
+        return load_wide<DT, MODE == EVEN_LARGE>(row, c, cols);
     else
         return load_run<DT>(row + (long long)c * item_bytes<DT>(), n);
 }
@@ -179,7 +181,7 @@ template <int DT, int MODE>
 __device__ __forceinline__ void row_values(Run<DT> r, int c, int n, int cols, float (&v)[8])
 {
     if constexpr (MODE == CUT) place_wide<DT>(r, c, cols, n > 0);
-    if constexpr (MODE == EVEN) {
+    if constexpr (even(MODE)) {
 #pragma unroll
         for (int k = 0; k < (DT == SS_F32 ? 2 : 1); k++) r.v[k] = n > 0 ? r.v[k] : u32x4{};
     }
@@ -324,25 +326,22 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : g
     const float inv = 1.f / (float)p.cols;
     const Inside<NV, MODE> inside(c, p.cols);
 
-    // sums of the row groups' registers, to dst[0 .. cols)
+    // sums of the row groups' registers: put(first channel, how many, 8 values)
     auto join = [&](const float (&v)[NV][8], auto &&put) {
         if constexpr (R == 1) {
 #pragma unroll
-            for (int j = 0; j < NV; j++)
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (c[j] + e < p.cols) put(c[j] + e, v[j][e]);
+            for (int j = 0; j < NV; j++) put(c[j], p.cols - c[j], v[j]);
         } else {
             static_assert(NV == 1, "one run to the lane");
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; e++) joined[rg * LPR * 8 + c[0] + e] = v[0][e];
+            for (int e = 0; e < 8; e++) joined[rg * LPR * 8 + e * LPR + lane] = v[0][e];
             __syncthreads();
             for (int col = threadIdx.x; col < p.cols; col += THREADS) {
-                float s = 0.f;
+                float s[8] = {};
 #pragma unroll
-                for (int k = 0; k < R; k++) s += joined[k * LPR * 8 + col];
-                put(col, s);
+                for (int k = 0; k < R; k++) s[0] += joined[k * LPR * 8 + col % 8 * LPR + col / 8];
+                put(col, 1, s);
             }
         }
     };
@@ -504,11 +503,11 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : g
                 if (base + R < last) fetch(base + R);
         }
         if (p.grouped && p.gate != nullptr) {
-            auto put = [&](int col, float v) {
+            auto put = [&](int col, int n, const float (&v)[8]) {
                 if (p.strips > 1)
-                    p.gate_part[unit * p.gate_cols + col] = v;
+                    store8<SS_F32>(p.gate_part + unit * p.gate_cols + col, n, v);
                 else
-                    store1<DT>(p.dgate + (group * p.gate_cols + col) * B, v);
+                    store8<DT>(p.dgate + (group * p.gate_cols + col) * B, n, v);
             };
             if constexpr (VECTOR_GATE) {
                 join(gate_acc, put);
@@ -517,14 +516,14 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : g
                 __syncthreads();
                 if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = gate_one;
                 __syncthreads();
-                float s = 0.f;
-                for (int k = 0; k < THREADS / 64; k++) s += waves[k];
-                if (threadIdx.x == 0) put(0, s);
+                float s[8] = {};
+                for (int k = 0; k < THREADS / 64; k++) s[0] += waves[k];
+                if (threadIdx.x == 0) put(0, 1, s);
             }
         }
     }
     const size_t at = (size_t)blockIdx.x * p.cols, step = (size_t)gridDim.x * p.cols;
-    auto part = [&](int a, const float (&v)[NV][8]) { join(v, [&](int col, float s) { p.part[a * step + at + col] = s; }); };
+    auto part = [&](int a, const float (&v)[NV][8]) { join(v, [&](int col, int n, const float (&s)[8]) { store8<SS_F32>(p.part + a * step + at + col, n, s); }); };
     if (p.norm != SS_NORM_NONE) {
         part(ACC_W, acc[ACC_W]);
         part(ACC_B, acc[ACC_B]);
@@ -538,42 +537,57 @@ __global__ __launch_bounds__(grad_threads(LPR, POST), LPR >= 512 || POST ? 0 : g
 
 struct NormSumArgs {
     const float *part, *gate_part;
-    float *out[ACC_COUNT];
+    float *out[ACC_COUNT];                 // those that are wanted, first
+    int which[ACC_COUNT];                  // their accumulators
     char *dgate;
-    int cols, parts, strips, column_tiles;
+    int cols, parts, strips, wanted, tiles;
     long long gates;                       // elements of the gate's gradient that are still in `strips` parts, or 0
     int gate_cols;
 };
 
-// 16 columns to the workgroup, 64 slices of the partial sums; behind those workgroups, one thread for an element of the gate's gradient.
+constexpr int kSumColumns = 16;            // columns of a workgroup where 64 slices of the parts share them
+constexpr int sum_columns(int parts) { return parts > 64 ? kSumColumns : 1024; }
+
+// The workgroups' partial sums: 16 columns to the workgroup and 64 slices of the parts, or, of few parts, a column to the thread.  Behind those workgroups, one thread
+// for an element of the gate's gradient.
 template <int DT>
 __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(NormSumArgs p)
 {
-    __shared__ float s[64][17];
-    const int tiles = p.column_tiles * ACC_COUNT;
-    if ((int)blockIdx.x < tiles) {
-        const int a = blockIdx.x / p.column_tiles, col = (blockIdx.x - a * p.column_tiles) * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
-        if (p.out[a] == nullptr) return;                 // uniform
+    __shared__ float s[64][kSumColumns + 1];
+    const int columns = sum_columns(p.parts), blocks = p.tiles * p.wanted;
+    if ((int)blockIdx.x < blocks) {
+        const int a = blockIdx.x / p.tiles, tile = blockIdx.x - a * p.tiles;
+        const float *const src = p.part + (size_t)p.which[a] * p.parts * p.cols;
+        if (columns != kSumColumns) {
+            const int col = tile * 1024 + threadIdx.x;
+            if (col >= p.cols) return;
+            float v = 0.f;
+#pragma unroll 8
+            for (int i = 0; i < p.parts; i++) v += src[(size_t)i * p.cols + col];
+            p.out[a][col] = v;
+            return;
+        }
+        const int col = tile * kSumColumns + threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns;
         float v = 0.f;
         if (col < p.cols) {
-            const float *src = p.part + (size_t)a * p.parts * p.cols + col;
 #pragma unroll 8
-            for (int i = slice; i < p.parts; i += 64) v += src[(size_t)i * p.cols];
+            for (int i = slice; i < p.parts; i += 64) v += src[(size_t)i * p.cols + col];
         }
-        s[slice][threadIdx.x % 16] = v;
+        s[slice][threadIdx.x % kSumColumns] = v;
         __syncthreads();
         for (int half = 32; half > 0; half >>= 1) {
-            if (slice < half) s[slice][threadIdx.x % 16] += s[slice + half][threadIdx.x % 16];
+            if (slice < half) s[slice][threadIdx.x % kSumColumns] += s[slice + half][threadIdx.x % kSumColumns];
             __syncthreads();
         }
         if (slice == 0 && col < p.cols) p.out[a][col] = s[0][threadIdx.x];
         return;
     }
-    const long long i = (long long)(blockIdx.x - tiles) * 1024 + threadIdx.x;
+    const long long i = (long long)(blockIdx.x - blocks) * 1024 + threadIdx.x;
     if (i >= p.gates) return;
     const long long group = i / p.gate_cols, col = i - group * p.gate_cols;
     const float *src = p.gate_part + group * p.strips * p.gate_cols + col;
     float v = 0.f;
+#pragma unroll 8
     for (int k = 0; k < p.strips; k++) v += src[(long long)k * p.gate_cols];
     store1<DT>(p.dgate + i * item_bytes<DT>(), v);
 }
@@ -590,6 +604,9 @@ inline RowShape row_shape(int cols)
 }
 
 template <int M> using Mode = std::integral_constant<int, M>;
+
+// bytes: what the call reads and writes, against the last-level cache's 256 MB
+inline int width_mode(int cols, long long bytes) { return cols < 8 ? NARROW : cols % 8 ? CUT : bytes > 256ll << 20 ? EVEN_LARGE : EVEN; }
 
 template <int DT>
 void launch_norm(const NormArgs &a, bool mx4, bool post, hipStream_t s)
@@ -615,7 +632,8 @@ void launch_norm(const NormArgs &a, bool mx4, bool post, hipStream_t s)
         }
     };
     const auto widths = [&](auto m, auto ps) {
-        a.cols < 8 ? pick(m, ps, Mode<NARROW>{}) : a.cols % 8 ? pick(m, ps, Mode<CUT>{}) : pick(m, ps, Mode<EVEN>{});
+        const int mode = width_mode(a.cols, (long long)a.rows * a.cols * item_bytes<DT>() * (a.h != nullptr ? 4 : 2));
+        mode == NARROW ? pick(m, ps, Mode<NARROW>{}) : mode == CUT ? pick(m, ps, Mode<CUT>{}) : mode == EVEN ? pick(m, ps, Mode<EVEN>{}) : pick(m, ps, Mode<EVEN_LARGE>{});
     };
     const auto posts = [&](auto m) { post ? widths(m, std::true_type{}) : widths(m, std::false_type{}); };
     mx4 ? posts(std::true_type{}) : posts(std::false_type{});
@@ -640,7 +658,8 @@ void launch_norm_grad(const NormGradArgs &a, bool post, int workgroups, hipStrea
         }
     };
     const auto widths = [&](auto ps, auto vg) {
-        a.cols < 8 ? pick(ps, vg, Mode<NARROW>{}) : a.cols % 8 ? pick(ps, vg, Mode<CUT>{}) : pick(ps, vg, Mode<EVEN>{});
+        const int mode = width_mode(a.cols, (long long)a.rows * a.cols * item_bytes<DT>() * (a.h != nullptr ? 6 : 4));
+        mode == NARROW ? pick(ps, vg, Mode<NARROW>{}) : mode == CUT ? pick(ps, vg, Mode<CUT>{}) : mode == EVEN ? pick(ps, vg, Mode<EVEN>{}) : pick(ps, vg, Mode<EVEN_LARGE>{});
     };
     const auto gates = [&](auto ps) { a.gate != nullptr && (a.gate_cols > 1 || a.cols == 1) ? widths(ps, std::true_type{}) : widths(ps, std::false_type{}); };
     post ? gates(std::true_type{}) : gates(std::false_type{});
@@ -649,7 +668,7 @@ void launch_norm_grad(const NormGradArgs &a, bool post, int workgroups, hipStrea
 template <int DT>
 void launch_norm_sum(const NormSumArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.column_tiles * ACC_COUNT + (a.gates + 1023) / 1024)), block(1024);
+    const dim3 grid((unsigned)(a.tiles * a.wanted + (a.gates + 1023) / 1024)), block(1024);
     norm_grad_sum_kernel<DT><<<grid, block, 0, s>>>(a);
 }
 

@@ -111,10 +111,11 @@ inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
     const double K = t.KB * 32.0, out = rows * t.Mt * 64.0;
     const long long blocks = (rows + 31) / 32, splits = rows_splits(t, rows, cus), units = (t.Mt + splits * 8 - 1) / (splits * 8);
     const double one = 4.0 + 0.0025 * K + 0.11 * units * t.Ks, rounds = (double)(blocks * splits) / (2.0 * cus);
-    const double lds = one + std::max((rounds - 1.0) * 0.7 * one, (rows * K * 2 + out) / 4.2e6);
+    const bool wide = rows >= 128 * cus && fits16(t, rows, PW16_ROWS_128);
+    const double lds = one + std::max((rounds - 1.0) * (wide ? 0.35 : 0.7) * one, (rows * K * 2 + out) / 4.2e6);
     const double codes = 2.5 + rows * K * 2.53 / 4e6 + (choose_codes(t, rows, cus) >= PW_FEW_32 ? 4.0 + 0.05 * t.Ks : tiles_us(t, rows, cus));
     if (codes < lds) return PW16_CODES;
-    return rows >= 128 * cus && fits16(t, rows, PW16_ROWS_128) ? PW16_ROWS_128 : PW16_ROWS;
+    return wide ? PW16_ROWS_128 : PW16_ROWS;
 }
 
 }  // namespace ss

@@ -304,7 +304,7 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
             rn[u] = run;
             if (base + u * THREADS < total) {              // uniform
                 if constexpr (WIDE)
-                    raw[u] = load_wide<DT>(x + (long long)min(row, rows - 1) * (int)r.ldx, run * 8, K);
+                    raw[u] = load_wide<DT, false>(x + (long long)min(row, rows - 1) * (int)r.ldx, run * 8, K);
                 else
                     raw[u] = load_run<DT>(x + (long long)row * (int)r.ldx + run * 8, row < rows ? K - run * 8 : 0);
             }

@@ -13,8 +13,11 @@ __device__ __forceinline__ uint32_t as_bits(float f) { return __builtin_bit_cast
 
 template <int DT> constexpr int item_bytes() { return DT == SS_F32 ? 4 : 2; }
 
-struct __attribute__((packed, aligned(2))) Vec16 { u32x4 v; };
-struct __attribute__((packed, aligned(4))) Vec32 { u32x4 v; };
+typedef u32x4 At2 __attribute__((aligned(2)));
+typedef u32x4 At4 __attribute__((aligned(4)));
+struct Vec16 { At2 v; };
+struct Vec32 { At4 v; };
+static_assert(sizeof(Vec16) == 16 && alignof(Vec16) == 2 && alignof(Vec32) == 4, "16 bytes on an element's boundary");
 
 // One value of type DT at p.
 template <int DT>
@@ -64,17 +67,19 @@ __device__ __forceinline__ Run<DT> load_run(const void *p, int n)
 }
 
 // Channels c .. c + 7 of a row of at least 8: one load from inside the row whatever the lane, so that loads follow each other without a branch between them.
-// place_wide then moves what a lane at the row's end got into place.
-template <int DT>
+// place_wide then moves what a lane at the row's end got into place.  LAST: nobody reads the row again soon, and its lines need not stay in the caches.
+template <int DT, bool LAST>
 __device__ __forceinline__ Run<DT> load_wide(const void *row, int c, int cols)
 {
     const char *const p = static_cast<const char *>(row) + (long long)min(c, cols - 8) * item_bytes<DT>();
     Run<DT> r;
     if constexpr (DT == SS_F32) {
-        r.v[0] = reinterpret_cast<const Vec32 *>(p)[0].v;
-        r.v[1] = reinterpret_cast<const Vec32 *>(p)[1].v;
+        const Vec32 *const v = reinterpret_cast<const Vec32 *>(p);
+        r.v[0] = LAST ? __builtin_nontemporal_load(&v[0].v) : v[0].v;
+        r.v[1] = LAST ? __builtin_nontemporal_load(&v[1].v) : v[1].v;
     } else {
-        r.v[0] = reinterpret_cast<const Vec16 *>(p)->v;
+        const Vec16 *const v = reinterpret_cast<const Vec16 *>(p);
+        r.v[0] = LAST ? __builtin_nontemporal_load(&v->v) : v->v;
     }
     return r;
 }
