@@ -269,3 +269,52 @@ def test_refusals(ss):
     refused(ss.ss_pw_mx4_q_fwd, desc, codes[:, :16], scales, packed)
     refused(ss.ss_pw_mx4_q_fwd, desc, codes, scales[:4], packed)
     refused(ss.ss_pw_mx4_q_fwd, desc, x, scales, packed)
+
+
+# every kernel in turn (ids of include/ss_debug.h): whole tiles and cut ones, less than a scale word of the reduction and several
+@pytest.mark.parametrize("kernel", range(70, 79))
+@pytest.mark.parametrize("rows,cin,cout", [(1, 8, 1), (32, 300, 96), (64, 96, 64), (70, 1000, 100), (128, 64, 256), (300, 544, 320), (517, 256, 70)])
+def test_every_kernel(ss, force_tile, kernel, rows, cin, cout):
+    desc, x, packed, bias, residual, xq, wq = _layer(ss, rows, cin, cout, BF16, 3 * rows + cin)
+    want, bound = ref.pointwise(xq, wq, bias.double().cpu().numpy(), residual.double().cpu().numpy(), ss.SS_ACT_RELU)
+    codes, scales = ss.ss_mx4_quantize(x)
+    force_tile(kernel)
+    if kernel < 75:
+        ref.close(ss.ss_pw_mx4_q_fwd(desc, codes, scales, packed, bias, residual, ss.SS_ACT_RELU), want, bound, BF16, f"kernel {kernel}")
+    else:
+        ref.close(ss.ss_pw_mx4_fwd(desc, x, packed, bias, residual, ss.SS_ACT_RELU), want, bound, BF16, f"kernel {kernel}")
+
+
+def test_small_integers_are_exact(ss, force_tile):
+    """Integers up to 6 with a power of two as each block's scale: every kernel gives the same, exact sums."""
+    rng = np.random.default_rng(3)
+    x = torch.from_numpy(rng.choice([-6.0, -4, -3, -2, -1, 0, 1, 2, 3, 4, 6], (200, 320))).cuda().to(F16)
+    W = torch.from_numpy(rng.choice([-1.0, 0, 0.5, 1], (96, 320))).cuda().to(F16)
+    x[:, ::32] = 4.0                                              # (each block's largest is 4 or 6: scale 1)
+    W[:, ::32] = 1.0                                              # (scale 1/4: all of these values are there)
+    desc = ss.make_desc(96, 320, 1, 1, ss.SS_F16)
+    packed, want = ss.ss_mx4_pack(desc, W), (x.double() @ W.double().t()).cpu()
+    codes, scales = ss.ss_mx4_quantize(x)
+    for kernel in range(70, 75):
+        force_tile(kernel)
+        assert torch.equal(ss.ss_pw_mx4_q_fwd(desc, codes, scales, packed).double().cpu(), want.half().double()), kernel
+    for kernel in range(76, 79):
+        force_tile(kernel)
+        assert torch.equal(ss.ss_pw_mx4_fwd(desc, x, packed).double().cpu(), want.half().double()), kernel
+
+
+def test_outputs_beyond_the_caches(ss):
+    """More than 128 MB of output (whose lines are not kept) and more than 2^31 bytes of it: rows at both ends, and those around the 2^31st byte."""
+    rows, cin, cout = 4200000, 32, 256
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((rows, cin), generator=g, device="cuda").half()
+    W = torch.randn((cout, cin), generator=g, device="cuda").half()
+    desc = ss.make_desc(cout, cin, 1, 1, ss.SS_F16)
+    packed = ss.ss_mx4_pack(desc, W)
+    wq = ref.through_mx4(W.double().cpu().numpy())
+    codes, scales = ss.ss_mx4_quantize(x)
+    around = torch.cat([torch.arange(0, 70), torch.arange(2 ** 22 - 70, 2 ** 22 + 70), torch.arange(rows - 70, rows)])
+    want, bound = ref.pointwise(ref.through_mx4(x[around].double().cpu().numpy()), wq, None, None, 0)
+    for y in (ss.ss_pw_mx4_fwd(desc, x, packed), ss.ss_pw_mx4_q_fwd(desc, codes, scales, packed)):
+        ref.close(y[around], want, bound, F16, "rows")
+        del y
