@@ -1033,6 +1033,10 @@ def ss_norm_fwd(desc: ss_norm_desc, x, w=None, b=None, h=None, scale=None, gate=
 def ss_norm_mx4_fwd(desc: ss_norm_desc, x, w=None, b=None, h=None, scale=None, gate=None, post_w=None, post_b=None, x_out=None, codes=None, scales=None,
                     stream=None):
     """ss_norm_fwd with y in MXFP4: -> (x_out, codes, scales), or (codes, scales) without h."""
+    if stream is None:
+        r = _native.norm_mx4_fwd(desc, x, w, b, h, scale, gate, post_w, post_b, x_out, codes, scales)
+        if r is not None:
+            return r if type(r[0]) is not int else _failed(r, "ss_norm_mx4_fwd")
     return _norm_fwd("ss_norm_mx4_fwd", desc, x, w, b, h, scale, gate, post_w, post_b, x_out, None, codes, scales, stream)
 
 

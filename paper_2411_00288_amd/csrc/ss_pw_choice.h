@@ -44,18 +44,18 @@ inline size_t rows_lds(const Mx4Dims &t, int px)
     return (size_t)2 * t.Ks * (px + 1) * 16 + ((size_t)t.Kq * 2 * (px + 1) * 4 + 15) / 16 * 16 + (size_t)t.Mt * 128;
 }
 
-// Estimated time of the tiled kernels in us.  A compute unit's n tiles of m x m take their loads and stores (a) and their steps (b each) one after the other, and
-// those of the last ones beside each other (c): 64 x 64 tiles a = 0.65, b = 0.08, 128 x 128 2.8 and 0.17, 256 x 256 10 and 0.43.  Measured on 14 layers of
-// 64 -> 256 to 8192 -> 8192 channels and 512 to 200704 rows, among them (estimates / measurements of the three):
-//     64 -> 256 on 200704 rows   39 / 40   39 / 36   42 / 42        1024 -> 256 on 12544        11 / 10     8 / 9    17 / 16
-//     8192 -> 1024 on 12544     140 / 132 101 / 95   65 / 65        8192 -> 8192 on 3136       276 / 259  156 / 164 130 / 141
+// Estimated time of the tiled kernels in us: what a compute unit's tiles cost besides their steps, and a step; small tiles of one unit run beside each other, which hides
+// their beginnings and ends, and, of 128 x 128, short reductions behind their stores.  From 19 layers of 64 -> 256 to 8192 -> 8192 channels and 100 to 401408 rows, among
+// them (estimates / measurements of 64 x 64, 128 x 128 and 256 x 256):
+//     64 -> 256 on 200704 rows   39 / 40   27 / 29   87 / 40        1024 -> 256 on 12544          9 / 9      7 / 7    16 / 13
+//     8192 -> 1024 on 12544     125 / 118  64 / 76   58 / 56        8192 -> 8192 on 3136        250 / 218  126 / 127 116 / 110
 inline double tile_us(const Mx4Dims &t, long long rows, int m, long long cus)
 {
     const double tiles = (double)((t.Mt * 32ll + m - 1) / m) * (double)((rows + m - 1) / m) / (double)cus;
-    const double n = m == 256 || tiles < 4 ? (double)(long long)(tiles + 0.999999) : tiles;
-    if (m == 256) return n * (10.0 + 0.43 * t.Ks);
-    if (m == 128) return 2.2 + n * (2.8 + 0.17 * t.Ks);
-    return 3.2 + 0.65 * n + 0.08 * t.Ks * std::max(n, 1.4);
+    const double whole = (double)(long long)(tiles + 0.999999);
+    if (m == 256) return whole * (10.5 + 0.37 * t.Ks);
+    if (m == 128) return 3.8 + (tiles < 2 ? whole : tiles) * std::max(1.9, 0.8 + 0.146 * t.Ks);
+    return 3.2 + 0.65 * (tiles < 4 ? whole : tiles) + 0.073 * t.Ks * std::max(tiles < 4 ? whole : tiles, 1.4);
 }
 
 inline PwKernel best_tile(const Mx4Dims &t, long long rows, long long cus)
@@ -64,12 +64,13 @@ inline PwKernel best_tile(const Mx4Dims &t, long long rows, long long cus)
     return large < small && large < middle ? PW_TILE_256 : middle < small ? PW_TILE_128 : PW_TILE_64;
 }
 
-// On codes.  Few rows until their workgroups of 32 channels and 32 rows fill the chip (768 -> 2304 on 100 rows, 288 of them: 4.6 us, in tiles 5.1; 4096 -> 4096 on 100, 512
-// of them: 13.3 and 10.5), and of wide layers with long reductions up to 64 rows, two tiles of them to the workgroup (8192 -> 8192 on 33 rows 14.2, in tiles 22.6).
+// On codes.  Few rows until their workgroups of 32 channels and 32 rows fill the chip (768 -> 2304 on 100 rows, 288 of them: 4.6 us, in tiles 4.7; 4096 -> 4096 on 100, 512
+// of them: 13.2 and 8.2), and of wide layers with long reductions up to 48 rows, two tiles of them to the workgroup (8192 -> 8192 on 33 rows 14 us, in tiles 17; on 64
+// 19 and 17).
 inline PwKernel choose_codes(const Mx4Dims &t, long long rows, long long cus)
 {
     if (rows <= 32 || (rows + 31) / 32 * t.Mt <= cus * 5 / 4) return PW_FEW_32;
-    if (rows <= 64 && t.Kq > 8) return PW_FEW_64;
+    if (rows <= 48 && t.Kq > 8) return PW_FEW_64;
     return best_tile(t, rows, cus);
 }
 
@@ -101,8 +102,8 @@ inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
 // On 16-bit input.  Few rows while every workgroup's own quantisation of them is short (1024 -> 4096: 16 rows 4.6 us, and with a quantisation of its own 3.3 + 2.9; 4096 ->
 // 4096: 24 rows 9.1 and 6.3 + 3.0).  Otherwise the shorter estimate: of the kernel that quantises in LDS, whose waves walk down the channels, two workgroups to the compute unit
 // (4 us, 2.6 for each 1024 channels of the reduction and 0.11 a step and 32 channels; what follows the first overlaps, with 4.2 TB/s for what is moved), or of a quantisation at
-// 4 TB/s and the tiled product.  Estimated / measured, the former and the latter: 512 -> 2048 on 100 rows 6.2 / 6.4 and 6.9 / 7.1 us, on 12544 28 / 28 and 34 / 32; 4096 -> 4096 on
-// 1024 rows 22 / 33 and 21 / 26; 64 -> 256 on 200704 36 / 32 and 55 / 46.  128 rows to the workgroup, one tile of them to the wave, with short reductions and many rows (64 -> 256 on
+// 4 TB/s and the tiled product (measured, the former and the latter: 2048 -> 512 on 3136 rows 13 and 14 us, 512 -> 2048 on 12544 28 and 29, 4096 -> 4096 on 2048 47 and 33, 1024 ->
+// 8192 on 12544 135 and 103).  128 rows to the workgroup, one tile of them to the wave, with short reductions and many rows (64 -> 256 on
 // 200704 rows 47 -> 31 us, on 12544 7.4 and 8.2).
 inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
 {
@@ -113,7 +114,7 @@ inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
     const double one = 4.0 + 0.0025 * K + 0.11 * units * t.Ks, rounds = (double)(blocks * splits) / (2.0 * cus);
     const bool wide = rows >= 128 * cus && fits16(t, rows, PW16_ROWS_128);
     const double lds = one + std::max((rounds - 1.0) * (wide ? 0.35 : 0.7) * one, (rows * K * 2 + out) / 4.2e6);
-    const double codes = 2.5 + rows * K * 2.53 / 4e6 + (choose_codes(t, rows, cus) >= PW_FEW_32 ? 4.0 + 0.05 * t.Ks : tiles_us(t, rows, cus));
+    const double codes = 3.2 + rows * K * 2.53 / 4e6 + (choose_codes(t, rows, cus) >= PW_FEW_32 ? 4.0 + 0.05 * t.Ks : tiles_us(t, rows, cus));
     if (codes < lds) return PW16_CODES;
     return wide ? PW16_ROWS_128 : PW16_ROWS;
 }

@@ -158,25 +158,38 @@ __device__ __forceinline__ void step_mx4(int s, const u32x4 (&a)[MI], const u32x
         }
 }
 
-// Large products: four waves, MI x NI tiles of 32 x 32 each, make 64 MI output channels and 64 NI pixels.
+// Waits until at most N of the wave's loads from memory are under way.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
+}
+
+// Large products: four waves of MI x NI tiles of 32 x 32, WM of them across the output channels.
 //   weights     straight from memory into registers, in the instruction's own order, three steps (of 64 reduction indices) ahead
-//   activation  256 channels at a time through two LDS buffers, filled from registers that were loaded a chunk earlier; 16-byte pieces trade
-//               places within their row so that neither the fill nor a wave's read of 32 rows meets a bank twice
-// A reduction past the last block meets zero scales on both sides; rows past the last read zeros from the buffer's end.
-template <int DT, int MI, int NI>
+//   activation  256 channels at a time, straight from memory into one of two LDS buffers, a chunk ahead; 16-byte pieces trade places within their row so that
+//               a wave's read of 32 rows does not meet a bank twice
+// What goes through registers to LDS, or is loaded by two waves, costs: with the activation in registers on its way and 2 x 2 waves of 4 x 4 tiles 8192^3 took 287 us, with loads to
+// LDS 257, with four waves across the channels, 2 x 8 tiles each, none of whose weights another loads, 255; in 128 x 128 tiles 1 x 4 instead of 2 x 2 376 -> 345, and 315 with
+// the pixels' scales, of which a load finds 64 lines, brought for two chunks at a time.
+// A reduction past the last block meets zero scales on both sides; rows past the last are not stored.
+template <int DT, int MI, int NI, int WM>
 __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel(PwArgs p, int tiles_m, int tiles_n)
 {
-    constexpr int BN = 64 * NI, PIECES = BN * kChunk / 256;
-    __shared__ __attribute__((aligned(16))) uint8_t codes_s[2][BN * kChunk * 16];
-    __shared__ uint32_t scales_s[2][2][BN];                // [buffer][half][pixel]: the four steps' bytes
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    constexpr int WN = 4 / WM, BN = 32 * WN * NI, PIECES = BN / 32;
+    // (two variables: reads of one do not wait for loads to the other)
+    __shared__ __attribute__((aligned(16))) uint8_t even_s[BN * kChunk * 16], odd_s[BN * kChunk * 16];
+    constexpr int NW = NI < 4 ? NI : 4;                    // scale words of a read
+    using Words = std::conditional_t<NW == 1, uint32_t, uint32_t __attribute__((ext_vector_type(NW)))>;
+    __shared__ Words scales_s[2][4][BN / NW];              // [pair of chunks][word: two to the chunk][wave and lane]: each of the lane's pixels
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int KB = (p.K + 31) / 32, S = (KB + 3) / 4 * 4, Ks = (KB + 1) / 2, Kq = (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
     // An XCD (workgroups b, b + 8, ...) works on neighbouring tiles, in bands of eight tiles of channels: 32 of them in flight read 8 + 4 panels.
     const int total = tiles_m * tiles_n, xcd = blockIdx.x % 8;
     const int id = xcd * (total / 8) + min(xcd, total % 8) + blockIdx.x / 8;
     const int band = id / (8 * tiles_n), band_m = min(8, tiles_m - band * 8), in_band = id - band * 8 * tiles_n;
     const int tm = band * 8 + in_band % band_m, tn = in_band / band_m;
-    const int mt0 = tm * 2 * MI + __builtin_amdgcn_readfirstlane(wave / 2) * MI;
+    const int mt0 = (tm * WM + wave / WN) * MI;
     const long long row0 = (long long)tn * BN;
     const unsigned pitch = (unsigned)KB * 16u;
     const int rows = (int)min((long long)BN, p.P - row0);
@@ -184,30 +197,29 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.scales) + row0 * S, 0, rows * S, 0x00020000);
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, Mt * Ks * 1024, 0x00020000);
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 256, 0x00020000);
-    u32x4 piece[PIECES];
-    uint32_t ps[2];
-    auto fetch = [&](int q) {                               // chunk q of the activation, to registers
+    constexpr int WORDS = BN / 64;                         // scale words that a thread brings of a pair of chunks
+    const int px = tid % BN, word0 = tid / BN * WORDS;
+    uint32_t ps[WORDS];
+    // (place l%8 of row l/8 of eight holds block l%8 ^ l/8, in every other eight rows with the lowest bit turned)
+    const unsigned from = (unsigned)(wave * 8 + lane / 8) * pitch + (unsigned)(lane % 8 ^ lane / 8 ^ wave % 2) * 16u;
+    auto stage = [&](int q, uint8_t *to) {                  // chunk q of the activation, to LDS; past the last, nothing from memory
+        const unsigned at = q < Kq ? from + (unsigned)q * (kChunk * 16) : 0x80000000u;
 #pragma unroll
-        for (int i = 0; i < PIECES; i++) {
-            const int at = tid + 256 * i, row = at / 8, b = q * kChunk + at % 8;
-            piece[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)(row * pitch + b * 16), 0, 0));
-        }
+        for (int i = 0; i < PIECES; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void *)(to + (i * 4 + wave) * 1024), 16, (int)(at + (unsigned)i * 32u * pitch), 0, 0, 0);
+    };
+    // The scales of a pair of chunks, to registers and on to LDS: a line of them is not loaded twice for two chunks.
+    auto fetch = [&](int pair, int first, int last) {
 #pragma unroll
-        for (int d = 0; d < 2; d++) {
-            const int b = q * kChunk + 4 * d;              // (past a row's scales: past the buffer's end, which reads zero)
-            ps[d] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, b < S ? tid * S + b : -4, 0, 0);
+        for (int d = first; d < last; d++) {
+            const int b = (pair * 4 + word0 + d) * 4;      // (past a row's scales: past the buffer's end, which reads zero)
+            ps[d] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, b < S ? px * S + b : -4, 0, 0);
         }
     };
-    auto fill = [&](int buf) {
+    auto fill = [&](int pair) {
 #pragma unroll
-        for (int i = 0; i < PIECES; i++) {
-            const int at = tid + 256 * i, row = at / 8, b = at % 8;
-            *reinterpret_cast<u32x4 *>(codes_s[buf] + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16)) = piece[i];
-        }
-        if (BN >= 256 || tid < BN) {
-            scales_s[buf][0][tid] = __builtin_amdgcn_perm(ps[1], ps[0], 0x06040200u);
-            scales_s[buf][1][tid] = __builtin_amdgcn_perm(ps[1], ps[0], 0x07050301u);
-        }
+        for (int d = 0; d < WORDS; d++)
+            reinterpret_cast<uint32_t *>(scales_s[pair & 1][word0 + d])[(px / (32 * NI) * 32 + px % 32) * NI + px / 32 % NI] = ps[d];
     };
     u32x4 wa[4][MI];
     uint32_t sa[MI], na[MI];
@@ -222,43 +234,68 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         for (int i = 0; i < MI; i++)
             to[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, lane * 4, (min(mt0 + i, Mt - 1) * Kq + min(q, Kq - 1)) * 256, 0);
     };
-    const int px0 = (wave % 2) * NI * 32, half = lane / 32;
+    const int px0 = (wave % WN) * NI * 32, half = lane / 32;
     u32x4 xb[2][NI];
     uint32_t sb[NI];
-    auto pixels = [&](int buf, int s, u32x4 (&to)[NI]) {
+    auto pixels = [&](const uint8_t *codes_s, int s, u32x4 (&to)[NI]) {
 #pragma unroll
         for (int j = 0; j < NI; j++) {
             const int row = px0 + j * 32 + lane % 32, b = 2 * s + half;
-            to[j] = *reinterpret_cast<const u32x4 *>(codes_s[buf] + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16));
+            to[j] = *reinterpret_cast<const u32x4 *>(codes_s + row * 128 + ((b ^ (row & 7) ^ ((row >> 3) & 1)) * 16));
         }
     };
     f32x16 acc[MI][NI] = {};
-    fetch(0);
+    // (what the loop waits for first comes first: it is compiled to wait for as few younger loads as either way into it has)
+    fetch(0, 0, WORDS);
     weight_scales(0, sa);
+    __builtin_amdgcn_sched_barrier(0);
+    stage(0, even_s);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < 3; s++) weights(s, wa[s]);
     fill(0);
-    fetch(1);
-    __syncthreads();
-    pixels(0, 0, xb[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_loads<3 * MI>();                                   // chunk 0 is there
+    lds_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    stage(1, odd_s);
+    pixels(even_s, 0, xb[0]);
     // One wave to the SIMD has nothing to hide a wait behind but its own matrix instructions, so everything a step needs is asked for a step or more before: the
-    // pixels' next step while the current one is multiplied, the weights three steps ahead, the activation's next chunk written to LDS in step 1, its successor loaded in
-    // step 2, and the barrier stands between step 2 and step 3, in front of the next chunk's first read and behind the last of the current one's.  (With reads at
-    // their step's start and the barrier at the chunk's end 8192^3 took 302 us.)  No branches: the compiler moves matrix instructions behind one, away from
-    // their loads; what is loaded behind the last chunk is not used.
-    for (int q = 0; q < Kq; q++) {
-        const int buf = q & 1;
+    // pixels' next step while the current one is multiplied, the weights three steps ahead, and the barrier stands between step 2 and step 3, in front of the next
+    // chunk's first read and behind the last of the current one's, whose buffer is then filled with the chunk after the next.  No branches: the compiler moves matrix
+    // instructions behind one, away from their loads; what is loaded behind the last chunk is not used.
+    const uint32_t mine_of = half ? 0x07050301u : 0x06040200u;         // the bytes of the lane's blocks
+    auto chunk = [&](int q, auto odd) {
+        constexpr int parity = decltype(odd)::value;
+        uint8_t *const mine = parity ? odd_s : even_s, *const other = parity ? even_s : odd_s;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < NI; j++) sb[j] = scales_s[buf][half][px0 + j * 32 + lane % 32];
+        for (int j = 0; j < NI; j += NW) {
+            const int at = ((wave % WN * 32 + lane % 32) * NI + j) / NW;
+            const Words low = scales_s[q / 2 & 1][2 * parity][at], high = scales_s[q / 2 & 1][2 * parity + 1][at];
+#pragma unroll
+            for (int k = 0; k < NW; k++) {
+                if constexpr (NW == 1)
+                    sb[j] = __builtin_amdgcn_perm(high, low, mine_of);
+                else
+                    sb[j + k] = __builtin_amdgcn_perm(high[k], low[k], mine_of);
+            }
+        }
 #pragma unroll
         for (int s = 0; s < 4; s++) {
             __builtin_amdgcn_sched_barrier(0);              // (loads stay in their step: moved ahead they take more registers than there are)
-            if (s == 3) lds_barrier();
-            pixels(s == 3 ? buf ^ 1 : buf, (s + 1) % 4, xb[(s + 1) % 2]);
+            if (s == 3) {
+                wait_loads<4 * MI + (parity ? 0 : WORDS)>();                   // the next chunk is there: what steps 0 to 2 asked for may be under way
+                lds_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                stage(q + 2, mine);
+            }
+            pixels(s == 3 ? other : mine, (s + 1) % 4, xb[(s + 1) % 2]);
             weights(q * 4 + s + 3, wa[(s + 3) % 4]);
             if (s == 0) weight_scales(q + 1, na);
-            if (s == 1) fill(buf ^ 1);
-            if (s == 2) fetch(q + 2);
+            if (s == 1 && parity == 1) fill(q / 2 + 1);
+            if (s == 1 && parity == 0) fetch(q / 2 + 1, 0, WORDS / 2);
+            if (s == 2 && parity == 0) fetch(q / 2 + 1, WORDS / 2, WORDS);
             step_mx4<MI, NI>(s, wa[s], xb[s % 2], acc, sa, sb);
 #pragma unroll
             for (int i = 0; i < MI * NI / 2; i++) {         // between two matrix instructions each, one of the others
@@ -268,7 +305,14 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
         }
 #pragma unroll
         for (int i = 0; i < MI; i++) sa[i] = na[i];
+    };
+    int q = 0;
+    for (; q + 1 < Kq; q += 2) {
+        chunk(q, std::integral_constant<int, 0>{});
+        chunk(q + 1, std::integral_constant<int, 1>{});
     }
+    if (q < Kq) chunk(q, std::integral_constant<int, 0>{});
+    wait_loads<0>();                                        // (no load to LDS outlives its workgroup)
     if ((mt0 + MI) * 32 <= p.cout && row0 + px0 + NI * 32 <= p.P)              // uniform
         pw_store<DT, MI, NI, true, true, false>(p, acc, mt0, row0 + px0, lane);
     else
@@ -607,11 +651,11 @@ template <int N> using Int = std::integral_constant<int, N>;
 template <int DT>
 int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
 {
-    const auto tile = [&](auto ni) -> int {
-        constexpr int NI = decltype(ni)::value;
-        const long long tm = (t.Mt + 2 * NI - 1) / (2 * NI), tn = ((long long)a.P + 64 * NI - 1) / (64 * NI);
+    const auto tile = [&](auto mi, auto ni, auto wm) -> int {
+        constexpr int MI = decltype(mi)::value, NI = decltype(ni)::value, WM = decltype(wm)::value, BN = 32 * NI * (4 / WM);
+        const long long tm = (t.Mt + MI * WM - 1) / (MI * WM), tn = ((long long)a.P + BN - 1) / BN;
         if (tm * tn > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
-        pw_mx4_tile_kernel<DT, NI, NI><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
+        pw_mx4_tile_kernel<DT, MI, NI, WM><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
         return launched();
     };
     const auto few = [&](auto ni) -> int {
@@ -622,9 +666,9 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
         return launch_lds<pw_mx4_few_kernel<DT, 4, NI, false, false>>(blocks, 256, few_lds(t, 4, 0), s, a, PwRowsArgs{});
     };
     switch (codes_kernel(t, a.P)) {
-        case PW_TILE_64: return tile(Int<1>{});
-        case PW_TILE_128: return tile(Int<2>{});
-        case PW_TILE_256: return tile(Int<4>{});
+        case PW_TILE_64: return tile(Int<1>{}, Int<1>{}, Int<2>{});
+        case PW_TILE_128: return tile(Int<1>{}, Int<4>{}, Int<4>{});
+        case PW_TILE_256: return tile(Int<2>{}, Int<8>{}, Int<4>{});
         case PW_FEW_32: return few(Int<1>{});
         default: return few(Int<2>{});
     }

@@ -627,23 +627,27 @@ bool read_gate(PyObject *o, int64_t cols, at::ScalarType st, const at::Tensor **
 }
 
 // norm_fwd(desc, x, w, b, h, scale, gate, post_w, post_b, x_out, y) -> y, x_out, (x_out, y), (status, row, block) or None
+// norm_mx4_fwd(desc, x, ..., x_out, codes, scales) -> (codes, scales), (x_out, codes, scales), (status, row, block) or None
+template <bool MX4>
 PyObject *norm_fwd(PyObject *const *a, Py_ssize_t n)
 {
     ss_norm_desc d;
     at::ScalarType st;
     Rows x, h;
     ss_norm_io io{};
-    if (n != 11 || !read_named(a[0], "ss_norm_desc", &d) || !row_type(d.dtype, &st) || !read_rows(a[1], &x) || x.t->size(-1) != d.cols ||
+    if (n != (MX4 ? 12 : 11) || !read_named(a[0], "ss_norm_desc", &d) || !row_type(d.dtype, &st) || !read_rows(a[1], &x) || x.t->size(-1) != d.cols ||
         x.t->scalar_type() != st || !read_channels(a[2], d.cols, &io.w) || !read_channels(a[3], d.cols, &io.b) || !read_channels(a[5], d.cols, &io.scale) ||
         !read_channels(a[7], d.cols, &io.post_w) || !read_channels(a[8], d.cols, &io.post_b))
         Py_RETURN_NONE;
     const at::Tensor *gate;
     if ((a[4] != Py_None && !read_rows(a[4], x.rows, d.cols, st, &h)) || !read_gate(a[6], d.cols, st, &gate, &io.groups, &io.gate_cols)) Py_RETURN_NONE;
     const bool norm = d.norm != SS_NORM_NONE;
-    if ((!h.t && a[9] != Py_None) || (!norm && (!h.t || a[10] != Py_None))) Py_RETURN_NONE;
-    at::Tensor x_out, y;
+    if ((!h.t && a[9] != Py_None) || (!norm && (MX4 || !h.t || a[10] != Py_None))) Py_RETURN_NONE;
+    at::Tensor x_out, y, scales;
     if (h.t && !rows_out(a[9], *x.t, x.rows, d.cols, st, &x_out, &io.ldx_out)) Py_RETURN_NONE;
-    if (norm && !rows_out(a[10], *x.t, x.rows, d.cols, st, &y, &io.ldy)) Py_RETURN_NONE;
+    if (MX4 ? !bytes_out(a[10], *x.t, x.rows, mx4_code_bytes(d.cols), &y) || !bytes_out(a[11], *x.t, x.rows, mx4_scale_bytes(d.cols), &scales)
+            : norm && !rows_out(a[10], *x.t, x.rows, d.cols, st, &y, &io.ldy))
+        Py_RETURN_NONE;
     io.rows = x.rows;
     io.x = x.t->const_data_ptr();
     io.ldx = x.ld;
@@ -651,10 +655,16 @@ PyObject *norm_fwd(PyObject *const *a, Py_ssize_t n)
     io.ldh = h.ld;
     io.gate = gate ? gate->const_data_ptr() : nullptr;
     io.x_out = h.t ? x_out.data_ptr() : nullptr;
-    io.y = norm ? y.data_ptr() : nullptr;
+    if (MX4) {
+        io.codes = y.data_ptr();
+        io.scales = scales.data_ptr();
+    } else if (norm) {
+        io.y = y.data_ptr();
+    }
     const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
     const int status = unlocked([&] { return ss_norm_fwd(&d, &io, s); });
     if (status != SS_OK) return refuse(status);
+    if (MX4) return h.t ? give_all({give(a[9], x_out), give(a[10], y), give(a[11], scales)}) : give_all({give(a[10], y), give(a[11], scales)});
     if (!h.t) return give(a[10], y);
     return norm ? give_all({give(a[9], x_out), give(a[10], y)}) : give(a[9], x_out);
 }
@@ -900,7 +910,8 @@ PyMethodDef methods[] = {
     {"mx4_quantize", reinterpret_cast<PyCFunction>(entry<mx4_quantize>), METH_FASTCALL, nullptr},
     {"mx4_dequantize", reinterpret_cast<PyCFunction>(entry<mx4_dequantize>), METH_FASTCALL, nullptr},
     {"pw_mx4", reinterpret_cast<PyCFunction>(entry<pw_mx4>), METH_FASTCALL, nullptr},
-    {"norm_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd>), METH_FASTCALL, nullptr},
+    {"norm_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd<false>>), METH_FASTCALL, nullptr},
+    {"norm_mx4_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd<true>>), METH_FASTCALL, nullptr},
     {"norm_bwd", reinterpret_cast<PyCFunction>(entry<norm_bwd>), METH_FASTCALL, nullptr},
     {"launch", launch, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
