@@ -173,7 +173,7 @@ __device__ __forceinline__ void wait_loads()
 // LDS 257, with four waves across the channels, 2 x 8 tiles each, none of whose weights another loads, 255; in 128 x 128 tiles 1 x 4 instead of 2 x 2 376 -> 345, and 315 with
 // the pixels' scales, of which a load finds 64 lines, brought for two chunks at a time.
 // A reduction past the last block meets zero scales on both sides; rows past the last are not stored.
-template <int DT, int MI, int NI, int WM>
+template <int DT, int MI, int NI, int WM, bool STREAM>
 __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel(PwArgs p, int tiles_m, int tiles_n)
 {
     constexpr int WN = 4 / WM, BN = 32 * WN * NI, PIECES = BN / 32;
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
     if (q < Kq) chunk(q, std::integral_constant<int, 0>{});
     wait_loads<0>();                                        // (no load to LDS outlives its workgroup)
     if ((mt0 + MI) * 32 <= p.cout && row0 + px0 + NI * 32 <= p.P)              // uniform
-        pw_store<DT, MI, NI, true, true, false>(p, acc, mt0, row0 + px0, lane);
+        pw_store<DT, MI, NI, true, true, STREAM>(p, acc, mt0, row0 + px0, lane);
     else
         pw_store<DT, MI, NI, false, true, false>(p, acc, mt0, row0 + px0, lane);
 }
@@ -330,7 +330,7 @@ struct PwRowsArgs {
     unsigned mul, sh;                      // division by a row's runs, 8 Ks
     int step_row, step_run;                // the kernel's threads over and modulo the runs
     unsigned blocks;                       // workgroups that share the rows (the others take other output channels)
-    int units;                             // units of 64 channels of a workgroup
+    int units;                             // units of output channels of a workgroup: 64 of them with one chunk, 32 with more
 };
 
 template <int DT, int THREADS, int U, bool WIDE>
@@ -373,12 +373,12 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
     }
 }
 
-// Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its four waves take units of 64 output channels and 32 rows
-// in turn (the units of one 64 channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels, unless there are
-// few rows: then several workgroups share the channels of one's rows.  The next
-// weights are on their way from the L2 while the current ones are multiplied or, with a reduction of one chunk (SHORT), while the sums are finished: that
-// is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
-// (one chunk: four waves, units of 64 channels; longer: eight, of 32, so that the rows are loaded and quantised by twice as many threads)
+// Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its waves take units of output channels and 32 rows in turn (the
+// units of the same channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels, unless there are few
+// rows: then several workgroups share the channels of one's rows.  The next weights are on their way from the L2 while the current ones are multiplied or, with a
+// reduction of one chunk (SHORT), while the sums are finished: that is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
+// One chunk: four waves, units of 64 channels; longer: eight, of 32, so that the rows are loaded and quantised by twice as many threads (1024 -> 256 on 12544 rows
+// 13.9 -> 12.2 us).  Bound by memory: 96 -> 384 on 401408 rows 95 us (4.1 TB/s), with GELU 100 to 106; 96 -> 96 34 us (4.5 TB/s).
 constexpr int rows_threads(bool brief) { return brief ? 256 : 512; }
 
 template <int DT, int NT, bool SHORT, bool WIDE>
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwA
 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
 // the reduction, a chunk each in turn, and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first
-// weights are on their way.
+// weights are on their way.  2048 -> 1000 on one row 3.6 us, 8192 -> 8192 on 16 rows on codes 10 us (36 MB of weights and scales at 3.5 TB/s).
 template <int DT, int NW, int NI, bool QUANT, bool WIDE>
 __global__ __launch_bounds__(NW * 64) void pw_mx4_few_kernel(PwArgs p, PwRowsArgs r)
 {
@@ -625,9 +625,9 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
-    // An output of more than half the last-level cache is gone from it before anyone reads it, and its lines leave in the order of their rows only if they are not
-    // kept: 401408 x 96 -> 384 (308 MB) 138 -> 101 us, 192 channels (154 MB) 50.0 -> 49.1, 96 (77 MB) 33.5 -> 32.8 on its own.
-    a.stream = (long long)rows * d->cout * 2 > 128ll << 20;
+    // The lines of an output larger than the last-level cache are gone from it before anyone reads them, and leave in the order of their rows only if they are not
+    // kept: 96 -> 384 on 401408 rows (308 MB) in tiles 104 -> 88 us, with rows in LDS 126 -> 96; of 154 MB, on 200704 rows, 38 -> 44 and 46 -> 52.
+    a.stream = (long long)rows * d->cout * 2 > 256ll << 20;
     return a;
 }
 
@@ -655,15 +655,19 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
         constexpr int MI = decltype(mi)::value, NI = decltype(ni)::value, WM = decltype(wm)::value, BN = 32 * NI * (4 / WM);
         const long long tm = (t.Mt + MI * WM - 1) / (MI * WM), tn = ((long long)a.P + BN - 1) / BN;
         if (tm * tn > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
-        pw_mx4_tile_kernel<DT, MI, NI, WM><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
+        if (a.stream)
+            pw_mx4_tile_kernel<DT, MI, NI, WM, true><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
+        else
+            pw_mx4_tile_kernel<DT, MI, NI, WM, false><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
         return launched();
     };
     const auto few = [&](auto ni) -> int {
         constexpr int NI = decltype(ni)::value;
         const long long blocks = ((long long)a.P + 32 * NI - 1) / (32 * NI) * t.Mt;
-        if (t.Kq > 8) return launch_lds<pw_mx4_few_kernel<DT, 16, NI, false, false>>(blocks, 1024, few_lds(t, 16, 0), s, a, PwRowsArgs{});
-        if (t.Kq > 4) return launch_lds<pw_mx4_few_kernel<DT, 8, NI, false, false>>(blocks, 512, few_lds(t, 8, 0), s, a, PwRowsArgs{});
-        return launch_lds<pw_mx4_few_kernel<DT, 4, NI, false, false>>(blocks, 256, few_lds(t, 4, 0), s, a, PwRowsArgs{});
+        if (NI == 2 || t.Kq > 8) return launch_lds<pw_mx4_few_kernel<DT, 16, NI, false, false>>(blocks, 1024, few_lds(t, 16, 0), s, a, PwRowsArgs{});
+        if constexpr (NI == 1)              // (two tiles of rows are for long reductions)
+            return t.Kq > 4 ? launch_lds<pw_mx4_few_kernel<DT, 8, NI, false, false>>(blocks, 512, few_lds(t, 8, 0), s, a, PwRowsArgs{})
+                            : launch_lds<pw_mx4_few_kernel<DT, 4, NI, false, false>>(blocks, 256, few_lds(t, 4, 0), s, a, PwRowsArgs{});
     };
     switch (codes_kernel(t, a.P)) {
         case PW_TILE_64: return tile(Int<1>{}, Int<1>{}, Int<2>{});
