@@ -9,6 +9,8 @@ namespace ss {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 struct __attribute__((packed, aligned(2))) Half16 { u32x2 v; };        // four 16-bit values
 
+template <int N> using Int = std::integral_constant<int, N>;
+
 struct PwArgs {
     const uint8_t *codes, *scales;         // quantised activation
     const uint8_t *w;                      // first weight tile
@@ -46,10 +48,10 @@ __device__ __forceinline__ f32x16 tile_bias(const PwArgs &p, int o0, int half)
     return s;
 }
 
-// A 32 x 32 tile of sums, finished and stored: residual, activation, rounding, and whole 16-byte runs where the channels allow it.  ALL: the tile ends
-// within the matrix.  BIAS: it is not in the sums yet.  STREAM: the output's lines are not kept in the caches.
-template <int DT, bool ALL, bool BIAS, bool STREAM>
-__device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, const f32x16 &bias, int o0, long long px0, int half)
+// A 32 x 32 tile of sums, finished: residual, activation, rounding.  A lane gets channels lane / 16 % 2 * 16 + half * 8 to 7 more of pixels lane % 16 and 16 more.  ALL: the
+// tile ends within the matrix.  BIAS: it is not in the sums yet.
+template <int DT, bool ALL, bool BIAS>
+__device__ __forceinline__ void finish_tile(const PwArgs &p, const f32x16 &acc, const f32x16 &bias, int o0, long long px0, int half, u32x4 (&run)[2])
 {
     const long long px = px0 + threadIdx.x % 32;
     const bool in = ALL || px < p.P;
@@ -90,7 +92,6 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, c
         d[q][0] = cvt_pack2<DT>(z[4 * q], z[4 * q + 1]);
         d[q][1] = cvt_pack2<DT>(z[4 * q + 2], z[4 * q + 3]);
     }
-    u32x4 run[2];
 #pragma unroll
     for (int q = 0; q < 2; q++)
 #pragma unroll
@@ -106,17 +107,32 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, c
         run[0][e] = s[0];
         run[1][e] = s[1];
     }
-    const int lane = threadIdx.x % 64, o = o0 + lane / 16 % 2 * 16 + half * 8;
+}
+
+// How an output leaves: by the caches, past them, or past them in whole lines where two tiles of 32 channels stand side by side.  (Whole lines where the caches do not put them
+// together: 96 -> 384 on 401408 rows 98 -> 66 us; of 154 MB, which they do, 46 -> 49.  With a GELU the vector ALU has no time for the trade: 100 and 103.)
+enum { KEPT = 0, PAST = 1, LINES = 2 };
+
+template <bool STREAM>
+__device__ __forceinline__ void store_run(uint16_t *dst, const u32x4 &v)
+{
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(v, &reinterpret_cast<Vec16 *>(dst)->v);
+    else
+        reinterpret_cast<Vec16 *>(dst)->v = v;
+}
+
+template <int DT, bool ALL, bool STREAM>
+__device__ __forceinline__ void store_tile(const PwArgs &p, const u32x4 (&run)[2], int o0, long long px0, int lane)
+{
+    const int o = o0 + lane / 16 % 2 * 16 + lane / 32 * 8;
 #pragma unroll
     for (int q = 0; q < 2; q++) {
         const long long to = px0 + 16 * q + lane % 16;
         if (!ALL && to >= p.P) continue;
         uint16_t *dst = p.y + to * p.ldy + o;
         if (ALL || o + 8 <= p.cout) {
-            if constexpr (STREAM)
-                __builtin_nontemporal_store(run[q], &reinterpret_cast<Vec16 *>(dst)->v);
-            else
-                reinterpret_cast<Vec16 *>(dst)->v = run[q];
+            store_run<STREAM>(dst, run[q]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; e++)
@@ -125,21 +141,47 @@ __device__ __forceinline__ void store_tile(const PwArgs &p, const f32x16 &acc, c
     }
 }
 
+// Two tiles of 64 channels side by side: every other eight pixels of the one are traded for the other's, so that a store writes all 128 bytes, a cache line, of 8 pixels.
+__device__ __forceinline__ void store_pair(const PwArgs &p, const u32x4 (&left)[2], const u32x4 (&right)[2], int o0, long long px0, int lane)
+{
+    const bool upper = lane & 8;
+    uint16_t *const dst = p.y + (px0 + lane % 8) * p.ldy + o0 + upper * 32 + lane / 16 % 2 * 16 + lane / 32 * 8;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        u32x4 low, high;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t a = left[q][e], b = right[q][e];
+            const uint32_t from_a = (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x128, 0xF, 0xF, true), from_b = (uint32_t)__builtin_amdgcn_mov_dpp((int)b, 0x128, 0xF, 0xF, true);
+            low[e] = upper ? from_b : a;
+            high[e] = upper ? b : from_a;
+        }
+        store_run<true>(dst + 16 * q * p.ldy, low);
+        store_run<true>(dst + (16 * q + 8) * p.ldy, high);
+    }
+}
+
 // A wave's MI x NI tiles, from row tile mt0 and pixel px0 on.  BIAS: it is not in the sums yet.
-template <int DT, int MI, int NI, bool ALL, bool BIAS, bool STREAM>
+template <int DT, int MI, int NI, bool ALL, bool BIAS, int OUT>
 __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI][NI], int mt0, long long px0, int lane)
 {
+    constexpr bool lines = MI == 2 && ALL && OUT == LINES;
+    f32x16 bias[MI] = {};
+    if constexpr (BIAS)
 #pragma unroll
-    for (int i = 0; i < MI; i++) {
-        const int o0 = (mt0 + i) * 32;
-        if (!ALL && o0 >= p.cout) return;
-        f32x16 bias = {};
-        if constexpr (BIAS) bias = tile_bias<ALL>(p, o0, lane / 32);
+        for (int i = 0; i < MI; i++) bias[i] = tile_bias<ALL>(p, (mt0 + i) * 32, lane / 32);
 #pragma unroll
-        for (int j = 0; j < NI; j++) {
+    for (int j = 0; j < NI; j++) {
+        u32x4 run[MI][2];
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
             __builtin_amdgcn_sched_barrier(0);
-            store_tile<DT, ALL, BIAS, STREAM>(p, acc[i][j], bias, o0, px0 + j * 32, lane / 32);
+            const int o0 = (mt0 + i) * 32;
+            if (!ALL && o0 >= p.cout) break;
+            finish_tile<DT, ALL, BIAS>(p, acc[i][j], bias[i], o0, px0 + j * 32, lane / 32, run[i]);
+            if constexpr (!lines) store_tile<DT, ALL, OUT != KEPT>(p, run[i], o0, px0 + j * 32, lane);
         }
+        if constexpr (lines) store_pair(p, run[0], run[1], mt0 * 32, px0 + j * 32, lane);
     }
 }
 
@@ -173,7 +215,7 @@ __device__ __forceinline__ void wait_loads()
 // LDS 257, with four waves across the channels, 2 x 8 tiles each, none of whose weights another loads, 255; in 128 x 128 tiles 1 x 4 instead of 2 x 2 376 -> 345, and 315 with
 // the pixels' scales, of which a load finds 64 lines, brought for two chunks at a time.
 // A reduction past the last block meets zero scales on both sides; rows past the last are not stored.
-template <int DT, int MI, int NI, int WM, bool STREAM>
+template <int DT, int MI, int NI, int WM, int OUT>
 __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel(PwArgs p, int tiles_m, int tiles_n)
 {
     constexpr int WN = 4 / WM, BN = 32 * WN * NI, PIECES = BN / 32;
@@ -308,15 +350,15 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_mx4_tile_kernel
     };
     int q = 0;
     for (; q + 1 < Kq; q += 2) {
-        chunk(q, std::integral_constant<int, 0>{});
-        chunk(q + 1, std::integral_constant<int, 1>{});
+        chunk(q, Int<0>{});
+        chunk(q + 1, Int<1>{});
     }
-    if (q < Kq) chunk(q, std::integral_constant<int, 0>{});
+    if (q < Kq) chunk(q, Int<0>{});
     wait_loads<0>();                                        // (no load to LDS outlives its workgroup)
     if ((mt0 + MI) * 32 <= p.cout && row0 + px0 + NI * 32 <= p.P)              // uniform
-        pw_store<DT, MI, NI, true, true, STREAM>(p, acc, mt0, row0 + px0, lane);
+        pw_store<DT, MI, NI, true, true, OUT>(p, acc, mt0, row0 + px0, lane);
     else
-        pw_store<DT, MI, NI, false, true, false>(p, acc, mt0, row0 + px0, lane);
+        pw_store<DT, MI, NI, false, true, KEPT>(p, acc, mt0, row0 + px0, lane);
 }
 
 // 16-bit input rows of a workgroup, quantised into LDS.  Block b of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
@@ -378,7 +420,7 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
 // rows: then several workgroups share the channels of one's rows.  The next weights are on their way from the L2 while the current ones are multiplied or, with a
 // reduction of one chunk (SHORT), while the sums are finished: that is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
 // One chunk: four waves, units of 64 channels; longer: eight, of 32, so that the rows are loaded and quantised by twice as many threads (1024 -> 256 on 12544 rows
-// 13.9 -> 12.2 us).  Bound by memory: 96 -> 384 on 401408 rows 95 us (4.1 TB/s), with GELU 100 to 106; 96 -> 96 34 us (4.5 TB/s).
+// 13.9 -> 12.2 us).  Bound by memory: 96 -> 384 on 401408 rows 66 us (5.8 TB/s), 96 -> 96 34 us (4.5 TB/s); by the vector ALU with a GELU, the former 100 to 106.
 constexpr int rows_threads(bool brief) { return brief ? 256 : 512; }
 
 template <int DT, int NT, bool SHORT, bool WIDE>
@@ -436,10 +478,11 @@ __global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwA
     quantise_rows<DT, THREADS, SHORT ? 4 : 8, WIDE>(r, row0, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, codes_s, scales_s);
     __syncthreads();
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
-    // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us).
+    // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us, then).
     __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt 0, the first weights: so that the loop is entered with none on their way)
-    const auto walk = [&](auto whole, auto stream) {
-        constexpr bool ALL = decltype(whole)::value, STREAM = decltype(stream)::value;
+    const auto walk = [&](auto whole, auto out) {
+        constexpr bool ALL = decltype(whole)::value;
+        constexpr int OUT = decltype(out)::value;
         f32x16 acc[MI][1];
         int unit = first + wave, q = 0;
         start(unit / NT * MI, acc);
@@ -449,7 +492,7 @@ __global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwA
                 multiply(at, 0, acc);
                 unit += WAVES;
                 fetch(min(unit / NT * MI, Mt - 1), 0, wa, sa);
-                pw_store<DT, MI, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
+                pw_store<DT, MI, 1, ALL, false, OUT>(p, acc, mt, row0 + at, lane);
                 __builtin_amdgcn_sched_barrier(0);
                 start(unit / NT * MI, acc);
             } else {
@@ -464,7 +507,7 @@ __global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwA
                 fetch(min(next / NT * MI, Mt - 1), nq, wn, sn);
                 multiply(at, q, acc);
                 if (done) {
-                    pw_store<DT, MI, 1, ALL, false, STREAM>(p, acc, mt, row0 + at, lane);
+                    pw_store<DT, MI, 1, ALL, false, OUT>(p, acc, mt, row0 + at, lane);
                     start(next / NT * MI, acc);
                 }
                 unit = next;
@@ -473,9 +516,13 @@ __global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwA
         }
     };
     if (p.cout % 64 != 0 || row0 + PX > p.P)
-        walk(std::false_type{}, std::false_type{});
-    else
-        p.stream ? walk(std::true_type{}, std::true_type{}) : walk(std::true_type{}, std::false_type{});
+        walk(std::false_type{}, Int<KEPT>{});
+    else if (!p.stream)
+        walk(std::true_type{}, Int<KEPT>{});
+    else if (!SHORT || p.act == SS_ACT_GELU)
+        walk(std::true_type{}, Int<PAST>{});
+    else if constexpr (SHORT)
+        walk(std::true_type{}, Int<LINES>{});
 }
 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
@@ -626,7 +673,7 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     a.K = d->cin;
     a.act = act;
     // The lines of an output larger than the last-level cache are gone from it before anyone reads them, and leave in the order of their rows only if they are not
-    // kept: 96 -> 384 on 401408 rows (308 MB) in tiles 104 -> 88 us, with rows in LDS 126 -> 96; of 154 MB, on 200704 rows, 38 -> 44 and 46 -> 52.
+    // kept: 96 -> 384 on 401408 rows (308 MB) in tiles 104 -> 88 us, with rows in LDS 126 -> 96 (and 66 in whole lines); of 154 MB, on 200704 rows, 38 -> 44 and 46 -> 52.
     a.stream = (long long)rows * d->cout * 2 > 256ll << 20;
     return a;
 }
@@ -646,8 +693,6 @@ PwKernel kernel16(const Mx4Dims &t, long long rows)
     return choose16(t, rows, std::max(compute_units(), 1));
 }
 
-template <int N> using Int = std::integral_constant<int, N>;
-
 template <int DT>
 int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
 {
@@ -656,9 +701,9 @@ int product_codes(const PwArgs &a, const Mx4Dims &t, hipStream_t s)
         const long long tm = (t.Mt + MI * WM - 1) / (MI * WM), tn = ((long long)a.P + BN - 1) / BN;
         if (tm * tn > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
         if (a.stream)
-            pw_mx4_tile_kernel<DT, MI, NI, WM, true><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
+            pw_mx4_tile_kernel<DT, MI, NI, WM, LINES><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
         else
-            pw_mx4_tile_kernel<DT, MI, NI, WM, false><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
+            pw_mx4_tile_kernel<DT, MI, NI, WM, KEPT><<<dim3((unsigned)(tm * tn)), dim3(256), 0, s>>>(a, (int)tm, (int)tn);
         return launched();
     };
     const auto few = [&](auto ni) -> int {
