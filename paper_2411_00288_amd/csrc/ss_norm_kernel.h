@@ -4,7 +4,8 @@
 //
 // post and norm: none, LayerNorm or RMS over the channels of a row.  A row lives in the registers of `LPR` lanes, 8 channels to the lane (NV runs of
 // 8 in the widest rows), from its only read to its only write; means and sums of squares are fp32, the variance is the mean square of the
-// differences from the mean.  Bound by memory.
+// differences from the mean.  Bound by memory: 401408 x 96, x, h and two outputs, LayerNorm, 61 us (5.0 TB/s), a copy's rate; calls of a few rows by their launch and one
+// memory latency (4 x 4096 with both norms 3.6 us).
 #ifndef SS_NORM_KERNEL_H_
 #define SS_NORM_KERNEL_H_
 #include "ss_mx4.h"
@@ -302,6 +303,8 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_kernel(NormArgs p)
 //     dx = t,  dw = sum dy xh,  db = sum dy,  dscale = sum t gate u,  dgate = sum t scale u,  du = t scale gate,  and the same through post.
 // Statistics are found again from the rows, which have to be read anyway.  Sums over rows: a workgroup's own rows in registers, in their order,
 // then its partial sums in the workspace, which norm_grad_sum_kernel adds in a fixed order: the same bits every time.
+// 401408 x 96 without post norm 94 us (4.9 TB/s).  With a post norm the sums are a chain of five joins to a row, and five accumulators and four vectors leave one workgroup to
+// the compute unit: 2049 x 1001 26 us, three rounds of rows at 2 to 3 us each, then the sums' launch (4 us); 4096 x 4096 in bfloat16 35 and 7 us.
 enum { ACC_W = 0, ACC_B, ACC_SCALE, ACC_POST_W, ACC_POST_B, ACC_COUNT };
 
 // Waves to the SIMD: what the registers of a kernel without post norm leave.
