@@ -419,15 +419,14 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
 // units of the same channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels, unless there are few
 // rows: then several workgroups share the channels of one's rows.  The next weights are on their way from the L2 while the current ones are multiplied or, with a
 // reduction of one chunk (SHORT), while the sums are finished: that is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
-// One chunk: four waves, units of 64 channels; longer: eight, of 32, so that the rows are loaded and quantised by twice as many threads (1024 -> 256 on 12544 rows
-// 13.9 -> 12.2 us).  Bound by memory: 96 -> 384 on 401408 rows 66 us (5.8 TB/s), 96 -> 96 34 us (4.5 TB/s); by the vector ALU with a GELU, the former 100 to 106.
-constexpr int rows_threads(bool brief) { return brief ? 256 : 512; }
-
-template <int DT, int NT, bool SHORT, bool WIDE>
-__global__ __launch_bounds__(rows_threads(SHORT), 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
+// One chunk: four waves, units of 64 channels; longer: units of 32, and eight waves, so that the rows are loaded and quantised by twice as many threads (1024 -> 256 on 12544 rows
+// 13.9 -> 12.2 us), or, of many rows, four (384 -> 96 on 401408 rows 109 -> 77 us, 512 -> 256 on 50176 23 -> 22; of few, 1024 -> 128 on 3136, 7.6 and 9.2).
+// Bound by memory: 96 -> 384 on 401408 rows 66 us (5.8 TB/s), 96 -> 96 34 us (4.5 TB/s); by the vector ALU with a GELU, the former 100 to 106.
+template <int DT, int NT, bool SHORT, bool WIDE, int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    constexpr int PX = 32 * NT, PAD = PX + 1, THREADS = rows_threads(SHORT), WAVES = THREADS / 64, MI = SHORT ? 2 : 1;
+    constexpr int PX = 32 * NT, PAD = PX + 1, WAVES = THREADS / 64, MI = SHORT ? 2 : 1;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const int KB = (p.K + 31) / 32, Ks = (KB + 1) / 2, Kq = SHORT ? 1 : (Ks + 3) / 4, Mt = (p.cout + 31) / 32;
     const unsigned part = blockIdx.x / r.blocks;
@@ -739,9 +738,8 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
             r.step_run = NW * 64 % runs;
             return launch_lds<pw_mx4_few_kernel<DT, NW, 1, true, WIDE>>(t.Mt, NW * 64, few_lds(t, NW, a.P), s, a, r);
         };
-        const auto rows = [&](auto nt, auto brief) -> int {
-            constexpr int NT = decltype(nt)::value;
-            constexpr int THREADS = rows_threads(decltype(brief)::value);
+        const auto rows = [&](auto nt, auto brief, auto threads) -> int {
+            constexpr int NT = decltype(nt)::value, THREADS = decltype(threads)::value;
             r.step_row = THREADS / runs;
             r.step_run = THREADS % runs;
             const long long blocks = ((long long)a.P + 32 * NT - 1) / (32 * NT);
@@ -749,13 +747,15 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
             r.blocks = (unsigned)blocks;
             r.units = (decltype(brief)::value ? (t.Mt + 1) / 2 : t.Mt) + splits - 1;
             r.units /= splits;
-            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE>>(blocks * splits, THREADS, rows_lds(t, 32 * NT), s, a, r);
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, rows_lds(t, 32 * NT), s, a, r);
         };
         // (as many waves as there are scale words, or as the quantisation keeps busy)
         const int elements = a.P * a.K;
         if (kernel == PW16_FEW) return t.Kq > 8 || elements > 16384 ? few(Int<16>{}) : t.Kq > 4 || elements > 8192 ? few(Int<8>{}) : few(Int<4>{});
-        if (kernel == PW16_ROWS_128) return rows(Int<4>{}, std::true_type{});
-        return t.Kq == 1 ? rows(Int<1>{}, std::true_type{}) : rows(Int<1>{}, std::false_type{});
+        if (kernel == PW16_ROWS_128) return rows(Int<4>{}, std::true_type{}, Int<256>{});
+        if (t.Kq == 1) return rows(Int<1>{}, std::true_type{}, Int<256>{});
+        // (many rows: four workgroups of four waves to the compute unit hide each other's loads and quantisation)
+        return a.P >= 128ll * std::max(compute_units(), 1) ? rows(Int<1>{}, std::false_type{}, Int<256>{}) : rows(Int<1>{}, std::false_type{}, Int<512>{});
     };
     return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
 }

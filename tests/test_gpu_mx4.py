@@ -318,3 +318,10 @@ def test_outputs_beyond_the_caches(ss):
     for y in (ss.ss_pw_mx4_fwd(desc, x, packed), ss.ss_pw_mx4_q_fwd(desc, codes, scales, packed)):
         ref.close(y[around], want, bound, F16, "rows")
         del y
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(33000, 544, 70), (32801, 300, 96), (70000, 264, 33)])
+def test_many_rows_of_longer_reductions(ss, rows, cin, cout):
+    desc, x, packed, bias, residual, xq, wq = _layer(ss, rows, cin, cout, BF16, rows)
+    want, bound = ref.pointwise(xq, wq, bias.double().cpu().numpy(), residual.double().cpu().numpy(), ss.SS_ACT_GELU)
+    ref.close(ss.ss_pw_mx4_fwd(desc, x, packed, bias, residual, ss.SS_ACT_GELU), want, bound, BF16, "rows")
