@@ -520,7 +520,8 @@ int ss_norm_fwd(const ss_norm_desc *desc, const ss_norm_io *io /*[host]*/, void 
  * Gradient of ss_norm_fwd for a gradient dy of y and one, dx_out, of x_out (NULL: none; needed with SS_NORM_NONE).  Takes the forward pass's x_out
  * (x where there was no h) and h; statistics are computed again.  dx is the gradient of x; dh, and dgate in the type and shape of gate, are
  * needed where there is an h and a gate, the fp32 vectors only where they are not NULL.  Sums over rows are made in a fixed order: the
- * same call gives the same bits.  dx may be dy or dx_out, dh may be h.  rows = 0 gives zero vectors.
+ * same call gives the same bits.  dx may be dy or dx_out, dh may be h.  rows = 0 gives zero vectors, and
+ * a zero dgate to a gate of any number of groups.
  *   workspace  ss_norm_bwd_workspace_bytes bytes (gate_cols 0: no gate), 16-byte aligned, not initialised.  Asynchronous on `stream`.
  */
 typedef struct {

@@ -1087,7 +1087,7 @@ def ss_norm_bwd(desc: ss_norm_desc, dy, x_out, w=None, b=None, h=None, scale=Non
             io.dgate = _dev_ptr(dgate, "dgate")
         need = ss_norm_bwd_workspace_bytes(desc, rows, io.groups, io.gate_cols)
         if rows == 0:                                        # sums over no rows
-            return NormGrads(dx, dh, dgate, *(None if v is None else v.zero_() for v in (dw, db, dscale, dpost_w, dpost_b)))
+            return NormGrads(dx, dh, *(None if v is None else v.zero_() for v in (dgate, dw, db, dscale, dpost_w, dpost_b)))
         if need > 0 and workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
         st = _lib.ss_norm_bwd(ctypes.byref(desc), ctypes.byref(io), _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))

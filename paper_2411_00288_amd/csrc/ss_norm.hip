@@ -53,8 +53,8 @@ int check_norm(const ss_norm_desc *d, int64_t rows, int64_t groups, int32_t gate
     if (!(d->eps >= 0.f) || !(d->post_eps >= 0.f) || std::isinf(d->eps) || std::isinf(d->post_eps)) return SS_ERR_INVALID_ARG;
     if (rows < 0 || gate_cols < 0) return SS_ERR_INVALID_ARG;
     if (gate_cols != 0 && gate_cols != 1 && gate_cols != d->cols) return SS_ERR_INVALID_ARG;
-    if (gate_cols != 0 && rows > 0 && (groups <= 0 || rows % groups != 0)) return SS_ERR_INVALID_ARG;
-    return d->cols <= kMaxCols && rows <= INT32_MAX ? SS_OK : SS_ERR_UNSUPPORTED;
+    if (gate_cols != 0 && (rows > 0 ? groups <= 0 || rows % groups != 0 : groups < 0)) return SS_ERR_INVALID_ARG;
+    return d->cols <= kMaxCols && rows <= INT32_MAX && (gate_cols == 0 || groups <= INT32_MAX) ? SS_OK : SS_ERR_UNSUPPORTED;
 }
 
 // A tensor of rows: there (or allowed to be absent), on an element's boundary, with a pitch that holds a row.
@@ -139,7 +139,14 @@ extern "C" int ss_norm_bwd(const ss_norm_desc *d, const ss_norm_grad_io *io, voi
         d->dtype == SS_F16 ? launch_norm_sum<SS_F16>(sum, s) : d->dtype == SS_BF16 ? launch_norm_sum<SS_BF16>(sum, s) : launch_norm_sum<SS_F32>(sum, s);
         return launched();
     };
-    if (io->rows == 0) return sum.wanted ? finish(0) : SS_OK;   // sums over no rows
+    if (io->rows == 0) {                                        // sums over no rows
+        const long long gates = io->gate ? io->groups * (long long)io->gate_cols : 0;
+        if (io->dgate && !aligned(io->dgate, d->dtype == SS_F32 ? 4 : 2)) return SS_ERR_INVALID_ARG;
+        if (gates > INT32_MAX) return SS_ERR_UNSUPPORTED;       // (a thread to the element)
+        sum.dgate = static_cast<char *>(io->dgate);
+        sum.gate_cols = io->gate_cols;
+        return sum.wanted || gates ? finish(gates) : SS_OK;
+    }
     if (!rows_ok(d, io->dy, io->lddy, norm) || !rows_ok(d, io->x_out, io->ldx_out, norm) || !rows_ok(d, io->dx_out, io->lddx_out, false) ||
         !rows_ok(d, io->h, io->ldh, false) || !rows_ok(d, io->dx, io->lddx, true) || !rows_ok(d, io->dh, io->lddh, io->h != nullptr) ||
         (io->gate && (!aligned(io->gate, d->dtype == SS_F32 ? 4 : 2) || !aligned(io->dgate, d->dtype == SS_F32 ? 4 : 2))))
