@@ -51,8 +51,10 @@ class Stage4bit:
         return ss.ss_pw_mx4_fwd(self.contract, wide, block["contract"], block["contract_bias"])
 
     def forward(self, x: torch.Tensor, gates=None):
-        """x [N, H, W, channels] -> (the stream behind the last block, its LayerNorm).  gates: one [N, 1] of x's type for each block, or None."""
-        gates = gates or [None] * len(self.blocks)
+        """x [N, H, W, channels] -> (the stream behind the last block, its LayerNorm).  gates: one [N, 1] of x's type, or None, for each block; or None."""
+        gates = [None] * len(self.blocks) if gates is None else list(gates)
+        if len(gates) != len(self.blocks):
+            raise ValueError(f"{len(gates)} gates for {len(self.blocks)} blocks")
         for block, gate in zip(self.blocks[:-1], gates):
             x = ss.ss_norm_fwd(self.sum, x, None, None, self.branch(block, x), block["scale"], gate)
         last = self.blocks[-1]
