@@ -3,7 +3,7 @@
 A block is: depthwise 7x7 (dense, 16-bit) -> LayerNorm, written as MXFP4 -> pointwise expansion on those codes with GELU -> pointwise contraction
 (its 16-bit input quantised on the way) -> layer scale, a stochastic-depth gate per image, and the residual sum.  Both pointwise matrices carry a 2:4
 mask and are kept in MXFP4.  The stage ends in the LayerNorm in front of the downsample, fused with the last block's tail; ``tail_gradient`` is that
-call's gradient, which is where learning the layer scale and the norms of a network with frozen 4-bit layers begins.  Weights are random
+call's gradient for a forward pass, which is where learning the layer scale and the norms of a network with frozen 4-bit layers begins.  Weights are random
 (``workloads.make_weights``), as everywhere in this package.
 """
 from __future__ import annotations
@@ -15,6 +15,15 @@ import paper_2411_00288_amd as ss
 from . import workloads as wl
 
 EPS = 1e-6
+
+
+class StageOutput(tuple):
+    """(the stream behind the last block, its LayerNorm) of one forward pass; `tail` is what the gradient of its last call takes."""
+
+    def __new__(cls, x: torch.Tensor, y: torch.Tensor, h: torch.Tensor, gate: torch.Tensor | None):
+        self = super().__new__(cls, (x, y))
+        self.tail = (x, h, gate)
+        return self
 
 
 class Stage4bit:
@@ -41,7 +50,7 @@ class Stage4bit:
                 block[name] = ss.ss_mx4_pack(desc, block[name + "_W"], block[name + "_M"])
             self.blocks.append(block)
         self.w, self.b = vector(1, 0.1), vector(0, 0.1)
-        self._saved = None
+        self._last, self._passes = None, 0      # the last forward pass, and how many there were since the last gradient
 
     def branch(self, block: dict, x: torch.Tensor) -> torch.Tensor:
         """A block without its tail: x NHWC -> h of the same shape."""
@@ -50,7 +59,7 @@ class Stage4bit:
         wide = ss.ss_pw_mx4_q_fwd(self.expand, codes, scales, block["expand"], block["expand_bias"], None, ss.SS_ACT_GELU)
         return ss.ss_pw_mx4_fwd(self.contract, wide, block["contract"], block["contract_bias"])
 
-    def forward(self, x: torch.Tensor, gates=None):
+    def forward(self, x: torch.Tensor, gates=None) -> StageOutput:
         """x [N, H, W, channels] -> (the stream behind the last block, its LayerNorm).  gates: one [N, 1] of x's type, or None, for each block; or None."""
         gates = [None] * len(self.blocks) if gates is None else list(gates)
         if len(gates) != len(self.blocks):
@@ -60,11 +69,20 @@ class Stage4bit:
         last = self.blocks[-1]
         h = self.branch(last, x)
         x, y = ss.ss_norm_fwd(self.norm, x, self.w, self.b, h, last["scale"], gates[-1])
-        self._saved = (x, h, gates[-1])
-        return x, y
+        self._last = StageOutput(x, y, h, gates[-1])
+        self._passes += 1
+        return self._last
 
-    def tail_gradient(self, dy: torch.Tensor, dx_out: torch.Tensor | None = None) -> "ss.NormGrads":
-        """Gradients at the last forward's closing norm: of the stream before the last block, of its branch, its gate, the norm's vectors and the layer
-        scale, for a gradient dy of the norm's output and dx_out of the stream."""
-        x, h, gate = self._saved
+    def tail_gradient(self, dy: torch.Tensor, dx_out: torch.Tensor | None = None, of: StageOutput | None = None) -> "ss.NormGrads":
+        """Gradients at a forward pass's closing norm: of the stream before the last block, of its branch, its gate, the norm's vectors and the layer
+        scale, for a gradient dy of the norm's output and dx_out of the stream.  of: what that pass returned (its tensors as they were); it may be left out
+        where there was one pass only since the last gradient."""
+        if of is None:
+            if self._passes > 1:
+                raise ValueError(f"{self._passes} forward passes since the last gradient: which one's is wanted (of=)?")
+            if self._last is None:
+                raise ValueError("no forward pass to take the gradient of")
+            of = self._last
+        self._passes = 0
+        x, h, gate = of.tail
         return ss.ss_norm_bwd(self.norm, dy, x, self.w, self.b, h, self.blocks[-1]["scale"], gate, dx_out=dx_out)
