@@ -494,7 +494,8 @@ typedef struct {
     float eps, post_eps;
 } ss_norm_desc;
 
-/* Operands of ss_norm_fwd: device pointers, pitches in elements, NULL where there is none.  x_out may be x or h, y may be h; rows begin at any element. */
+/* Operands of ss_norm_fwd: device pointers, pitches in elements, NULL where there is none (an operand that the call has no use for is refused).  x_out may be x or h, y
+ * may be h; rows begin at any element. */
 typedef struct {
     int64_t rows;
     int64_t groups;     /* rows of `gate`; rows r*rows/groups .. (r+1)*rows/groups - 1 share its row r.  Divides rows. */

@@ -77,7 +77,8 @@ extern "C" int ss_norm_fwd(const ss_norm_desc *d, const ss_norm_io *io, void *st
     const bool mx4 = io->codes != nullptr || io->scales != nullptr, norm = d->norm != SS_NORM_NONE;
     if (io->gate && io->gate_cols == 0) return SS_ERR_INVALID_ARG;
     if (!io->h && (io->x_out || io->gate || io->scale || d->post != SS_NORM_NONE)) return SS_ERR_INVALID_ARG;
-    if (!norm && (io->y || mx4 || !io->h)) return SS_ERR_INVALID_ARG;
+    if (!norm && (io->y || mx4 || !io->h || io->w || io->b)) return SS_ERR_INVALID_ARG;
+    if (d->post == SS_NORM_NONE && (io->post_w || io->post_b)) return SS_ERR_INVALID_ARG;
     if (io->rows == 0) return SS_OK;
     if (!rows_ok(d, io->x, io->ldx, true) || !rows_ok(d, io->h, io->ldh, false) || !rows_ok(d, io->x_out, io->ldx_out, io->h != nullptr) ||
         !rows_ok(d, io->y, io->ldy, norm && !mx4) || (mx4 && (io->y || !io->codes || !io->scales || !aligned(io->codes, 16) || !aligned(io->scales, 4))) ||
@@ -118,7 +119,7 @@ extern "C" int ss_norm_bwd(const ss_norm_desc *d, const ss_norm_grad_io *io, voi
     const bool norm = d->norm != SS_NORM_NONE, post = d->post != SS_NORM_NONE;
     if (io->gate && io->gate_cols == 0) return SS_ERR_INVALID_ARG;
     if (!io->h && (io->dh || io->gate || io->scale || post)) return SS_ERR_INVALID_ARG;
-    if ((!norm && (io->dy || io->dw || io->db || !io->dx_out)) || (io->dscale && !io->h) || (io->dgate && !io->gate) || (io->gate && !io->dgate) ||
+    if ((!norm && (io->dy || io->w || io->dw || io->db || !io->dx_out)) || (!post && (io->post_w || io->post_b)) || (io->dscale && !io->h) || (io->dgate && !io->gate) || (io->gate && !io->dgate) ||
         ((io->dpost_w || io->dpost_b) && !(post && io->h)))
         return SS_ERR_INVALID_ARG;
     for (const float *v : {io->w, io->scale, io->post_w, io->post_b, (const float *)io->dw, (const float *)io->db, (const float *)io->dscale, (const float *)io->dpost_w,

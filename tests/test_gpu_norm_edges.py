@@ -53,3 +53,63 @@ def test_no_rows_at_the_c_interface(ss, dtype, gate_cols, vectors):
     assert call() == ss.SS_ERR_INVALID_ARG
     io.groups = 2 ** 31
     assert call() == ss.SS_ERR_UNSUPPORTED
+
+
+def _refused(ss, call):
+    with pytest.raises(ss.SSError) as e:
+        call()
+    assert e.value.status == ss.SS_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("rows", [1, 8])
+@pytest.mark.parametrize("stream", [False, True])
+def test_vectors_of_a_norm_that_is_not_there(ss, rows, stream):
+    """w and b with SS_NORM_NONE, post_w and post_b without a post norm: refused in both directions, not dropped."""
+    x = torch.randn((rows, 64), device="cuda")
+    v = torch.full((64,), 3.0, device="cuda")
+    none, bare = ss.make_norm_desc(64, ss.SS_F32, ss.SS_NORM_NONE), ss.make_norm_desc(64, ss.SS_F32)
+    both = ss.make_norm_desc(64, ss.SS_F32, ss.SS_NORM_NONE, 1e-6, ss.SS_NORM_RMS)
+    k = {"stream": torch.cuda.current_stream()} if stream else {}
+    for desc in (none, both):
+        _refused(ss, lambda: ss.ss_norm_fwd(desc, x, v, None, x, **k))
+        _refused(ss, lambda: ss.ss_norm_fwd(desc, x, None, v, x, **k))
+        _refused(ss, lambda: ss.ss_norm_bwd(desc, None, None, v, None, x, dx_out=x, **k))
+        _refused(ss, lambda: ss.ss_norm_bwd(desc, None, None, None, v, x, dx_out=x, **k))
+    for h in (x, None):
+        for name in ("post_w", "post_b"):
+            _refused(ss, lambda: ss.ss_norm_fwd(bare, x, v, None, h, **{name: v}, **k))
+            _refused(ss, lambda: ss.ss_norm_mx4_fwd(bare, x, v, None, h, **{name: v}, **k))
+            _refused(ss, lambda: ss.ss_norm_bwd(bare, x, x, v, None, h, **{name: v}, **k))
+    assert torch.equal(ss.ss_norm_fwd(none, x, None, None, x, **k), x + x)
+    assert len(ss.ss_norm_fwd(bare, x, v, v, x, v, **k)) == 2
+
+
+def test_vectors_of_a_norm_that_is_not_there_at_the_c_interface(ss):
+    from paper_2411_00288_amd import binding
+    x, v = torch.randn((2, 64), device="cuda"), torch.ones(64, device="cuda")
+    out = [torch.empty((2, 64), device="cuda") for _ in range(2)]
+
+    def forward(norm, post, **vectors):
+        desc = ss.make_norm_desc(64, ss.SS_F32, norm, 1e-6, post)
+        io = binding.ss_norm_io(rows=2, x=x.data_ptr(), ldx=64, h=x.data_ptr(), ldh=64, x_out=out[0].data_ptr(), ldx_out=64)
+        if norm:
+            io.y, io.ldy = out[1].data_ptr(), 64
+        for name in vectors:
+            setattr(io, name, v.data_ptr())
+        return binding._lib.ss_norm_fwd(ctypes.byref(desc), ctypes.byref(io), binding._stream_ptr())
+
+    def backward(norm, post, **vectors):
+        desc = ss.make_norm_desc(64, ss.SS_F32, norm, 1e-6, post)
+        io = binding.ss_norm_grad_io(rows=2, dx_out=x.data_ptr(), lddx_out=64, h=x.data_ptr(), ldh=64, dx=out[0].data_ptr(), lddx=64, dh=out[1].data_ptr(), lddh=64)
+        if norm:
+            io.dy, io.lddy, io.x_out, io.ldx_out = x.data_ptr(), 64, x.data_ptr(), 64
+        for name in vectors:
+            setattr(io, name, v.data_ptr())
+        ws = torch.empty(ss.ss_norm_bwd_workspace_bytes(desc, 2), dtype=torch.uint8, device="cuda")
+        return binding._lib.ss_norm_bwd(ctypes.byref(desc), ctypes.byref(io), ws.data_ptr(), ws.numel(), binding._stream_ptr())
+
+    for call in (forward, backward):
+        assert call(0, 0) == call(0, 1, post_w=v) == call(1, 0, w=v) == call(2, 2, w=v, post_w=v) == ss.SS_OK
+        assert call(0, 0, w=v) == call(0, 1, w=v) == call(1, 0, post_w=v) == call(0, 0, post_b=v) == ss.SS_ERR_INVALID_ARG
+    assert forward(0, 2, b=v) == ss.SS_ERR_INVALID_ARG and forward(1, 0, b=v) == ss.SS_OK
+    torch.cuda.synchronize()
