@@ -972,7 +972,11 @@ def make_norm_desc(cols, dtype=SS_BF16, norm=SS_NORM_LAYER, eps=1e-6, post=SS_NO
     return ss_norm_desc(int(cols), int(dtype), int(norm), int(post), float(eps), float(post_eps))
 
 
-def _norm_io(what, io, desc, lead, rows, gate, vectors, tensors):
+# An empty tensor has no address, by which the library tells an operand from none; it gets this one, which no call without rows reads or writes at.
+_NOWHERE = ctypes.c_void_p(4096)
+
+
+def _norm_io(what, io, desc, rows, gate, vectors, tensors):
     """Fills a struct of ss.h: the gate, the channel vectors and the tensors of rows, by their names."""
     dtype = _ROW_DTYPES.get(desc.dtype)
     io.rows = rows
@@ -981,13 +985,13 @@ def _norm_io(what, io, desc, lead, rows, gate, vectors, tensors):
             raise SSError(SS_ERR_INVALID_ARG, f"{what}: gate must be [..., 1] or [..., {desc.cols}] {dtype}")
         io.gate_cols = gate.shape[-1]
         io.groups = gate.numel() // io.gate_cols
-        io.gate = _dev_ptr(gate, f"{what}: gate")
+        io.gate = _dev_ptr(gate, f"{what}: gate") if gate.numel() else _NOWHERE
     for name, t in vectors.items():
         setattr(io, name, _channel_vector(what, name, t, desc.cols))
     for name, t in tensors.items():
         if t is not None:
             p, _, ld = _row_tensor(what, name, t, desc.cols, dtype, rows)
-            setattr(io, name, p)
+            setattr(io, name, p if rows else _NOWHERE)
             setattr(io, f"ld{name}", ld)
 
 
@@ -1005,12 +1009,11 @@ def _norm_fwd(what, desc, x, w, b, h, scale, gate, post_w, post_b, x_out, y, cod
             scales = torch.empty((*x.shape[:-1], ns), dtype=torch.uint8, device=x.device) if scales is None else scales
         elif y is None and desc.norm != SS_NORM_NONE:
             y = torch.empty(x.shape, dtype=dtype, device=x.device)
-    _norm_io(what, io, desc, x.shape[:-1], rows, gate, {"w": w, "b": b, "scale": scale, "post_w": post_w, "post_b": post_b},
+    _norm_io(what, io, desc, rows, gate, {"w": w, "b": b, "scale": scale, "post_w": post_w, "post_b": post_b},
              {"x": x, "h": h, "x_out": x_out, "y": y})
     if quantised:
-        io.codes, io.scales = _byte_tensor(what, "codes", codes, rows, nc), _byte_tensor(what, "scales", scales, rows, ns)
-    # (an empty tensor has no address, by which the library tells an operand from none)
-    st = _lib.ss_norm_fwd(ctypes.byref(desc), ctypes.byref(io), _stream_ptr(stream)) if rows else SS_OK
+        io.codes, io.scales = (p if rows else _NOWHERE for p in (_byte_tensor(what, "codes", codes, rows, nc), _byte_tensor(what, "scales", scales, rows, ns)))
+    st = _lib.ss_norm_fwd(ctypes.byref(desc), ctypes.byref(io), _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, what)
     out = (codes, scales) if quantised else () if y is None else (y,)
@@ -1079,15 +1082,13 @@ def ss_norm_bwd(desc: ss_norm_desc, dy, x_out, w=None, b=None, h=None, scale=Non
         dgate = None if gate is None else torch.empty(gate.shape, dtype=gate.dtype, device=like.device)
         dw, db, dscale, dpost_w, dpost_b = (None if v is None else torch.empty(v.shape, dtype=torch.float32, device=like.device)
                                             for v in (w, b, scale, post_w, post_b))
-        _norm_io(what, io, desc, like.shape[:-1], rows, gate,
+        _norm_io(what, io, desc, rows, gate,
                  {"w": w, "scale": scale, "post_w": post_w, "post_b": post_b, "dw": dw, "db": db, "dscale": dscale, "dpost_w": dpost_w, "dpost_b": dpost_b},
                  {"dy": dy, "x_out": x_out, "dx_out": dx_out, "h": h, "dx": dx, "dh": dh})
         _channel_vector(what, "b", b, desc.cols)
         if dgate is not None:
-            io.dgate = _dev_ptr(dgate, "dgate")
+            io.dgate = _dev_ptr(dgate, "dgate") if dgate.numel() else _NOWHERE
         need = ss_norm_bwd_workspace_bytes(desc, rows, io.groups, io.gate_cols)
-        if rows == 0:                                        # sums over no rows
-            return NormGrads(dx, dh, *(None if v is None else v.zero_() for v in (dgate, dw, db, dscale, dpost_w, dpost_b)))
         if need > 0 and workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
         st = _lib.ss_norm_bwd(ctypes.byref(desc), ctypes.byref(io), _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))

@@ -113,3 +113,52 @@ def test_vectors_of_a_norm_that_is_not_there_at_the_c_interface(ss):
         assert call(0, 0, w=v) == call(0, 1, w=v) == call(1, 0, post_w=v) == call(0, 0, post_b=v) == ss.SS_ERR_INVALID_ARG
     assert forward(0, 2, b=v) == ss.SS_ERR_INVALID_ARG and forward(1, 0, b=v) == ss.SS_OK
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_calls_without_rows_are_checked_like_others(ss, dtype):
+    """The same refusals with x [0, 64] as with rows, and the same empty results."""
+    code = getattr(ss, DTYPES[dtype])
+    x = torch.empty((0, 64), dtype=dtype, device="cuda")
+    v = torch.ones(64, device="cuda")
+    gate = torch.empty((0, 1), dtype=dtype, device="cuda")
+    none, bare = ss.make_norm_desc(64, code, ss.SS_NORM_NONE), ss.make_norm_desc(64, code)
+    both = ss.make_norm_desc(64, code, ss.SS_NORM_LAYER, 1e-6, ss.SS_NORM_RMS)
+    _refused(ss, lambda: ss.ss_norm_fwd(none, x))
+    _refused(ss, lambda: ss.ss_norm_fwd(none, x, v, None, x))
+    _refused(ss, lambda: ss.ss_norm_mx4_fwd(none, x, None, None, x))
+    _refused(ss, lambda: ss.ss_norm_fwd(ss.make_norm_desc(64, code, 7), x, v))
+    _refused(ss, lambda: ss.ss_norm_fwd(ss.make_norm_desc(64, code, eps=-1.0), x, v))
+    _refused(ss, lambda: ss.ss_norm_fwd(both, x, v))
+    _refused(ss, lambda: ss.ss_norm_fwd(bare, x, v, None, None, v))
+    _refused(ss, lambda: ss.ss_norm_fwd(bare, x, v, None, None, None, gate))
+    _refused(ss, lambda: ss.ss_norm_bwd(bare, x, x, v, None, None, v))
+    _refused(ss, lambda: ss.ss_norm_bwd(none, x, x, None, None, x, dx_out=x))
+    _refused(ss, lambda: ss.ss_norm_bwd(none, None, None, None, None, x))
+    assert ss.ss_norm_fwd(bare, x, v).shape == ss.ss_norm_fwd(none, x, None, None, x).shape == (0, 64)
+    assert [tuple(t.shape) for t in ss.ss_norm_mx4_fwd(both, x, v, v, x, v, gate, v)] == [(0, 64), (0, 32), (0, 4)]
+    g = ss.ss_norm_bwd(both, x, x, v, v, x, v, gate, v, v, dx_out=x)
+    assert g.dx.shape == g.dh.shape == (0, 64) and g.dgate.shape == (0, 1)
+    assert all((t == 0).all() and t.shape == (64,) for t in (g.dw, g.db, g.dscale, g.dpost_w, g.dpost_b))
+    image = torch.empty((0, 7, 7, 64), dtype=dtype, device="cuda")
+    assert ss.ss_norm_fwd(none, image, None, None, image, v, torch.ones((1, 64), dtype=dtype, device="cuda")).shape == image.shape
+
+
+def test_no_rows_on_a_stream_and_in_a_graph(ss):
+    x = torch.empty((0, 64), device="cuda")
+    v, gate = torch.ones(64, device="cuda"), torch.ones((5, 64), device="cuda")
+    desc = ss.make_norm_desc(64, ss.SS_F32)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = ss.ss_norm_bwd(desc, x, x, v, v, x, v, gate, stream=stream)
+    stream.synchronize()
+    assert all((t == 0).all() for t in (g.dw, g.db, g.dscale, g.dgate))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g = ss.ss_norm_bwd(desc, x, x, v, v, x, v, gate)
+    for _ in range(3):
+        for t in (g.dw, g.db, g.dscale, g.dgate):
+            t.fill_(1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all((t == 0).all() for t in (g.dw, g.db, g.dscale, g.dgate))
