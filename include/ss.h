@@ -69,6 +69,7 @@ enum { SS_F16 = 0, SS_BF16 = 1, SS_I8 = 2, SS_F8 = 3 /* OCP FP8 E4M3 (no infinit
        SS_F32 = 4 /* activations of the norm and quantisation calls only */ };
 enum { SS_K_CRS = 0, SS_K_RSC = 1 };
 enum { SS_ACT_NONE = 0, SS_ACT_RELU = 1, SS_ACT_GELU = 2 };
+enum { SS_WEIGHTS_DENSE = 0, SS_WEIGHTS_SPARSE = 1, SS_WEIGHTS_MX4 = 2 }; /* which packing call wrote a weight buffer */
 
 /* Describes one weight matrix W in R^{cout x (cin*kh*kw)} (Eq. 5).  Plain data, passed by pointer [host]. */
 typedef struct {
@@ -168,17 +169,19 @@ int ss_dense_pack(const ss_weight_desc *desc, const void *W, const uint8_t *M, v
                   void *stream);
 
 /*
- * Set-up-time check that a weight buffer belongs to a descriptor.  The convolution calls are asynchronous and
+ * Set-up-time check that a weight buffer belongs to a descriptor.  The convolution and pointwise calls are asynchronous and
  * trust their weight operand: they read it with the sizes the descriptor implies and never look at its header.
  * This call reads the buffer's 256-byte header back (one stream synchronisation, like ss_mask_compress) and returns
- *   SS_ERR_INVALID_ARG  when the buffer was not written by ss_mask_compress / ss_mask_update_compress (sparse != 0)
- *                       or ss_dense_pack (sparse == 0), or was written for another cout, cin, kh, kw, dtype or
- *                       korder than desc states (e.g. a dense operand offered to ss_conv2d_fwd);
+ *   SS_ERR_INVALID_ARG  when the buffer was not written by ss_dense_pack (kind SS_WEIGHTS_DENSE), by ss_mx4_pack
+ *                       (SS_WEIGHTS_MX4) or by ss_mask_compress / ss_mask_update_compress (any other), or was written
+ *                       for another cout, cin, kh, kw, dtype or korder than desc states (e.g. a dense operand offered
+ *                       to ss_conv2d_fwd);
+ *   SS_ERR_UNSUPPORTED  with SS_WEIGHTS_MX4, for a descriptor that ss_mx4_pack does not take;
  *   SS_ERR_BAD_MASK     when it was written by a compression call that rejected its mask (Eq. 2 violated);
  *   SS_OK               otherwise.
  * Call it once per weight buffer, after packing and before the first convolution.
  */
-int ss_weights_check(const ss_weight_desc *desc, const void *weights, int32_t sparse, void *stream);
+int ss_weights_check(const ss_weight_desc *desc, const void *weights, int32_t kind, void *stream);
 
 /*
  * Scratch the convolution needs for the given problem on the current device: 0 for most problems.  Where the output

@@ -22,7 +22,8 @@ _BINDING_NAMES = {
     "ss_debug_force_split", "ss_debug_issue_peak", "ss_debug_lds_bandwidth", "DEBUG_EXPORTS", "ss_weight_desc",
     "SSError", "torch_dtype", "EXPORTS", "LIB_PATH", "SS_OK", "SS_ERR_INVALID_ARG", "SS_ERR_BAD_MASK",
     "SS_ERR_UNSUPPORTED", "SS_ERR_WORKSPACE", "SS_ERR_HIP", "SS_F16", "SS_BF16", "SS_K_CRS", "SS_K_RSC",
-    "SS_ACT_NONE", "SS_ACT_RELU", "SS_ACT_GELU", "SS_F32", "SS_NORM_NONE", "SS_NORM_LAYER", "SS_NORM_RMS",
+    "SS_ACT_NONE", "SS_ACT_RELU", "SS_ACT_GELU", "SS_WEIGHTS_DENSE", "SS_WEIGHTS_SPARSE", "SS_WEIGHTS_MX4",
+    "SS_F32", "SS_NORM_NONE", "SS_NORM_LAYER", "SS_NORM_RMS",
     "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_packed_bytes", "ss_mx4_pack", "ss_mx4_unpack", "ss_pw_mx4_workspace_bytes",
     "ss_pw_mx4_fwd", "ss_pw_mx4_q_fwd", "make_norm_desc", "ss_norm_fwd", "ss_norm_mx4_fwd", "ss_norm_bwd",
     "ss_norm_bwd_workspace_bytes", "ss_norm_desc", "NormGrads",

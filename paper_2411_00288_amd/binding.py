@@ -25,6 +25,7 @@ SS_ERR_INVALID_ARG, SS_ERR_BAD_MASK, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ER
 SS_F16, SS_BF16, SS_I8, SS_F8, SS_F32 = 0, 1, 2, 3, 4
 SS_K_CRS, SS_K_RSC = 0, 1
 SS_ACT_NONE, SS_ACT_RELU, SS_ACT_GELU = 0, 1, 2
+SS_WEIGHTS_DENSE, SS_WEIGHTS_SPARSE, SS_WEIGHTS_MX4 = 0, 1, 2
 SS_NORM_NONE, SS_NORM_LAYER, SS_NORM_RMS = 0, 1, 2
 
 EXPORTS = ["ss_status_string", "ss_packed_bytes", "ss_dense_bytes", "ss_mask_compress", "ss_mask_decompress",
@@ -275,13 +276,15 @@ def ss_dense_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None,
     return dense
 
 
-def ss_weights_check(desc: ss_weight_desc, weights: torch.Tensor, sparse: bool = True, stream=None) -> None:
+def ss_weights_check(desc: ss_weight_desc, weights: torch.Tensor, sparse: bool | int = True, stream=None) -> None:
     """Raises unless `weights` was written for `desc` by the matching packing call (and, for the sparse form, with a
-    valid mask).  One stream synchronisation; call once per buffer at set-up."""
-    need = ss_packed_bytes(desc) if sparse else ss_dense_bytes(desc)
+    valid mask); sparse: True, False, or SS_WEIGHTS_MX4 for weights of ss_mx4_pack.  One stream synchronisation; call
+    once per buffer at set-up."""
+    kind = SS_WEIGHTS_MX4 if sparse == SS_WEIGHTS_MX4 else SS_WEIGHTS_SPARSE if sparse else SS_WEIGHTS_DENSE
+    need = (ss_dense_bytes, ss_packed_bytes, ss_mx4_packed_bytes)[kind](desc)
     if weights is None or weights.numel() * weights.element_size() < need:
         raise SSError(SS_ERR_INVALID_ARG, "ss_weights_check: buffer smaller than the descriptor's size query")
-    st = _lib.ss_weights_check(ctypes.byref(desc), _dev_ptr(weights, "weights"), 1 if sparse else 0, _stream_ptr(stream))
+    st = _lib.ss_weights_check(ctypes.byref(desc), _dev_ptr(weights, "weights"), kind, _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, "ss_weights_check")
 

@@ -11,8 +11,6 @@
 
 namespace ss {
 
-constexpr uint32_t kMagicMx4 = 0x344D5353u;      // "SSM4"
-
 inline size_t mx4_packed_size(const Mx4Dims &t) { return (size_t)kHeaderBytes + (size_t)t.Mt * t.Ks * 1024 + (size_t)t.Mt * t.Kq * 256; }
 
 // Largest magnitude pattern of 8 values (as an integer it orders finite values by size, and infinities and NaN above them).

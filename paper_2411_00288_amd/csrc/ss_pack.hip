@@ -2,6 +2,7 @@
 // Integer / bit work only: no floating-point instruction touches a weight.
 #include "ss_internal.h"
 #include "ss_pack_wait.h"
+#include "ss_pw_choice.h"
 #include <hip/hip_ext.h>
 #include <chrono>
 #include <thread>
@@ -423,17 +424,26 @@ extern "C" int ss_mask_decompress(const ss_weight_desc *desc, const void *packed
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_HIP;
 }
 
-extern "C" int ss_weights_check(const ss_weight_desc *desc, const void *weights, int32_t sparse, void *stream)
+extern "C" int ss_weights_check(const ss_weight_desc *desc, const void *weights, int32_t kind, void *stream)
 {
-    int st = check_desc(desc, sparse != 0);
+    const bool mx4 = kind == SS_WEIGHTS_MX4, sparse = !mx4 && kind != SS_WEIGHTS_DENSE;
+    int st = check_desc(desc, sparse);
     if (st != SS_OK) return st;
+    if (mx4 && (desc->kh != 1 || desc->kw != 1 || is_byte_type(desc->dtype))) return SS_ERR_UNSUPPORTED;
     if (!weights || !aligned(weights, 16)) return SS_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     uint32_t hdr[kHdrFirstBad + 1];
     if (hipMemcpyAsync(hdr, weights, sizeof(hdr), hipMemcpyDeviceToHost, s) != hipSuccess) return SS_ERR_HIP;
     if (hipStreamSynchronize(s) != hipSuccess) return SS_ERR_HIP;
-    const TileDims t = tile_dims(desc);
-    const uint32_t want[10] = {sparse ? kMagicSparse : kMagicDense, 1u, (uint32_t)desc->cout, (uint32_t)desc->cin,
+    TileDims t{};
+    if (mx4) {
+        const Mx4Dims m = mx4_dims(desc->cout, desc->cin);
+        t.Mt = m.Mt;
+        t.Ks = m.Ks;
+    } else {
+        t = tile_dims(desc);
+    }
+    const uint32_t want[10] = {mx4 ? kMagicMx4 : sparse ? kMagicSparse : kMagicDense, 1u, (uint32_t)desc->cout, (uint32_t)desc->cin,
                                (uint32_t)desc->kh, (uint32_t)desc->kw, (uint32_t)desc->dtype, (uint32_t)desc->korder,
                                (uint32_t)t.Mt, (uint32_t)t.Ks};
     for (int i = 0; i < 10; i++)
