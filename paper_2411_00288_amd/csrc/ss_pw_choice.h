@@ -88,6 +88,13 @@ inline int rows_splits(const Mx4Dims &t, long long rows, long long cus)
     return (int)std::max(1ll, std::min((units + 3) / 4, cus / blocks));
 }
 
+// Waves of the few-row kernel on 16-bit input: as many as there are scale words, or as the quantisation keeps busy.
+inline int few16_waves(const Mx4Dims &t, long long rows, int K)
+{
+    const long long elements = rows * K;
+    return t.Kq > 8 || elements > 16384 ? 16 : t.Kq > 4 || elements > 8192 ? 8 : 4;
+}
+
 // Does the kernel take such a layer at all?
 inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
 {

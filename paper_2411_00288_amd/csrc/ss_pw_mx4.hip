@@ -749,9 +749,10 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
             r.units /= splits;
             return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, rows_lds(t, 32 * NT), s, a, r);
         };
-        // (as many waves as there are scale words, or as the quantisation keeps busy)
-        const int elements = a.P * a.K;
-        if (kernel == PW16_FEW) return t.Kq > 8 || elements > 16384 ? few(Int<16>{}) : t.Kq > 4 || elements > 8192 ? few(Int<8>{}) : few(Int<4>{});
+        if (kernel == PW16_FEW) {
+            const int waves = few16_waves(t, a.P, a.K);
+            return waves == 16 ? few(Int<16>{}) : waves == 8 ? few(Int<8>{}) : few(Int<4>{});
+        }
         if (kernel == PW16_ROWS_128) return rows(Int<4>{}, std::true_type{}, Int<256>{});
         if (t.Kq == 1) return rows(Int<1>{}, std::true_type{}, Int<256>{});
         // (many rows: four workgroups of four waves to the compute unit hide each other's loads and quantisation)
