@@ -95,6 +95,14 @@ inline int few16_waves(const Mx4Dims &t, long long rows, int K)
     return t.Kq > 8 || elements > 16384 ? 16 : t.Kq > 4 || elements > 8192 ? 8 : 4;
 }
 
+// Waves of that kernel's workgroups with 32 rows.  Of many rows with longer reductions four, where LDS holds four such workgroups: they hide each other's loads and quantisation
+// (384 -> 96 on 401408 rows 109 -> 77 us).  Fewer of them leave the compute unit idle (4096 -> 4096 on 32768 rows, one workgroup, 905 us, with eight waves 544; 4096 -> 1024, two,
+// 181 and 164).
+inline int rows_waves(const Mx4Dims &t, long long rows, long long cus)
+{
+    return t.Kq == 1 || (rows >= 128 * cus && 4 * rows_lds(t, 32) <= kPwLds) ? 4 : 8;
+}
+
 // Does the kernel take such a layer at all?
 inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
 {
@@ -107,10 +115,12 @@ inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
 }
 
 // On 16-bit input.  Few rows while every workgroup's own quantisation of them is short (1024 -> 4096: 16 rows 4.6 us, and with a quantisation of its own 3.3 + 2.9; 4096 ->
-// 4096: 24 rows 9.1 and 6.3 + 3.0).  Otherwise the shorter estimate: of the kernel that quantises in LDS, whose waves walk down the channels, two workgroups to the compute unit
-// (4 us, 2.6 for each 1024 channels of the reduction and 0.11 a step and 32 channels; what follows the first overlaps, with 4.2 TB/s for what is moved), or of a quantisation at
+// 4096: 24 rows 9.1 and 6.3 + 3.0).  Otherwise the shorter estimate: of the kernel that quantises in LDS, whose waves walk down the channels (a workgroup's 4 us, 2.6 for each
+// 1024 channels of the reduction and 0.11 a step and 32 channels; what follows the first two of a compute unit overlaps, with 4.2 TB/s for what is moved; where LDS holds one
+// workgroup of them, nothing overlaps, and there are whole rounds; and the weights, which every 32 rows read again, come at 11 TB/s), or of a quantisation at
 // 4 TB/s and the tiled product (measured, the former and the latter: 2048 -> 512 on 3136 rows 13 and 14 us, 512 -> 2048 on 12544 28 and 29, 4096 -> 4096 on 2048 47 and 33, 1024 ->
-// 8192 on 12544 135 and 103).  128 rows to the workgroup, one tile of them to the wave, with short reductions and many rows (64 -> 256 on
+// 8192 on 12544 135 and 103; many rows and two workgroups of LDS, 2048 -> 2048 on 20000 rows 100 and 76, on 65536 291 and 241, 1024 -> 1024 on 65536 93 and 94; one workgroup,
+// 4096 -> 4096 on 20000 rows 378 and 226, on 32768 544 and 340).  128 rows to the workgroup, one tile of them to the wave, with short reductions and many rows (64 -> 256 on
 // 200704 rows 47 -> 31 us, on 12544 7.4 and 8.2).
 inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
 {
@@ -120,7 +130,9 @@ inline PwKernel choose16(const Mx4Dims &t, long long rows, long long cus)
     const long long blocks = (rows + 31) / 32, splits = rows_splits(t, rows, cus), units = (t.Mt + splits * 8 - 1) / (splits * 8);
     const double one = 4.0 + 0.0025 * K + 0.11 * units * t.Ks, rounds = (double)(blocks * splits) / (2.0 * cus);
     const bool wide = rows >= 128 * cus && fits16(t, rows, PW16_ROWS_128);
-    const double lds = one + std::max((rounds - 1.0) * (wide ? 0.35 : 0.7) * one, (rows * K * 2 + out) / 4.2e6);
+    double lds = one + std::max((rounds - 1.0) * (wide ? 0.35 : 0.7) * one, (rows * K * 2 + out) / 4.2e6);
+    if (2 * rows_lds(t, 32) > kPwLds) lds = std::max(lds, (double)((blocks * splits + cus - 1) / cus) * one);
+    if (!wide) lds = std::max(lds, (double)blocks * t.Mt * t.Ks * 1088 / 11e6);
     const double codes = 3.2 + rows * K * 2.53 / 4e6 + (choose_codes(t, rows, cus) >= PW_FEW_32 ? 4.0 + 0.05 * t.Ks : tiles_us(t, rows, cus));
     if (codes < lds) return PW16_CODES;
     return wide ? PW16_ROWS_128 : PW16_ROWS;

@@ -755,8 +755,7 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
         }
         if (kernel == PW16_ROWS_128) return rows(Int<4>{}, std::true_type{}, Int<256>{});
         if (t.Kq == 1) return rows(Int<1>{}, std::true_type{}, Int<256>{});
-        // (many rows: four workgroups of four waves to the compute unit hide each other's loads and quantisation)
-        return a.P >= 128ll * std::max(compute_units(), 1) ? rows(Int<1>{}, std::false_type{}, Int<256>{}) : rows(Int<1>{}, std::false_type{}, Int<512>{});
+        return rows_waves(t, a.P, std::max(compute_units(), 1)) == 4 ? rows(Int<1>{}, std::false_type{}, Int<256>{}) : rows(Int<1>{}, std::false_type{}, Int<512>{});
     };
     return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
 }
