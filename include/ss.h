@@ -207,7 +207,7 @@ int ss_conv2d_workspace_bytes(const ss_weight_desc *desc, int32_t N, int32_t H, 
  *   x         [N][H][Wd][cin]    16-bit, desc->dtype                        (read only)
  *   packed    buffer written by ss_mask_compress for the same desc          (read only)
  *   bias      [cout] fp32, or NULL for no bias                              (read only)
- *   act       SS_ACT_NONE | SS_ACT_RELU | SS_ACT_GELU (z * Phi(z), exact normal CDF; of +infinity +infinity, of -infinity a NaN)
+ *   act       SS_ACT_NONE | SS_ACT_RELU | SS_ACT_GELU (z * Phi(z), exact normal CDF; of +infinity +infinity, of -infinity 0)
  *   y         [N][Ho][Wo][cout]  16-bit, desc->dtype                        (written)
  *   workspace ws_bytes >= ss_conv2d_workspace_bytes(...) bytes, see there; may be NULL when that size is 0
  *             (SS_ERR_WORKSPACE when it is needed and missing or too small)

@@ -1,4 +1,4 @@
-"""GELU of infinities: z Phi(z) is +infinity at +infinity, and infinity times zero, a NaN, at -infinity.  In every kernel that has the activation; the other channels do not
+"""GELU of infinities: z Phi(z) has the limits +infinity at +infinity and 0 at -infinity.  In every kernel that has the activation; the other channels do not
 notice."""
 import numpy as np
 import pytest
@@ -16,7 +16,7 @@ def _bias(cout):
     b[:4] = torch.tensor([INF, -INF, float("nan"), 3.4e38])
     want = b.double()
     want = want * torch.special.ndtr(want)
-    want[0], want[1] = INF, float("nan")
+    want[0], want[1] = INF, 0.0
     return b, want
 
 
@@ -47,7 +47,7 @@ def test_pointwise_4bit(ss, force_tile, dtype, code, kernel, rows, cin, cout):
     zero = torch.zeros(cout, device="cuda")
     y = (ss.ss_pw_mx4_q_fwd(desc, codes, scales, packed, zero, residual, ss.SS_ACT_GELU) if kernel < 75
          else ss.ss_pw_mx4_fwd(desc, x, packed, zero, residual, ss.SS_ACT_GELU))
-    assert y[-1, 5] == INF and torch.isnan(y[0, 6]) and int((y == 0).sum()) == rows * cout - 2
+    assert y[-1, 5] == INF and y[0, 6] == 0 and int((y == 0).sum()) == rows * cout - 1
 
 
 @pytest.mark.parametrize("dtype,code", TYPES)
