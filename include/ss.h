@@ -485,7 +485,8 @@ int ss_pw_mx4_q_fwd(const ss_weight_desc *desc, const void *codes, const void *s
  * Norms before and after a block, with its gate, its residual scale and the residual sum, over the channels of each row:
  *     u = post(h)        x_out = x + scale * gate * u        y = norm(x_out)
  * LayerNorm: (v - mean) / sqrt(mean of squared differences + eps) * w + b.  RMS: v / sqrt(mean square + eps) * w + b.
- * Statistics and sums are fp32, y is computed from x_out before its rounding, and x_out and y are rounded once each.
+ * Statistics and sums are fp32 (a row whose sum of squares passes fp32's range, from values of about 1e19 on, counts as infinitely large), y is computed
+ * from x_out before its rounding, and x_out and y are rounded once each.
  */
 enum { SS_NORM_NONE = 0, SS_NORM_LAYER = 1, SS_NORM_RMS = 2 };
 

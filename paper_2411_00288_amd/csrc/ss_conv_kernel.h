@@ -1393,11 +1393,11 @@ void mlp_kernel(MlpParams p)
     int c_at = BN * XROW + (half * 32 + c) * CROW + 16 * g;
     asm volatile("" : "+v"(c_at));                        // (an address of its own: as an offset from another one it is too large for the instruction, and an addition per read)
     const uint16_t *const c_frag = smem + c_at;
-    // Bound by the vector ALU: 154 M GELUs on the ConvNeXt-T stage-1 block at batch 128 are 61 us of it (twelve full-rate instructions of 4
+    // Bound by the vector ALU: 154 M GELUs on the ConvNeXt-T stage-1 block at batch 128 are 66 us of it (thirteen full-rate instructions of 4
     // clocks and one of 8 per wave).  What else the vector ALU does is kept small: the activation is chosen outside the element loop, addresses
     // are scalar, biases start in accumulators, the residual is fetched behind the chunks (during the last one, behind a condition, its registers
     // travelled through copies in every chunk), and four waves per SIMD (128 registers) overlap one's matrix instructions with another's
-    // GELUs: 113 -> 96 us (graph of 20; counters in profiles/block_kernel_counters.md).
+    // GELUs: 113 -> 96 us (graph of 20; counters in profiles/block_kernel_counters.md; 97 to 99 with the minimum that keeps infinities).
     auto chunk = [&](auto act1, int mc) {
         // ---- first contraction: rows 128*mc + 32*wave + [0,32) of the intermediate, all 64 pixels
         f32x16 acc1[2];                                   // the bias starts in the accumulators
@@ -1510,11 +1510,11 @@ void mlp_kernel(MlpParams p)
 // blocks 0 1 | 2 3 | 4 5 | 6 7 of the two lane halves swapped to 0 4 | 1 5 | 2 6 | 3 7 (four V_PERMLANE32_SWAP) they are the second layer's operand.
 // So the intermediate passes neither LDS nor a barrier.  The weights of both layers lie in LDS, one workgroup per compute unit walks over its pixel
 // tiles, and a wave asks for its next tile's input while it works on this one.
-// Bound by memory with ReLU (231 MB in 46 us), by the vector ALU with GELU (of 2880 vector instructions per tile of 96 -> 384 -> 96 in bf16, 2500 are
+// Bound by memory with ReLU (231 MB in 46 us), by the vector ALU with GELU (of 3070 vector instructions per tile of 96 -> 384 -> 96 in bf16, 2690 are
 // the GELUs).  With the weights from memory for each wave the address unit took as long as the vector ALU; with an accumulator tile more, to
 // multiply ahead of the activations, three waves per SIMD had no registers left for weights on their way, and each matrix instruction waited for LDS.
 // 401408 pixels, 96 -> 384 -> 96, bf16, mlp_kernel against this one, us: ReLU sparse 69.0 -> 46.0, dense 88.9 -> 57.7; GELU dense 116.8 -> 98.6
-// (f16 114.9 -> 94.0).  TILES: 32-channel tiles of the input and of the output; WAVES: per workgroup.
+// (f16 114.9 -> 94.0; both 2 to 4 % more since infinities pass the GELU).  TILES: 32-channel tiles of the input and of the output; WAVES: per workgroup.
 template <int DT, bool SPARSE, int TILES, int WAVES, bool GELU1>
 __global__ __launch_bounds__(WAVES * 64)
 void mlp_resident_kernel(MlpParams p)
@@ -1712,7 +1712,7 @@ void mlp_resident_kernel(MlpParams p)
 // compute unit.  Here a workgroup owns 32 pixels and has a wave for each 32 channels of the intermediate: every wave computes
 // its row tile at once, the whole intermediate meets in LDS, and the waves share out the second layer's row tiles and its reduction;
 // the partial sums are added in the order of the reduction.  Weights, input and residual are one memory latency.  What is left is mostly the
-// activation: 32 x 384 GELUs of 56 clocks on four SIMDs are 1.1 us of the 3.9 us that 96 -> 384 -> 96 on 3136 pixels takes (7.6 -> 5.5 us with the launch).
+// activation: 32 x 384 GELUs of 60 clocks on four SIMDs are 1.2 us of the 3.9 us that 96 -> 384 -> 96 on 3136 pixels takes (7.6 -> 5.5 us with the launch).
 constexpr int mlp_wide_smem(int cin, int waves)
 {
     const int tiles = 32 * (cin + 8) * 2 + 32 * (32 * waves + 8) * 2, sums = waves * (int)kFuseRegion;      // (the partial sums take the place of both tiles)

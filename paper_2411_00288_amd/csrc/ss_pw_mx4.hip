@@ -421,7 +421,7 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
 // reduction of one chunk (SHORT), while the sums are finished: that is what such a layer's time goes to, a GELU foremost, so its registers go to waves instead.
 // One chunk: four waves, units of 64 channels; longer: units of 32, and eight waves, so that the rows are loaded and quantised by twice as many threads (1024 -> 256 on 12544 rows
 // 13.9 -> 12.2 us), or, of many rows, four (384 -> 96 on 401408 rows 109 -> 77 us, 512 -> 256 on 50176 23 -> 22; of few, 1024 -> 128 on 3136, 7.6 and 9.2).
-// Bound by memory: 96 -> 384 on 401408 rows 66 us (5.8 TB/s), 96 -> 96 34 us (4.5 TB/s); by the vector ALU with a GELU, the former 100 to 106.
+// Bound by memory: 96 -> 384 on 401408 rows 66 us (5.8 TB/s), 96 -> 96 34 us (4.5 TB/s); by the vector ALU with a GELU, the former 104 to 114.
 template <int DT, int NT, bool SHORT, bool WIDE, int THREADS>
 __global__ __launch_bounds__(THREADS, 4) void pw_mx4_rows_kernel(PwArgs p, PwRowsArgs r)
 {
