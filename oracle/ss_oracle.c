@@ -202,6 +202,7 @@ static int64_t kflat(int korder, int64_t c, int64_t r, int64_t t, int64_t cin, i
 static double layer_tail(double z, int act)
 {
     if (act == 1) return (z > 0.0 || z != z) ? z : 0.0;
+    if (act == 2 && z == -INFINITY) return 0.0;             /* the limit; the product would be infinity times zero */
     if (act == 2) return z * 0.5 * (1.0 + erf(z / sqrt(2.0)));
     return z;
 }
