@@ -772,12 +772,14 @@ def _pitch(t, what, name):
     rows, ld = 1, 0
     if t.dim() == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: the channels of {name} must be contiguous")
+    if t.numel() == 0:
+        return 0, t.shape[-1]                                # (whichever dimension is the empty one: there are no rows to be spaced)
     for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
         if size == 1:
             continue
         if rows == 1:
             ld = stride
-        elif size and stride != ld * rows:
+        elif stride != ld * rows:
             raise SSError(SS_ERR_INVALID_ARG, f"{what}: the rows of {name} must be evenly spaced")
         rows *= size
     return rows, ld if rows > 1 else t.shape[-1]
