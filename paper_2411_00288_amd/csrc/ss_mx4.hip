@@ -126,13 +126,17 @@ __global__ __launch_bounds__(256) void mx4_unpack_kernel(const uint8_t *__restri
 
 int mx4_quantize(const void *x, int64_t rows, int cols, int64_t ldx, int dtype, uint8_t *codes, uint8_t *scales, hipStream_t s)
 {
-    const unsigned runs = (unsigned)mx4_dims(1, cols).S * 4;
-    const long long total = rows * (long long)runs, blocks = (total + 1023) / 1024;
-    if (blocks > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
+    const Mx4Dims t = mx4_dims(1, cols);
+    const unsigned runs = (unsigned)t.S * 4;
     unsigned mul, sh;
     fast_div_setup(runs, &mul, &sh);
+    const long long piece = piece_rows(runs / 4);
     const auto go = [&](auto kern) {
-        kern<<<dim3((unsigned)blocks), dim3(256), 0, s>>>(static_cast<const char *>(x), (long long)ldx, codes, scales, total, cols, runs, mul, sh);
+        for (long long at = 0; at < rows; at += piece) {
+            const long long total = std::min(piece, (long long)rows - at) * runs;
+            kern<<<dim3((unsigned)((total + 1023) / 1024)), dim3(256), 0, s>>>(static_cast<const char *>(x) + at * ldx * (dtype == SS_F32 ? 4 : 2), (long long)ldx,
+                                                                              codes + at * t.KB * 16, scales + at * t.S, total, cols, runs, mul, sh);
+        }
     };
     const auto pick = [&](auto wide, auto last) {
         constexpr bool WIDE = decltype(wide)::value, LAST = decltype(last)::value;
@@ -181,14 +185,18 @@ extern "C" int ss_mx4_dequantize(const void *codes, const void *scales, int64_t 
     if (st != SS_OK) return st;
     if (rows == 0) return SS_OK;
     if (!y || !codes || !scales || !aligned(y, dtype == SS_F32 ? 4 : 2) || !aligned(codes, 16) || !aligned(scales, 4)) return SS_ERR_INVALID_ARG;
-    const unsigned runs = (unsigned)mx4_dims(1, cols).KB * 4;
-    const long long total = rows * (long long)runs, blocks = (total + 1023) / 1024;
-    if (blocks > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
+    const Mx4Dims t = mx4_dims(1, cols);
+    const unsigned runs = (unsigned)t.KB * 4;
     unsigned mul, sh;
     fast_div_setup(runs, &mul, &sh);
+    const long long piece = piece_rows(runs / 4);
     const auto go = [&](auto kern) {
-        kern<<<dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales),
-                                                                                         static_cast<char *>(y), (long long)ldy, total, cols, runs, mul, sh);
+        for (long long at = 0; at < rows; at += piece) {
+            const long long total = std::min(piece, (long long)rows - at) * runs;
+            kern<<<dim3((unsigned)((total + 1023) / 1024)), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(
+                static_cast<const uint8_t *>(codes) + at * t.KB * 16, static_cast<const uint8_t *>(scales) + at * t.S,
+                static_cast<char *>(y) + at * ldy * (dtype == SS_F32 ? 4 : 2), (long long)ldy, total, cols, runs, mul, sh);
+        }
     };
     dtype == SS_F16 ? go(mx4_dequantize_kernel<SS_F16>) : dtype == SS_BF16 ? go(mx4_dequantize_kernel<SS_BF16>) : go(mx4_dequantize_kernel<SS_F32>);
     return launched();

@@ -25,6 +25,9 @@ inline Mx4Dims mx4_dims(int rows, int K)
     return t;
 }
 
+// Rows of one launch, of `threads` threads to the row, in whole tiles of up to 256 rows: a launch has fewer than 2^32 threads, so that 2^30 rows and more go in pieces.
+inline long long piece_rows(long long threads) { return std::max(256ll, (1ll << 31) / threads / 256 * 256); }
+
 // The kernels, by the ids of the test hook.  On codes: tiles of 64 x 64, 128 x 128 and 256 x 256, few rows 32 and 64 at a time.  On 16-bit input: few rows,
 // reductions that fit LDS with 32 rows to the workgroup and (one chunk) with 128, and a quantisation of its own with the product on its codes.
 enum PwKernel { PW_TILE_64 = 70, PW_TILE_128, PW_TILE_256, PW_FEW_32, PW_FEW_64, PW16_FEW, PW16_ROWS, PW16_ROWS_128, PW16_CODES };

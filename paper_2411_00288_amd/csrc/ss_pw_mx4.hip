@@ -760,12 +760,29 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
     return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
 }
 
-int product(const ss_weight_desc *d, PwArgs a, const uint8_t *codes, const uint8_t *scales, hipStream_t s)
+// The layer in pieces of `piece` rows: launch(arguments, first row).
+template <typename F>
+int in_pieces(const PwArgs &all, long long piece, F &&launch)
+{
+    for (long long at = 0; at < all.P; at += piece) {
+        PwArgs a = all;
+        a.P = (int)std::min(piece, all.P - at);
+        a.y += at * a.ldy;
+        if (a.residual != nullptr) a.residual += at * a.ldr;
+        const int st = launch(a, at);
+        if (st != SS_OK) return st;
+    }
+    return SS_OK;
+}
+
+int product(const ss_weight_desc *d, const PwArgs &all, const uint8_t *codes, const uint8_t *scales, hipStream_t s)
 {
     const Mx4Dims t = mx4_dims(d->cout, d->cin);
-    a.codes = codes;
-    a.scales = scales;
-    return d->dtype == SS_F16 ? product_codes<SS_F16>(a, t, s) : product_codes<SS_BF16>(a, t, s);
+    return in_pieces(all, piece_rows(4ll * ((t.Mt + 1) / 2)), [&](PwArgs &a, long long at) {       // (tiles of 64 x 64 have the most threads)
+        a.codes = codes + at * t.KB * 16;
+        a.scales = scales + at * t.S;
+        return d->dtype == SS_F16 ? product_codes<SS_F16>(a, t, s) : product_codes<SS_BF16>(a, t, s);
+    });
 }
 
 }  // namespace
@@ -810,7 +827,11 @@ extern "C" int ss_pw_mx4_fwd(const ss_weight_desc *desc, const void *x, int64_t 
     if (kernel == PW16_CODES && (!workspace || !aligned(workspace, 16) || ws_bytes < codes_bytes(t, rows) + (size_t)rows * t.S)) return SS_ERR_WORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const PwArgs a = pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy);
-    if (kernel != PW16_CODES) return desc->dtype == SS_F16 ? product16<SS_F16>(a, t, kernel, x, ldx, s) : product16<SS_BF16>(a, t, kernel, x, ldx, s);
+    if (kernel != PW16_CODES)
+        return in_pieces(a, piece_rows(16), [&](const PwArgs &part, long long at) {                // (eight waves to 32 rows)
+            const void *const first = static_cast<const uint16_t *>(x) + at * ldx;
+            return desc->dtype == SS_F16 ? product16<SS_F16>(part, t, kernel, first, ldx, s) : product16<SS_BF16>(part, t, kernel, first, ldx, s);
+        });
     uint8_t *codes = static_cast<uint8_t *>(workspace), *scales = codes + codes_bytes(t, rows);
     st = mx4_quantize(x, rows, desc->cin, ldx, desc->dtype, codes, scales, s);
     if (st != SS_OK) return st;
