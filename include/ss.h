@@ -523,7 +523,7 @@ int ss_norm_fwd(const ss_norm_desc *desc, const ss_norm_io *io /*[host]*/, void 
 
 /*
  * Gradient of ss_norm_fwd for a gradient dy of y and one, dx_out, of x_out (NULL: none; needed with SS_NORM_NONE).  Takes the forward pass's x_out
- * (x where there was no h) and h; statistics are computed again.  dx is the gradient of x; dh, and dgate in the type and shape of gate, are
+ * (x where there was no h; not looked at with SS_NORM_NONE) and h; statistics are computed again.  dx is the gradient of x; dh, and dgate in the type and shape of gate, are
  * needed where there is an h and a gate, the fp32 vectors only where they are not NULL.  Sums over rows are made in a fixed order: the
  * same call gives the same bits.  dx may be dy or dx_out, dh may be h.  rows = 0 gives zero vectors, and
  * a zero dgate to a gate of any number of groups.

@@ -1,6 +1,7 @@
 // Max pooling over NHWC 16-bit activations: the one non-convolution step between the convolutions of a
 // ResNet trunk (after the stem), so that a chained stack runs without leaving the library.
 #include "ss_internal.h"
+#include <algorithm>
 
 namespace ss {
 
@@ -136,13 +137,18 @@ extern "C" int ss_maxpool2d(const void *x, int32_t N, int32_t H, int32_t Wd, int
     if (((uintptr_t)x & 15) || ((uintptr_t)y & 15)) return SS_ERR_INVALID_ARG;
     if (H + 2 * pad < k || Wd + 2 * pad < k) return SS_ERR_INVALID_ARG;
     const int Ho = (H + 2 * pad - k) / stride + 1, Wo = (Wd + 2 * pad - k) / stride + 1;
-    const long long total = (long long)N * Ho * Wo * (C / 8);
-    if (total <= 0 || (total + 255) / 256 > 0x7FFFFFFFll) return SS_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((total + 255) / 256)), block(256);
+    // (a launch has fewer than 2^32 threads, and the runtime cuts a larger one without an error: larger batches go in pieces of whole images)
+    const long long each = (long long)Ho * Wo * (C / 8), piece = each > 0 ? (0xFFFFFF00ll / each) : 0;
+    if (each <= 0 || piece == 0) return SS_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint16_t *xs = static_cast<const uint16_t *>(x);
     uint16_t *ys = static_cast<uint16_t *>(y);
-    auto go = [&](auto kern) { kern<<<grid, block, 0, s>>>(xs, ys, N, H, Wd, C, k, stride, pad, Ho, Wo); };
+    auto go = [&](auto kern) {
+        for (long long at = 0; at < N; at += piece) {
+            const int n = (int)std::min(piece, N - at);
+            kern<<<dim3((unsigned)((n * each + 255) / 256)), dim3(256), 0, s>>>(xs + at * H * Wd * C, ys + at * each * 8, n, H, Wd, C, k, stride, pad, Ho, Wo);
+        }
+    };
     if (dtype == SS_F16)
         k == 3 ? go(maxpool_kernel<SS_F16, 3>) : k == 2 ? go(maxpool_kernel<SS_F16, 2>) : go(maxpool_kernel<SS_F16, 0>);
     else

@@ -25,7 +25,8 @@ inline Mx4Dims mx4_dims(int rows, int K)
     return t;
 }
 
-// Rows of one launch, of `threads` threads to the row, in whole tiles of up to 256 rows: a launch has fewer than 2^32 threads, so that 2^30 rows and more go in pieces.
+// Rows of one launch, of `threads` threads to the row, in whole tiles of up to 256 rows: a launch has fewer than 2^32 threads (the
+// runtime cuts a larger one without an error: of 1140850765 rows 1073741773 were not written), so that 2^30 rows and more go in pieces.
 inline long long piece_rows(long long threads) { return std::max(256ll, (1ll << 31) / threads / 256 * 256); }
 
 // The kernels, by the ids of the test hook.  On codes: tiles of 64 x 64, 128 x 128 and 256 x 256, few rows 32 and 64 at a time.  On 16-bit input: few rows,
