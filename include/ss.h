@@ -69,7 +69,7 @@ enum { SS_F16 = 0, SS_BF16 = 1, SS_I8 = 2, SS_F8 = 3 /* OCP FP8 E4M3 (no infinit
        SS_F32 = 4 /* activations of the norm and quantisation calls only */ };
 enum { SS_K_CRS = 0, SS_K_RSC = 1 };
 enum { SS_ACT_NONE = 0, SS_ACT_RELU = 1, SS_ACT_GELU = 2 };
-enum { SS_WEIGHTS_DENSE = 0, SS_WEIGHTS_SPARSE = 1, SS_WEIGHTS_MX4 = 2 }; /* which packing call wrote a weight buffer */
+enum { SS_WEIGHTS_DENSE = 0, SS_WEIGHTS_SPARSE = 1, SS_WEIGHTS_MX4 = 2, SS_WEIGHTS_F8 = 3 }; /* which packing call wrote a weight buffer */
 
 /* Describes one weight matrix W in R^{cout x (cin*kh*kw)} (Eq. 5).  Plain data, passed by pointer [host]. */
 typedef struct {
@@ -173,10 +173,10 @@ int ss_dense_pack(const ss_weight_desc *desc, const void *W, const uint8_t *M, v
  * trust their weight operand: they read it with the sizes the descriptor implies and never look at its header.
  * This call reads the buffer's 256-byte header back (one stream synchronisation, like ss_mask_compress) and returns
  *   SS_ERR_INVALID_ARG  when the buffer was not written by ss_dense_pack (kind SS_WEIGHTS_DENSE), by ss_mx4_pack
- *                       (SS_WEIGHTS_MX4) or by ss_mask_compress / ss_mask_update_compress (any other), or was written
+ *                       (SS_WEIGHTS_MX4), by ss_f8_pack (SS_WEIGHTS_F8) or by ss_mask_compress / ss_mask_update_compress (any other), or was written
  *                       for another cout, cin, kh, kw, dtype or korder than desc states (e.g. a dense operand offered
  *                       to ss_conv2d_fwd);
- *   SS_ERR_UNSUPPORTED  with SS_WEIGHTS_MX4, for a descriptor that ss_mx4_pack does not take;
+ *   SS_ERR_UNSUPPORTED  with SS_WEIGHTS_MX4 or SS_WEIGHTS_F8, for a descriptor that ss_mx4_pack or ss_f8_pack does not take;
  *   SS_ERR_BAD_MASK     when it was written by a compression call that rejected its mask (Eq. 2 violated);
  *   SS_OK               otherwise.
  * Call it once per weight buffer, after packing and before the first convolution.
@@ -480,6 +480,78 @@ int ss_pw_mx4_fwd(const ss_weight_desc *desc, const void *x, int64_t rows, int64
 /* The same on an activation that is quantised already. */
 int ss_pw_mx4_q_fwd(const ss_weight_desc *desc, const void *codes, const void *scales, int64_t rows, const void *packed, const float *bias,
                     const void *residual, int64_t ldr, int32_t act, void *y, int64_t ldy, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * FP8 with a scale for each block of 128: the 8-bit point of the pointwise and linear layers.
+ *
+ * Blocks of 128 consecutive channels of a row share a scale 2^(byte - 127); an element is an OCP E4M3 byte.  With m the block's largest magnitude the scale is
+ * 2^max(ceil(log2(m / 448)), -127), the least power of two that leaves nothing above the type's largest value, and an element the value over the scale, rounded to
+ * nearest even.  A block of zeros has the byte 0.  A NaN or an infinity in a block makes its byte 0xFF: all 128 stand for NaN.
+ *
+ * A quantised activation of `rows` rows (pixels, tokens) and `cols` channels, KB = ceil(cols/128):
+ *   codes   [rows][64*ceil(cols/64)] bytes; those past the last channel are zero.  16-byte aligned.
+ *   scales  [rows][4*ceil(KB/4)] bytes, those past the KB-th zero.  4-byte aligned.
+ * Rows of a 16- or 32-bit tensor may lie further apart than they are long (ld*, in elements), and begin at any element.  rows = 0 does nothing.  At most 2^22 channels.
+ */
+
+/* x [rows][cols] (dtype SS_F16, SS_BF16 or SS_F32) -> codes, scales.  Asynchronous on `stream`. */
+int ss_f8_quantize(const void *x, int64_t rows, int32_t cols, int64_t ldx, int32_t dtype, void *codes, void *scales, void *stream);
+
+/* What codes and scales stand for, rounded to dtype.  Asynchronous on `stream`. */
+int ss_f8_dequantize(const void *codes, const void *scales, int64_t rows, int32_t cols, int32_t dtype, void *y, int64_t ldy, void *stream);
+
+/*
+ * Size in bytes of the weights that ss_f8_pack writes: with Mt = ceil(cout/32), Ks = ceil(cin/64) and Kq = ceil(cin/512)
+ *   bytes [0, 256)  header as at ss_packed_bytes (magic 0x384D5353)
+ *   codes           Mt*Ks*2 tiles of 64 lanes x 16 bytes: lane l of tile (mt, ks, h) holds channels 64*ks + 32*(l/32) + 16*h to 15 more of row 32*mt + l%32
+ *   scales          Mt*Kq tiles of 32 uint32: byte j of word r of tile (mt, q) is the scale of block 4*q + j of row 32*mt + r
+ * Rows, channels and blocks past the last are zero.  SS_ERR_UNSUPPORTED unless the kernel is 1x1, the type SS_F16 or SS_BF16, cin at most 2^22 and the tiles are less
+ * than 2^31 bytes.
+ */
+int ss_f8_packed_bytes(const ss_weight_desc *desc, size_t *packed_bytes /*[host] out*/);
+
+/*
+ * Quantises M (.) W [cout][cin] (blocks along cin) and lays it out for ss_pw_f8_fwd.  M == NULL means all ones; a zero byte drops the weight, and the mask
+ * is not validated here.  transposed = 1: W and M lie as [cin][cout].  (The gradient of a layer's input is the layer with its weights transposed: with a descriptor
+ * of cout and cin exchanged and transposed = 1 the forward weights themselves are packed for it.)  W is not changed.  packed: 16-byte aligned.  Asynchronous.
+ */
+int ss_f8_pack(const ss_weight_desc *desc, const void *W, const uint8_t *M, int32_t transposed, void *packed, void *stream);
+
+/* The values that packed weights stand for, [cout][cin] in desc->dtype (rounded, should the type not hold them).  Asynchronous. */
+int ss_f8_unpack(const ss_weight_desc *desc, const void *packed, void *W, void *stream);
+
+/*
+ * Pointwise (1x1) or linear layer on such operands:
+ *     y[r][o] = act( sum_c Wq[o][c] xq[r][c] + bias[o] + residual[r][o] )
+ * xq is x [rows][cin] (desc->dtype) quantised on the way, to the values of ss_f8_quantize.  One rounding to desc->dtype at the store.  Sums are fp32, but for the
+ * eight products of neighbouring channels (8j to 8j + 7) that the FP8 matrix instruction adds first: of those it drops what lies below 2^-13 of the largest.
+ *   bias      [cout] fp32 or NULL
+ *   residual  [rows][cout] of desc->dtype or NULL; it may be y.
+ *   act       SS_ACT_NONE | SS_ACT_RELU | SS_ACT_GELU
+ *   workspace ss_pw_f8_workspace_bytes bytes, 16-byte aligned, not initialised (SS_ERR_WORKSPACE if it is short); not shared by calls that may run at the same time
+ * Any cout; rows from 0 to 2^31 - 1.  Asynchronous on `stream`.
+ */
+int ss_pw_f8_workspace_bytes(const ss_weight_desc *desc, int64_t rows, size_t *bytes /*[host] out*/);
+int ss_pw_f8_fwd(const ss_weight_desc *desc, const void *x, int64_t rows, int64_t ldx, const void *packed, const float *bias, const void *residual,
+                 int64_t ldr, int32_t act, void *y, int64_t ldy, void *workspace, size_t ws_bytes, void *stream);
+
+/* The same on an activation that is quantised already. */
+int ss_pw_f8_q_fwd(const ss_weight_desc *desc, const void *codes, const void *scales, int64_t rows, const void *packed, const float *bias,
+                   const void *residual, int64_t ldr, int32_t act, void *y, int64_t ldy, void *stream);
+
+/*
+ * Gradient of a pointwise or linear layer's weights and bias, in fp32, for a gradient dy of what stands before its activation:
+ *     dw[o][c] = sum_r dy[r][o] x[r][c]          db[o] = sum_r dy[r][o]
+ * from 16-bit operands as they are, whatever the type of the forward product: the sums are 32 bits wide, which those of 8-bit matrix instructions are not.  A mask
+ * is the caller's to apply.
+ *   dy [rows][cout], x [rows][cin] of desc->dtype (SS_F16 or SS_BF16, a 1x1 kernel: anything else SS_ERR_UNSUPPORTED), pitches in elements, rows from any element on
+ *   dw [cout][cin]; db [cout] or NULL
+ *   workspace ss_pw_wgrad_workspace_bytes bytes, 16-byte aligned, not initialised; not shared by calls that may run at the same time
+ * Sums are made in a fixed order: the same call gives the same bits.  rows from 0 (zeros) to 2^31 - 1.  Asynchronous on `stream`.
+ */
+int ss_pw_wgrad_workspace_bytes(const ss_weight_desc *desc, int64_t rows, size_t *bytes /*[host] out*/);
+int ss_pw_wgrad(const ss_weight_desc *desc, const void *dy, int64_t lddy, const void *x, int64_t ldx, int64_t rows, float *dw, float *db,
+                void *workspace, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------------------------
  * Norms before and after a block, with its gate, its residual scale and the residual sum, over the channels of each row:

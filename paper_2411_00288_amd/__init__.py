@@ -27,6 +27,8 @@ _BINDING_NAMES = {
     "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_packed_bytes", "ss_mx4_pack", "ss_mx4_unpack", "ss_pw_mx4_workspace_bytes",
     "ss_pw_mx4_fwd", "ss_pw_mx4_q_fwd", "make_norm_desc", "ss_norm_fwd", "ss_norm_mx4_fwd", "ss_norm_bwd",
     "ss_norm_bwd_workspace_bytes", "ss_norm_desc", "NormGrads",
+    "SS_WEIGHTS_F8", "ss_f8_quantize", "ss_f8_dequantize", "ss_f8_packed_bytes", "ss_f8_pack", "ss_f8_unpack", "ss_pw_f8_workspace_bytes", "ss_pw_f8_fwd",
+    "ss_pw_f8_q_fwd", "ss_pw_wgrad_workspace_bytes", "ss_pw_wgrad",
 }
 
 

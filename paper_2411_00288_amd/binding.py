@@ -25,7 +25,7 @@ SS_ERR_INVALID_ARG, SS_ERR_BAD_MASK, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ER
 SS_F16, SS_BF16, SS_I8, SS_F8, SS_F32 = 0, 1, 2, 3, 4
 SS_K_CRS, SS_K_RSC = 0, 1
 SS_ACT_NONE, SS_ACT_RELU, SS_ACT_GELU = 0, 1, 2
-SS_WEIGHTS_DENSE, SS_WEIGHTS_SPARSE, SS_WEIGHTS_MX4 = 0, 1, 2
+SS_WEIGHTS_DENSE, SS_WEIGHTS_SPARSE, SS_WEIGHTS_MX4, SS_WEIGHTS_F8 = 0, 1, 2, 3
 SS_NORM_NONE, SS_NORM_LAYER, SS_NORM_RMS = 0, 1, 2
 
 EXPORTS = ["ss_status_string", "ss_packed_bytes", "ss_dense_bytes", "ss_mask_compress", "ss_mask_decompress",
@@ -35,7 +35,8 @@ EXPORTS = ["ss_status_string", "ss_packed_bytes", "ss_dense_bytes", "ss_mask_com
            "ss_weights_check", "ss_conv2d_fwd_static_ws", "ss_conv2d_pw_fused_query", "ss_conv2d_pw2_fused_fwd", "ss_conv2d_pw2_fused_dense_fwd",
            "ss_conv2d_pw2_fused_query", "ss_conv2d_maxpool_dense_fwd", "ss_conv2d_maxpool_dense_query",
            "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_packed_bytes", "ss_mx4_pack", "ss_mx4_unpack", "ss_pw_mx4_workspace_bytes",
-           "ss_pw_mx4_fwd", "ss_pw_mx4_q_fwd", "ss_norm_fwd", "ss_norm_bwd_workspace_bytes", "ss_norm_bwd"]
+           "ss_pw_mx4_fwd", "ss_pw_mx4_q_fwd", "ss_f8_quantize", "ss_f8_dequantize", "ss_f8_packed_bytes", "ss_f8_pack", "ss_f8_unpack",
+           "ss_pw_f8_workspace_bytes", "ss_pw_f8_fwd", "ss_pw_f8_q_fwd", "ss_pw_wgrad_workspace_bytes", "ss_pw_wgrad", "ss_norm_fwd", "ss_norm_bwd_workspace_bytes", "ss_norm_bwd"]
 DEBUG_EXPORTS = ["ss_debug_force_tile", "ss_debug_limit_blocks", "ss_debug_force_split", "ss_debug_issue_peak", "ss_debug_lds_bandwidth"]          # include/ss_debug.h: test hooks
 
 
@@ -119,6 +120,16 @@ def _load() -> ctypes.CDLL:
     lib.ss_pw_mx4_workspace_bytes.argtypes = [dp, i64, ctypes.POINTER(sz)]
     lib.ss_pw_mx4_fwd.argtypes = [dp, vp, i64, i64, vp, vp, vp, i64, i32, vp, i64, vp, sz, vp]
     lib.ss_pw_mx4_q_fwd.argtypes = [dp, vp, vp, i64, vp, vp, vp, i64, i32, vp, i64, vp]
+    lib.ss_f8_quantize.argtypes = lib.ss_mx4_quantize.argtypes
+    lib.ss_f8_dequantize.argtypes = lib.ss_mx4_dequantize.argtypes
+    lib.ss_f8_packed_bytes.argtypes = lib.ss_mx4_packed_bytes.argtypes
+    lib.ss_f8_pack.argtypes = [dp, vp, vp, i32, vp, vp]
+    lib.ss_f8_unpack.argtypes = lib.ss_mx4_unpack.argtypes
+    lib.ss_pw_f8_workspace_bytes.argtypes = lib.ss_pw_mx4_workspace_bytes.argtypes
+    lib.ss_pw_f8_fwd.argtypes = lib.ss_pw_mx4_fwd.argtypes
+    lib.ss_pw_f8_q_fwd.argtypes = lib.ss_pw_mx4_q_fwd.argtypes
+    lib.ss_pw_wgrad_workspace_bytes.argtypes = lib.ss_pw_mx4_workspace_bytes.argtypes
+    lib.ss_pw_wgrad.argtypes = [dp, vp, i64, vp, i64, i64, vp, vp, vp, sz, vp]
     lib.ss_norm_fwd.argtypes = [nd, ctypes.POINTER(ss_norm_io), vp]
     lib.ss_norm_bwd_workspace_bytes.argtypes = [nd, i64, i64, i32, ctypes.POINTER(sz)]
     lib.ss_norm_bwd.argtypes = [nd, ctypes.POINTER(ss_norm_grad_io), vp, sz, vp]
@@ -278,10 +289,10 @@ def ss_dense_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None,
 
 def ss_weights_check(desc: ss_weight_desc, weights: torch.Tensor, sparse: bool | int = True, stream=None) -> None:
     """Raises unless `weights` was written for `desc` by the matching packing call (and, for the sparse form, with a
-    valid mask); sparse: True, False, or SS_WEIGHTS_MX4 for weights of ss_mx4_pack.  One stream synchronisation; call
-    once per buffer at set-up."""
-    kind = SS_WEIGHTS_MX4 if sparse == SS_WEIGHTS_MX4 else SS_WEIGHTS_SPARSE if sparse else SS_WEIGHTS_DENSE
-    need = (ss_dense_bytes, ss_packed_bytes, ss_mx4_packed_bytes)[kind](desc)
+    valid mask); sparse: True, False, or SS_WEIGHTS_MX4 / SS_WEIGHTS_F8 for weights of ss_mx4_pack / ss_f8_pack.  One stream
+    synchronisation; call once per buffer at set-up."""
+    kind = sparse if sparse in (SS_WEIGHTS_MX4, SS_WEIGHTS_F8) else SS_WEIGHTS_SPARSE if sparse else SS_WEIGHTS_DENSE
+    need = (ss_dense_bytes, ss_packed_bytes, ss_mx4_packed_bytes, ss_f8_packed_bytes)[kind](desc)
     if weights is None or weights.numel() * weights.element_size() < need:
         raise SSError(SS_ERR_INVALID_ARG, "ss_weights_check: buffer smaller than the descriptor's size query")
     st = _lib.ss_weights_check(ctypes.byref(desc), _dev_ptr(weights, "weights"), kind, _stream_ptr(stream))
@@ -830,16 +841,19 @@ def ss_mx4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: 
         r = _native.mx4_quantize(x, codes, scales)
         if r is not None:
             return r if type(r[0]) is not int else _failed(r, "ss_mx4_quantize")
-    what = "ss_mx4_quantize"
+    return _quantize("ss_mx4_quantize", _mx4_sizes, x, codes, scales, stream)
+
+
+def _quantize(what, sizes, x, codes, scales, stream):
     if x is None or x.dim() == 0 or x.shape[-1] == 0:
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: x must be [..., cols]")
     cols = x.shape[-1]
     px, rows, ld = _row_tensor(what, "x", x, cols, None)
-    nc, ns = _mx4_sizes(cols)
+    nc, ns = sizes(cols)
     with _on(stream, x.device):
         codes = torch.empty((*x.shape[:-1], nc), dtype=torch.uint8, device=x.device) if codes is None else codes
         scales = torch.empty((*x.shape[:-1], ns), dtype=torch.uint8, device=x.device) if scales is None else scales
-    st = _lib.ss_mx4_quantize(px, rows, cols, ld, _ROW_TYPES[x.dtype], _byte_tensor(what, "codes", codes, rows, nc),
+    st = getattr(_lib, what)(px, rows, cols, ld, _ROW_TYPES[x.dtype], _byte_tensor(what, "codes", codes, rows, nc),
                               _byte_tensor(what, "scales", scales, rows, ns), _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, what)
@@ -853,17 +867,20 @@ def ss_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, cols: int, dtyp
         r = _native.mx4_dequantize(codes, scales, cols, _ROW_TYPES.get(dtype, -1), out)
         if r is not None:
             return r if type(r) is not tuple else _failed(r, "ss_mx4_dequantize")
-    what = "ss_mx4_dequantize"
+    return _dequantize("ss_mx4_dequantize", _mx4_sizes, codes, scales, cols, dtype, out, stream)
+
+
+def _dequantize(what, sizes, codes, scales, cols, dtype, out, stream):
     if dtype not in _ROW_TYPES or cols <= 0:
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: dtype {dtype}, {cols} channels")
-    nc, ns = _mx4_sizes(cols)
+    nc, ns = sizes(cols)
     pc = _byte_tensor(what, "codes", codes, None, nc)
     rows = codes.numel() // nc
     ps = _byte_tensor(what, "scales", scales, rows, ns)
     with _on(stream, codes.device):
         out = torch.empty((*codes.shape[:-1], cols), dtype=dtype, device=codes.device) if out is None else out
     po, _, ld = _row_tensor(what, "out", out, cols, dtype, rows)
-    st = _lib.ss_mx4_dequantize(pc, ps, rows, cols, _ROW_TYPES[dtype], po, ld, _stream_ptr(stream))
+    st = getattr(_lib, what)(pc, ps, rows, cols, _ROW_TYPES[dtype], po, ld, _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, what)
     return out
@@ -879,8 +896,11 @@ def ss_mx4_packed_bytes(desc: ss_weight_desc) -> int:
 
 def ss_mx4_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None = None, packed: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """W [cout, cin] 16-bit, M [cout, cin] uint8 or None -> the masked weights in MXFP4, laid out for ss_pw_mx4_fwd."""
-    what = "ss_mx4_pack"
-    need = ss_mx4_packed_bytes(desc)
+    return _pack("ss_mx4_pack", desc, ss_mx4_packed_bytes(desc), W, M, (), packed, stream)
+
+
+def _pack(what, desc, need, W, M, more, packed, stream):
+    """Checks and makes a packing call for block-scaled weights; `more`: its arguments behind the mask."""
     if W is None or W.numel() != desc.cout * desc.cin or (M is not None and M.numel() != desc.cout * desc.cin):
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: W/M size does not match the descriptor")
     pw, pm = _dev_ptr(W, "W", (torch_dtype(desc.dtype),)), _dev_ptr(M, "M", (torch.uint8, torch.bool), allow_none=True)
@@ -889,7 +909,7 @@ def ss_mx4_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None = 
             packed = torch.empty(need, dtype=torch.uint8, device=W.device)
     elif _nbytes(packed) < need:
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: packed buffer too small")
-    st = _lib.ss_mx4_pack(ctypes.byref(desc), pw, pm, _dev_ptr(packed, "packed"), _stream_ptr(stream))
+    st = getattr(_lib, what)(ctypes.byref(desc), pw, pm, *more, _dev_ptr(packed, "packed"), _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, what)
     return packed
@@ -897,15 +917,18 @@ def ss_mx4_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None = 
 
 def ss_mx4_unpack(desc: ss_weight_desc, packed: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The values [cout, cin] that packed weights stand for."""
-    what = "ss_mx4_unpack"
-    if _nbytes(packed) < ss_mx4_packed_bytes(desc):
+    return _unpack("ss_mx4_unpack", desc, ss_mx4_packed_bytes(desc), packed, out, stream)
+
+
+def _unpack(what, desc, need, packed, out, stream):
+    if _nbytes(packed) < need:
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: packed buffer too small")
     if out is None:
         with _on(stream, packed.device):
             out = torch.empty((desc.cout, desc.cin), dtype=torch_dtype(desc.dtype), device=packed.device)
     elif out.numel() != desc.cout * desc.cin:
         raise SSError(SS_ERR_INVALID_ARG, f"{what}: out does not match the descriptor")
-    st = _lib.ss_mx4_unpack(ctypes.byref(desc), _dev_ptr(packed, "packed"), _dev_ptr(out, "out", (torch_dtype(desc.dtype),)), _stream_ptr(stream))
+    st = getattr(_lib, what)(ctypes.byref(desc), _dev_ptr(packed, "packed"), _dev_ptr(out, "out", (torch_dtype(desc.dtype),)), _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, what)
     return out
@@ -919,10 +942,11 @@ def ss_pw_mx4_workspace_bytes(desc: ss_weight_desc, rows: int) -> int:
     return int(out.value)
 
 
-def _pw_mx4(what, desc, head, rows, lead, device, packed, bias, residual, act, y, workspace, stream):
-    """Checks and makes a pointwise MXFP4 call; `head` is its activation's arguments, `lead` the leading dimensions of y."""
-    if _nbytes(packed) < ss_mx4_packed_bytes(desc):
-        raise SSError(SS_ERR_INVALID_ARG, f"{what}: weight buffer holds {_nbytes(packed)} bytes, the descriptor needs {ss_mx4_packed_bytes(desc)}")
+def _pw(what, desc, need, scratch, head, rows, lead, device, packed, bias, residual, act, y, workspace, stream):
+    """Checks and makes a pointwise call on block-scaled operands; `need`: bytes of its weights, `scratch`: what tells the bytes of its workspace, or None,
+    `head`: its activation's arguments, `lead`: the leading dimensions of y."""
+    if _nbytes(packed) < need:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: weight buffer holds {_nbytes(packed)} bytes, the descriptor needs {need}")
     dtype = torch_dtype(desc.dtype)
     pb = _channel_vector(what, "bias", bias, desc.cout)
     pr, ldr = None, 0
@@ -933,13 +957,13 @@ def _pw_mx4(what, desc, head, rows, lead, device, packed, bias, residual, act, y
             y = torch.empty((*lead, desc.cout), dtype=dtype, device=device)
         py, _, ldy = _row_tensor(what, "y", y, desc.cout, dtype, rows)
         args = (ctypes.byref(desc), *head, _dev_ptr(packed, "packed"), pb, pr, ldr, act, py, ldy)
-        if what == "ss_pw_mx4_fwd":
-            need = ss_pw_mx4_workspace_bytes(desc, rows)
+        if scratch is not None:
+            need = scratch(desc, rows)
             if need > 0 and workspace is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
-            st = _lib.ss_pw_mx4_fwd(*args, _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))
+            st = getattr(_lib, what)(*args, _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))
         else:
-            st = _lib.ss_pw_mx4_q_fwd(*args, _stream_ptr(stream))
+            st = getattr(_lib, what)(*args, _stream_ptr(stream))
     if st != SS_OK:
         raise SSError(st, what)
     return y
@@ -954,7 +978,7 @@ def ss_pw_mx4_fwd(desc: ss_weight_desc, x: torch.Tensor, packed: torch.Tensor, b
             return r if type(r) is not tuple else _failed(r, "ss_pw_mx4_fwd")
     what = "ss_pw_mx4_fwd"
     px, rows, ld = _row_tensor(what, "x", x, desc.cin, torch_dtype(desc.dtype))
-    return _pw_mx4(what, desc, (px, rows, ld), rows, x.shape[:-1], x.device, packed, bias, residual, act, y, workspace, stream)
+    return _pw(what, desc, ss_mx4_packed_bytes(desc), ss_pw_mx4_workspace_bytes, (px, rows, ld), rows, x.shape[:-1], x.device, packed, bias, residual, act, y, workspace, stream)
 
 
 def ss_pw_mx4_q_fwd(desc: ss_weight_desc, codes: torch.Tensor, scales: torch.Tensor, packed: torch.Tensor, bias=None, residual=None, act=SS_ACT_NONE,
@@ -968,8 +992,128 @@ def ss_pw_mx4_q_fwd(desc: ss_weight_desc, codes: torch.Tensor, scales: torch.Ten
     nc, ns = _mx4_sizes(desc.cin)
     pc = _byte_tensor(what, "codes", codes, None, nc)
     rows = codes.numel() // nc
-    return _pw_mx4(what, desc, (pc, _byte_tensor(what, "scales", scales, rows, ns), rows), rows, codes.shape[:-1], codes.device, packed, bias, residual, act,
-                   y, None, stream)
+    return _pw(what, desc, ss_mx4_packed_bytes(desc), None, (pc, _byte_tensor(what, "scales", scales, rows, ns), rows), rows, codes.shape[:-1], codes.device, packed,
+               bias, residual, act, y, None, stream)
+
+
+def _f8_sizes(cols):
+    """Bytes of a row's codes and scales."""
+    return (cols + 63) // 64 * 64, (cols + 511) // 512 * 4
+
+
+def ss_f8_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
+    """x [..., cols] float16, bfloat16 or float32 -> (codes [..., 64*ceil(cols/64)], scales [..., 4*ceil(cols/512)]) uint8 (include/ss.h, FP8 with a scale
+    for each block of 128)."""
+    if stream is None:
+        r = _native.f8_quantize(x, codes, scales)
+        if r is not None:
+            return r if type(r[0]) is not int else _failed(r, "ss_f8_quantize")
+    return _quantize("ss_f8_quantize", _f8_sizes, x, codes, scales, stream)
+
+
+def ss_f8_dequantize(codes: torch.Tensor, scales: torch.Tensor, cols: int, dtype=torch.bfloat16, out: torch.Tensor | None = None,
+                     stream=None) -> torch.Tensor:
+    """The values [..., cols] that codes and scales stand for."""
+    if stream is None:
+        r = _native.f8_dequantize(codes, scales, cols, _ROW_TYPES.get(dtype, -1), out)
+        if r is not None:
+            return r if type(r) is not tuple else _failed(r, "ss_f8_dequantize")
+    return _dequantize("ss_f8_dequantize", _f8_sizes, codes, scales, cols, dtype, out, stream)
+
+
+def ss_f8_packed_bytes(desc: ss_weight_desc) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_f8_packed_bytes(ctypes.byref(desc), ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_f8_packed_bytes")
+    return int(out.value)
+
+
+def ss_f8_pack(desc: ss_weight_desc, W: torch.Tensor, M: torch.Tensor | None = None, transposed: bool = False, packed: torch.Tensor | None = None,
+               stream=None) -> torch.Tensor:
+    """W [cout, cin] 16-bit, M [cout, cin] uint8 or None -> the masked weights in FP8, laid out for ss_pw_f8_fwd.  transposed: W and M are [cin, cout] (the
+    gradient of a layer's input takes the layer's own weights so, with a descriptor of cout and cin exchanged)."""
+    shape = (desc.cin, desc.cout) if transposed else (desc.cout, desc.cin)
+    for name, t in (("W", W), ("M", M)):
+        if t is not None and t.dim() == 2 and tuple(t.shape) != shape:
+            raise SSError(SS_ERR_INVALID_ARG, f"ss_f8_pack: {name} is {tuple(t.shape)}, not {shape}")
+    return _pack("ss_f8_pack", desc, ss_f8_packed_bytes(desc), W, M, (int(bool(transposed)),), packed, stream)
+
+
+def ss_f8_unpack(desc: ss_weight_desc, packed: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The values [cout, cin] that packed weights stand for."""
+    return _unpack("ss_f8_unpack", desc, ss_f8_packed_bytes(desc), packed, out, stream)
+
+
+def ss_pw_f8_workspace_bytes(desc: ss_weight_desc, rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_pw_f8_workspace_bytes(ctypes.byref(desc), rows, ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_pw_f8_workspace_bytes")
+    return int(out.value)
+
+
+def ss_pw_f8_fwd(desc: ss_weight_desc, x: torch.Tensor, packed: torch.Tensor, bias=None, residual=None, act=SS_ACT_NONE, y=None, workspace=None,
+                 stream=None) -> torch.Tensor:
+    """Pointwise or linear layer on FP8 operands: x [..., cin] 16-bit, quantised on the way -> y [..., cout]."""
+    if stream is None:
+        r = _native.pw_f8(desc, x, None, packed, bias, residual, act, y, workspace)
+        if r is not None:
+            return r if type(r) is not tuple else _failed(r, "ss_pw_f8_fwd")
+    what = "ss_pw_f8_fwd"
+    px, rows, ld = _row_tensor(what, "x", x, desc.cin, torch_dtype(desc.dtype))
+    return _pw(what, desc, ss_f8_packed_bytes(desc), ss_pw_f8_workspace_bytes, (px, rows, ld), rows, x.shape[:-1], x.device, packed, bias, residual, act, y, workspace,
+               stream)
+
+
+def ss_pw_f8_q_fwd(desc: ss_weight_desc, codes: torch.Tensor, scales: torch.Tensor, packed: torch.Tensor, bias=None, residual=None, act=SS_ACT_NONE,
+                   y=None, stream=None) -> torch.Tensor:
+    """The same on an activation that ss_f8_quantize has quantised: [..., cin] as codes and scales -> y [..., cout]."""
+    if stream is None:
+        r = _native.pw_f8(desc, codes, scales, packed, bias, residual, act, y, None)
+        if r is not None:
+            return r if type(r) is not tuple else _failed(r, "ss_pw_f8_q_fwd")
+    what = "ss_pw_f8_q_fwd"
+    nc, ns = _f8_sizes(desc.cin)
+    pc = _byte_tensor(what, "codes", codes, None, nc)
+    rows = codes.numel() // nc
+    return _pw(what, desc, ss_f8_packed_bytes(desc), None, (pc, _byte_tensor(what, "scales", scales, rows, ns), rows), rows, codes.shape[:-1], codes.device, packed,
+               bias, residual, act, y, None, stream)
+
+
+def ss_pw_wgrad_workspace_bytes(desc: ss_weight_desc, rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_pw_wgrad_workspace_bytes(ctypes.byref(desc), rows, ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_pw_wgrad_workspace_bytes")
+    return int(out.value)
+
+
+def ss_pw_wgrad(desc: ss_weight_desc, dy: torch.Tensor, x: torch.Tensor, dw=None, db=None, with_bias: bool = True, workspace=None, stream=None):
+    """Gradient of a pointwise or linear layer's weights and bias: dy [..., cout] (of what stands before the activation), x [..., cin] -> (dw [cout, cin], db [cout] or None) float32,
+    from 16-bit operands as they are, whatever the type of the forward product."""
+    if stream is None:
+        r = _native.pw_wgrad(desc, dy, x, dw, db, int(with_bias), workspace)
+        if r is not None:
+            return r if type(r[0]) is not int else _failed(r, "ss_pw_wgrad")
+    what = "ss_pw_wgrad"
+    dtype = torch_dtype(desc.dtype)
+    pd, rows, ldd = _row_tensor(what, "dy", dy, desc.cout, dtype)
+    px, _, ldx = _row_tensor(what, "x", x, desc.cin, dtype, rows)
+    if not with_bias and db is not None:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: db without a bias")
+    need = ss_pw_wgrad_workspace_bytes(desc, rows)
+    with _on(stream, x.device):
+        dw = torch.empty((desc.cout, desc.cin), dtype=torch.float32, device=x.device) if dw is None else dw
+        if with_bias and db is None:
+            db = torch.empty(desc.cout, dtype=torch.float32, device=x.device)
+        if need > 0 and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    st = _lib.ss_pw_wgrad(ctypes.byref(desc), pd, ldd, px, ldx, rows, _channel_vector(what, "dw", dw, desc.cout * desc.cin), _channel_vector(what, "db", db, desc.cout),
+                             _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return dw, db
 
 
 def make_norm_desc(cols, dtype=SS_BF16, norm=SS_NORM_LAYER, eps=1e-6, post=SS_NORM_NONE, post_eps=1e-6) -> ss_norm_desc:

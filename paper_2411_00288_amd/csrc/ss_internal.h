@@ -12,6 +12,7 @@ namespace ss {
 constexpr uint32_t kMagicSparse = 0x34325353u;   // "SS24"
 constexpr uint32_t kMagicDense  = 0x44325353u;   // "SS2D"
 constexpr uint32_t kMagicMx4    = 0x344D5353u;   // "SSM4"
+constexpr uint32_t kMagicF8     = 0x384D5353u;   // "SSM8"
 constexpr uint32_t kNoBadBlock  = 0xFFFFFFFFu;
 constexpr int kHeaderBytes = 256;                // 64 x uint32
 constexpr int kHdrFirstBad = 10;                 // word index of the first-invalid-block field

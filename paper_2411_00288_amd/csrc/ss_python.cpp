@@ -505,6 +505,28 @@ bool rows_out(PyObject *o, const at::Tensor &like, int64_t rows, int64_t cols, a
 int64_t mx4_code_bytes(int64_t cols) { return (cols + 31) / 32 * 16; }
 int64_t mx4_scale_bytes(int64_t cols) { return (cols + 127) / 128 * 4; }
 
+// The block-scaled types: bytes of a row's codes and scales, and their calls.
+struct Mx4 {
+    static int64_t codes(int64_t cols) { return mx4_code_bytes(cols); }
+    static int64_t scales(int64_t cols) { return mx4_scale_bytes(cols); }
+    static constexpr auto quantize = ss_mx4_quantize;
+    static constexpr auto dequantize = ss_mx4_dequantize;
+    static constexpr auto packed_bytes = ss_mx4_packed_bytes;
+    static constexpr auto workspace_bytes = ss_pw_mx4_workspace_bytes;
+    static constexpr auto fwd = ss_pw_mx4_fwd;
+    static constexpr auto q_fwd = ss_pw_mx4_q_fwd;
+};
+struct F8 {
+    static int64_t codes(int64_t cols) { return (cols + 63) / 64 * 64; }
+    static int64_t scales(int64_t cols) { return (cols + 511) / 512 * 4; }
+    static constexpr auto quantize = ss_f8_quantize;
+    static constexpr auto dequantize = ss_f8_dequantize;
+    static constexpr auto packed_bytes = ss_f8_packed_bytes;
+    static constexpr auto workspace_bytes = ss_pw_f8_workspace_bytes;
+    static constexpr auto fwd = ss_pw_f8_fwd;
+    static constexpr auto q_fwd = ss_pw_f8_q_fwd;
+};
+
 // A tuple of what calls gave; nullptr (with Python's error) if one failed.
 PyObject *give_all(std::initializer_list<PyObject *> items)
 {
@@ -522,31 +544,33 @@ PyObject *give_all(std::initializer_list<PyObject *> items)
     return t;
 }
 
-// mx4_quantize(x, codes, scales) -> (codes, scales), (status, row, block) or None
-PyObject *mx4_quantize(PyObject *const *a, Py_ssize_t n)
+// mx4_quantize, f8_quantize(x, codes, scales) -> (codes, scales), (status, row, block) or None
+template <typename T>
+PyObject *block_quantize(PyObject *const *a, Py_ssize_t n)
 {
     Rows x;
     if (n != 3 || !read_rows(a[0], &x)) Py_RETURN_NONE;
     const at::ScalarType st = x.t->scalar_type();
     const int32_t dtype = st == at::kHalf ? SS_F16 : st == at::kBFloat16 ? SS_BF16 : st == at::kFloat ? SS_F32 : -1, cols = (int32_t)x.t->size(-1);
     at::Tensor codes, scales;
-    if (dtype < 0 || !bytes_out(a[1], *x.t, x.rows, mx4_code_bytes(cols), &codes) || !bytes_out(a[2], *x.t, x.rows, mx4_scale_bytes(cols), &scales)) Py_RETURN_NONE;
+    if (dtype < 0 || !bytes_out(a[1], *x.t, x.rows, T::codes(cols), &codes) || !bytes_out(a[2], *x.t, x.rows, T::scales(cols), &scales)) Py_RETURN_NONE;
     const void *xp = x.t->const_data_ptr();
     void *cp = codes.data_ptr(), *sp = scales.data_ptr();
     const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
-    const int status = unlocked([&] { return ss_mx4_quantize(xp, x.rows, cols, x.ld, dtype, cp, sp, s); });
+    const int status = unlocked([&] { return T::quantize(xp, x.rows, cols, x.ld, dtype, cp, sp, s); });
     return status == SS_OK ? give_all({give(a[1], codes), give(a[2], scales)}) : refuse(status);
 }
 
-// mx4_dequantize(codes, scales, cols, dtype, out) -> out, (status, row, block) or None
-PyObject *mx4_dequantize(PyObject *const *a, Py_ssize_t n)
+// mx4_dequantize, f8_dequantize(codes, scales, cols, dtype, out) -> out, (status, row, block) or None
+template <typename T>
+PyObject *block_dequantize(PyObject *const *a, Py_ssize_t n)
 {
     int32_t cols, dtype;
     at::ScalarType st;
     if (n != 5 || !read_int(a[2], &cols) || cols <= 0 || !read_int(a[3], &dtype) || !row_type(dtype, &st)) Py_RETURN_NONE;
     const at::Tensor *codes = dev_tensor(a[0]), *scales = dev_tensor(a[1]);
     if (!codes || !scales || codes->scalar_type() != at::kByte || scales->scalar_type() != at::kByte || codes->dim() == 0 || scales->dim() == 0 ||
-        codes->size(-1) != mx4_code_bytes(cols) || scales->size(-1) != mx4_scale_bytes(cols) || codes->numel() == 0)
+        codes->size(-1) != T::codes(cols) || scales->size(-1) != T::scales(cols) || codes->numel() == 0)
         Py_RETURN_NONE;
     const int64_t rows = codes->numel() / codes->size(-1);
     if (scales->numel() != rows * scales->size(-1)) Py_RETURN_NONE;
@@ -556,17 +580,18 @@ PyObject *mx4_dequantize(PyObject *const *a, Py_ssize_t n)
     const void *cp = codes->const_data_ptr(), *sp = scales->const_data_ptr();
     void *yp = y.data_ptr();
     const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
-    const int status = unlocked([&] { return ss_mx4_dequantize(cp, sp, rows, cols, dtype, yp, ld, s); });
+    const int status = unlocked([&] { return T::dequantize(cp, sp, rows, cols, dtype, yp, ld, s); });
     return status == SS_OK ? give(a[4], y) : refuse(status);
 }
 
-// pw_mx4(desc, x | codes, None | scales, packed, bias, residual, act, y, workspace) -> y, (status, row, block) or None
-PyObject *pw_mx4(PyObject *const *a, Py_ssize_t n)
+// pw_mx4, pw_f8(desc, x | codes, None | scales, packed, bias, residual, act, y, workspace) -> y, (status, row, block) or None
+template <typename T>
+PyObject *block_pw(PyObject *const *a, Py_ssize_t n)
 {
     ss_weight_desc d;
     int32_t act;
     size_t need = 0;
-    if (n != 9 || !read_named(a[0], "ss_weight_desc", &d) || !read_int(a[6], &act) || ss_mx4_packed_bytes(&d, &need) != SS_OK) Py_RETURN_NONE;
+    if (n != 9 || !read_named(a[0], "ss_weight_desc", &d) || !read_int(a[6], &act) || T::packed_bytes(&d, &need) != SS_OK) Py_RETURN_NONE;
     const at::Tensor *packed = dev_tensor(a[3]);
     const float *bias;
     if (!packed || packed->nbytes() < need || !read_channels(a[4], d.cout, &bias)) Py_RETURN_NONE;
@@ -577,7 +602,7 @@ PyObject *pw_mx4(PyObject *const *a, Py_ssize_t n)
     if (quantised) {
         const at::Tensor *c = dev_tensor(a[1]), *sc = dev_tensor(a[2]);
         if (!c || !sc || c->scalar_type() != at::kByte || sc->scalar_type() != at::kByte || c->dim() == 0 || sc->dim() == 0 || c->numel() == 0 ||
-            c->size(-1) != mx4_code_bytes(d.cin) || sc->size(-1) != mx4_scale_bytes(d.cin))
+            c->size(-1) != T::codes(d.cin) || sc->size(-1) != T::scales(d.cin))
             Py_RETURN_NONE;
         x = {c, c->numel() / c->size(-1), 0};
         if (sc->numel() != x.rows * sc->size(-1)) Py_RETURN_NONE;
@@ -597,7 +622,7 @@ PyObject *pw_mx4(PyObject *const *a, Py_ssize_t n)
         wsp = t->data_ptr();
         ws_bytes = t->nbytes();
     } else if (!quantised) {
-        if (ss_pw_mx4_workspace_bytes(&d, x.rows, &ws_bytes) != SS_OK) Py_RETURN_NONE;
+        if (T::workspace_bytes(&d, x.rows, &ws_bytes) != SS_OK) Py_RETURN_NONE;
         if (ws_bytes > 0) {
             ws = at::detail::empty_cuda({(int64_t)ws_bytes}, at::kByte, x.t->device(), c10::nullopt);
             wsp = ws.data_ptr();
@@ -607,10 +632,53 @@ PyObject *pw_mx4(PyObject *const *a, Py_ssize_t n)
     void *yp = y.data_ptr();
     const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
     const int status = unlocked([&] {
-        return quantised ? ss_pw_mx4_q_fwd(&d, xp, scales, x.rows, wp, bias, rp, residual.ld, act, yp, ldy, s)
-                         : ss_pw_mx4_fwd(&d, xp, x.rows, x.ld, wp, bias, rp, residual.ld, act, yp, ldy, wsp, ws_bytes, s);
+        return quantised ? T::q_fwd(&d, xp, scales, x.rows, wp, bias, rp, residual.ld, act, yp, ldy, s)
+                         : T::fwd(&d, xp, x.rows, x.ld, wp, bias, rp, residual.ld, act, yp, ldy, wsp, ws_bytes, s);
     });
     return status == SS_OK ? give(a[7], y) : refuse(status);
+}
+
+// pw_wgrad(desc, dy, x, dw, db, with_bias, workspace) -> (dw, db | None), (status, row, block) or None
+PyObject *pw_wgrad(PyObject *const *a, Py_ssize_t n)
+{
+    ss_weight_desc d;
+    int32_t with_bias;
+    size_t need = 0;
+    if (n != 7 || !read_named(a[0], "ss_weight_desc", &d) || !read_int(a[5], &with_bias) || (!with_bias && a[4] != Py_None) || (d.dtype != SS_F16 && d.dtype != SS_BF16)) Py_RETURN_NONE;
+    const at::ScalarType st = d.dtype == SS_F16 ? at::kHalf : at::kBFloat16;
+    Rows dy, x;
+    if (!read_rows(a[1], &dy) || dy.t->size(-1) != d.cout || dy.t->scalar_type() != st || !read_rows(a[2], dy.rows, d.cin, st, &x)) Py_RETURN_NONE;
+    if (ss_pw_wgrad_workspace_bytes(&d, dy.rows, &need) != SS_OK) Py_RETURN_NONE;
+    at::Tensor out[2], ws;
+    const int64_t sizes[2] = {(int64_t)d.cout * d.cin, d.cout};
+    for (int i = 0; i < (with_bias ? 2 : 1); i++) {
+        if (a[3 + i] == Py_None) {
+            out[i] = i == 0 ? at::detail::empty_cuda({d.cout, d.cin}, at::kFloat, x.t->device(), c10::nullopt) : at::detail::empty_cuda({d.cout}, at::kFloat, x.t->device(), c10::nullopt);
+            continue;
+        }
+        const at::Tensor *t = dev_tensor(a[3 + i]);
+        if (!t || t->scalar_type() != at::kFloat || t->numel() != sizes[i]) Py_RETURN_NONE;
+        out[i] = *t;
+    }
+    void *wsp;
+    size_t ws_bytes = need;
+    if (a[6] != Py_None) {
+        const at::Tensor *t = dev_tensor(a[6]);
+        if (!t) Py_RETURN_NONE;
+        wsp = t->data_ptr();
+        ws_bytes = t->nbytes();
+    } else {
+        ws = at::detail::empty_cuda({(int64_t)need}, at::kByte, x.t->device(), c10::nullopt);
+        wsp = ws.data_ptr();
+    }
+    const void *gp = dy.t->const_data_ptr(), *xp = x.t->const_data_ptr();
+    float *dw = static_cast<float *>(out[0].data_ptr()), *db = with_bias ? static_cast<float *>(out[1].data_ptr()) : nullptr;
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] { return ss_pw_wgrad(&d, gp, dy.ld, xp, x.ld, dy.rows, dw, db, wsp, ws_bytes, s); });
+    if (status != SS_OK) return refuse(status);
+    if (with_bias) return give_all({give(a[3], out[0]), give(a[4], out[1])});
+    Py_INCREF(Py_None);
+    return give_all({give(a[3], out[0]), Py_None});
 }
 
 // The gate of a norm call: [..., 1 or cols], dense, of the activations' type.
@@ -907,9 +975,13 @@ PyMethodDef methods[] = {
     {"maxpool", reinterpret_cast<PyCFunction>(entry<maxpool>), METH_FASTCALL, nullptr},
     {"dwconv", reinterpret_cast<PyCFunction>(entry<dwconv>), METH_FASTCALL, nullptr},
     {"pack", reinterpret_cast<PyCFunction>(entry<pack>), METH_FASTCALL, nullptr},
-    {"mx4_quantize", reinterpret_cast<PyCFunction>(entry<mx4_quantize>), METH_FASTCALL, nullptr},
-    {"mx4_dequantize", reinterpret_cast<PyCFunction>(entry<mx4_dequantize>), METH_FASTCALL, nullptr},
-    {"pw_mx4", reinterpret_cast<PyCFunction>(entry<pw_mx4>), METH_FASTCALL, nullptr},
+    {"mx4_quantize", reinterpret_cast<PyCFunction>(entry<block_quantize<Mx4>>), METH_FASTCALL, nullptr},
+    {"f8_quantize", reinterpret_cast<PyCFunction>(entry<block_quantize<F8>>), METH_FASTCALL, nullptr},
+    {"mx4_dequantize", reinterpret_cast<PyCFunction>(entry<block_dequantize<Mx4>>), METH_FASTCALL, nullptr},
+    {"f8_dequantize", reinterpret_cast<PyCFunction>(entry<block_dequantize<F8>>), METH_FASTCALL, nullptr},
+    {"pw_mx4", reinterpret_cast<PyCFunction>(entry<block_pw<Mx4>>), METH_FASTCALL, nullptr},
+    {"pw_f8", reinterpret_cast<PyCFunction>(entry<block_pw<F8>>), METH_FASTCALL, nullptr},
+    {"pw_wgrad", reinterpret_cast<PyCFunction>(entry<pw_wgrad>), METH_FASTCALL, nullptr},
     {"norm_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd<false>>), METH_FASTCALL, nullptr},
     {"norm_mx4_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd<true>>), METH_FASTCALL, nullptr},
     {"norm_bwd", reinterpret_cast<PyCFunction>(entry<norm_bwd>), METH_FASTCALL, nullptr},
