@@ -68,7 +68,7 @@ enum {
 enum { SS_F16 = 0, SS_BF16 = 1, SS_I8 = 2, SS_F8 = 3 /* OCP FP8 E4M3 (no infinities; S.1111.111 = NaN) */,
        SS_F32 = 4 /* activations of the norm and quantisation calls only */ };
 enum { SS_K_CRS = 0, SS_K_RSC = 1 };
-enum { SS_ACT_NONE = 0, SS_ACT_RELU = 1, SS_ACT_GELU = 2 };
+enum { SS_ACT_NONE = 0, SS_ACT_RELU = 1, SS_ACT_GELU = 2, SS_ACT_SILU = 3 /* z / (1 + e^-z); group norm only */ };
 enum { SS_WEIGHTS_DENSE = 0, SS_WEIGHTS_SPARSE = 1, SS_WEIGHTS_MX4 = 2, SS_WEIGHTS_F8 = 3 }; /* which packing call wrote a weight buffer */
 
 /* Describes one weight matrix W in R^{cout x (cin*kh*kw)} (Eq. 5).  Plain data, passed by pointer [host]. */
@@ -624,6 +624,42 @@ typedef struct {
 
 int ss_norm_bwd_workspace_bytes(const ss_norm_desc *desc, int64_t rows, int64_t groups, int32_t gate_cols, size_t *bytes /*[host] out*/);
 int ss_norm_bwd(const ss_norm_desc *desc, const ss_norm_grad_io *io /*[host]*/, void *workspace, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Group norm of channels-last images with its activation.  For each image and each group of channels/groups neighbouring channels, over its pixels and channels:
+ *     xh = (x - mean) / sqrt(var + eps)        y = act( xh * w + b )
+ * var: the mean of squared differences.  Statistics, sums and the value before the activation are fp32; y is rounded once.
+ * groups = channels normalises each channel of an image by itself, groups = 1 all of them together.
+ */
+
+/* Plain data, passed by pointer [host]. */
+typedef struct {
+    int32_t channels, groups; /* groups divides channels, of which there are at most 16384 */
+    int32_t dtype;            /* SS_F16 | SS_BF16 | SS_F32: x, y, dy, dx */
+    int32_t act;              /* SS_ACT_* */
+    float eps;
+    int32_t reserved;         /* 0 */
+} ss_groupnorm_desc;
+
+/*
+ *   x, y      [images][pixels][channels], pitches of a pixel in elements (images follow each other at that pitch), pixels from any element on; y may be x
+ *   w, b      [channels] fp32 or NULL (1 and 0)
+ *   stats     [images][groups][2] fp32, written: mean and 1 / sqrt(var + eps), for the backward call; 8-byte aligned, or NULL
+ *   workspace ss_groupnorm_workspace_bytes bytes, 16-byte aligned, not initialised; not shared by calls that may run at the same time
+ * No images or no pixels: nothing is done.  At most 2^24 pixels to the image and 2^31 - 1 in all (SS_ERR_UNSUPPORTED).  Asynchronous on `stream`.
+ */
+int ss_groupnorm_workspace_bytes(const ss_groupnorm_desc *desc, int64_t images, int64_t pixels, int32_t backward, size_t *bytes /*[host] out*/);
+int ss_groupnorm_fwd(const ss_groupnorm_desc *desc, const void *x, int64_t ldx, int64_t images, int64_t pixels, const float *w, const float *b,
+                     void *y, int64_t ldy, float *stats, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Its gradient for a gradient dy of y: dx of x (it may be dy), dw and db of the vectors (fp32 [channels], or NULL).  x, stats, w and b as in and from the forward call;
+ * a ReLU's slope at a value that rounds to zero is that of the value in 64 bits, 0 at zero itself.  Sums are made in a fixed order: the same call gives the
+ * same bits.  No images or no pixels: dw and db are zero.  Workspace: with backward = 1.  Asynchronous on `stream`.
+ */
+int ss_groupnorm_bwd(const ss_groupnorm_desc *desc, const void *dy, int64_t lddy, const void *x, int64_t ldx, int64_t images, int64_t pixels,
+                     const float *stats, const float *w, const float *b, void *dx, int64_t lddx, float *dw, float *db,
+                     void *workspace, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -29,6 +29,7 @@ _BINDING_NAMES = {
     "ss_norm_bwd_workspace_bytes", "ss_norm_desc", "NormGrads",
     "SS_WEIGHTS_F8", "ss_f8_quantize", "ss_f8_dequantize", "ss_f8_packed_bytes", "ss_f8_pack", "ss_f8_unpack", "ss_pw_f8_workspace_bytes", "ss_pw_f8_fwd",
     "ss_pw_f8_q_fwd", "ss_pw_wgrad_workspace_bytes", "ss_pw_wgrad",
+    "SS_ACT_SILU", "ss_groupnorm_desc", "make_groupnorm_desc", "ss_groupnorm_workspace_bytes", "ss_groupnorm_fwd", "ss_groupnorm_bwd", "GroupNormGrads",
 }
 
 

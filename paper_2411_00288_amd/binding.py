@@ -24,7 +24,7 @@ SS_OK = 0
 SS_ERR_INVALID_ARG, SS_ERR_BAD_MASK, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE, SS_ERR_HIP = -1, -2, -3, -4, -5
 SS_F16, SS_BF16, SS_I8, SS_F8, SS_F32 = 0, 1, 2, 3, 4
 SS_K_CRS, SS_K_RSC = 0, 1
-SS_ACT_NONE, SS_ACT_RELU, SS_ACT_GELU = 0, 1, 2
+SS_ACT_NONE, SS_ACT_RELU, SS_ACT_GELU, SS_ACT_SILU = 0, 1, 2, 3
 SS_WEIGHTS_DENSE, SS_WEIGHTS_SPARSE, SS_WEIGHTS_MX4, SS_WEIGHTS_F8 = 0, 1, 2, 3
 SS_NORM_NONE, SS_NORM_LAYER, SS_NORM_RMS = 0, 1, 2
 
@@ -36,7 +36,8 @@ EXPORTS = ["ss_status_string", "ss_packed_bytes", "ss_dense_bytes", "ss_mask_com
            "ss_conv2d_pw2_fused_query", "ss_conv2d_maxpool_dense_fwd", "ss_conv2d_maxpool_dense_query",
            "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_packed_bytes", "ss_mx4_pack", "ss_mx4_unpack", "ss_pw_mx4_workspace_bytes",
            "ss_pw_mx4_fwd", "ss_pw_mx4_q_fwd", "ss_f8_quantize", "ss_f8_dequantize", "ss_f8_packed_bytes", "ss_f8_pack", "ss_f8_unpack",
-           "ss_pw_f8_workspace_bytes", "ss_pw_f8_fwd", "ss_pw_f8_q_fwd", "ss_pw_wgrad_workspace_bytes", "ss_pw_wgrad", "ss_norm_fwd", "ss_norm_bwd_workspace_bytes", "ss_norm_bwd"]
+           "ss_pw_f8_workspace_bytes", "ss_pw_f8_fwd", "ss_pw_f8_q_fwd", "ss_pw_wgrad_workspace_bytes", "ss_pw_wgrad", "ss_norm_fwd", "ss_norm_bwd_workspace_bytes", "ss_norm_bwd",
+           "ss_groupnorm_workspace_bytes", "ss_groupnorm_fwd", "ss_groupnorm_bwd"]
 DEBUG_EXPORTS = ["ss_debug_force_tile", "ss_debug_limit_blocks", "ss_debug_force_split", "ss_debug_issue_peak", "ss_debug_lds_bandwidth"]          # include/ss_debug.h: test hooks
 
 
@@ -48,6 +49,11 @@ class ss_weight_desc(ctypes.Structure):
 class ss_norm_desc(ctypes.Structure):
     _fields_ = [("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("post", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("post_eps", ctypes.c_float)]
+
+
+class ss_groupnorm_desc(ctypes.Structure):
+    _fields_ = [("channels", ctypes.c_int32), ("groups", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
 
 
 def _fields(text):
@@ -133,6 +139,10 @@ def _load() -> ctypes.CDLL:
     lib.ss_norm_fwd.argtypes = [nd, ctypes.POINTER(ss_norm_io), vp]
     lib.ss_norm_bwd_workspace_bytes.argtypes = [nd, i64, i64, i32, ctypes.POINTER(sz)]
     lib.ss_norm_bwd.argtypes = [nd, ctypes.POINTER(ss_norm_grad_io), vp, sz, vp]
+    gd = ctypes.POINTER(ss_groupnorm_desc)
+    lib.ss_groupnorm_workspace_bytes.argtypes = [gd, i64, i64, i32, ctypes.POINTER(sz)]
+    lib.ss_groupnorm_fwd.argtypes = [gd, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp, sz, vp]
+    lib.ss_groupnorm_bwd.argtypes = [gd, vp, i64, vp, i64, i64, i64, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
     lib.ss_debug_force_tile.argtypes = [i32]
     lib.ss_debug_limit_blocks.argtypes = [i32]
     lib.ss_debug_force_split.argtypes = [i32]
@@ -1244,3 +1254,95 @@ def ss_norm_bwd(desc: ss_norm_desc, dy, x_out, w=None, b=None, h=None, scale=Non
     if st != SS_OK:
         raise SSError(st, what)
     return NormGrads(dx, dh, dgate, dw, db, dscale, dpost_w, dpost_b)
+
+
+# --------------------------------------------------------------------------------------------
+# Group norm of channels-last images
+# --------------------------------------------------------------------------------------------
+def make_groupnorm_desc(channels, groups, dtype=SS_BF16, act=SS_ACT_NONE, eps=1e-5) -> ss_groupnorm_desc:
+    """Group norm over `groups` groups of neighbouring channels, with the activation behind it; dtype: of every activation."""
+    return ss_groupnorm_desc(int(channels), int(groups), int(dtype), int(act), float(eps), 0)
+
+
+def ss_groupnorm_workspace_bytes(desc: ss_groupnorm_desc, images: int, pixels: int, backward: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    st = _lib.ss_groupnorm_workspace_bytes(ctypes.byref(desc), images, pixels, int(bool(backward)), ctypes.byref(out))
+    if st != SS_OK:
+        raise SSError(st, "ss_groupnorm_workspace_bytes")
+    return int(out.value)
+
+
+def _images(what, name, t, desc, like=None):
+    """Checks a tensor of images [images, ..., channels]; (address, images, pixels, pitch)."""
+    p, rows, ld = _row_tensor(what, name, t, desc.channels, _ROW_DTYPES.get(desc.dtype))
+    if t.dim() < 2:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} must be [images, ..., {desc.channels}]")
+    images = t.shape[0]
+    pixels = 1
+    for size in t.shape[1:-1]:
+        pixels *= size
+    if like is not None and (images, pixels) != like:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: {name} has {images} images of {pixels} pixels, not {like[0]} of {like[1]}")
+    return p, images, pixels, ld
+
+
+def _group_stats(what, stats, images, desc):
+    if stats.numel() != images * desc.groups * 2:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: stats must be [{images}, {desc.groups}, 2] float32")
+    return _dev_ptr(stats, f"{what}: stats", (torch.float32,))
+
+
+def ss_groupnorm_fwd(desc: ss_groupnorm_desc, x: torch.Tensor, w=None, b=None, y=None, stats=None, workspace=None, stream=None):
+    """y = act(groupnorm(x) * w + b) -> (y, stats): x [images, ..., channels], channels last; w, b [channels] float32 or None; stats [images, groups, 2] float32,
+    mean and reciprocal deviation, which ss_groupnorm_bwd takes."""
+    if stream is None:
+        r = _native.groupnorm_fwd(desc, x, w, b, y, stats, workspace)
+        if r is not None:
+            return r if type(r[0]) is not int else _failed(r, "ss_groupnorm_fwd")
+    what = "ss_groupnorm_fwd"
+    px, images, pixels, ldx = _images(what, "x", x, desc)
+    need = ss_groupnorm_workspace_bytes(desc, images, pixels)
+    with _on(stream, x.device):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+        stats = torch.empty((images, desc.groups, 2), dtype=torch.float32, device=x.device) if stats is None else stats
+        if need > 0 and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    py, _, ldy = _row_tensor(what, "y", y, desc.channels, x.dtype, images * pixels)
+    st = _lib.ss_groupnorm_fwd(ctypes.byref(desc), px, ldx, images, pixels, _channel_vector(what, "w", w, desc.channels), _channel_vector(what, "b", b, desc.channels),
+                               py, ldy, _group_stats(what, stats, images, desc), _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace), _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return y, stats
+
+
+class GroupNormGrads(NamedTuple):
+    """Gradients of ss_groupnorm_fwd; None where the call had no such operand."""
+    dx: torch.Tensor
+    dw: torch.Tensor | None
+    db: torch.Tensor | None
+
+
+def ss_groupnorm_bwd(desc: ss_groupnorm_desc, dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, w=None, b=None, workspace=None, stream=None) -> GroupNormGrads:
+    """Gradient of ss_groupnorm_fwd for a gradient dy of y; x, w and b as in the forward call, stats as it gave them."""
+    if stream is None:
+        r = _native.groupnorm_bwd(desc, dy, x, stats, w, b, workspace)
+        if r is not None:
+            return GroupNormGrads(*r) if type(r[0]) is not int else _failed(r, "ss_groupnorm_bwd")
+    what = "ss_groupnorm_bwd"
+    px, images, pixels, ldx = _images(what, "x", x, desc)
+    pd, _, _, ldd = _images(what, "dy", dy, desc, (images, pixels))
+    if stats is None:
+        raise SSError(SS_ERR_INVALID_ARG, f"{what}: stats is None")
+    ps, pw, pb = _group_stats(what, stats, images, desc), _channel_vector(what, "w", w, desc.channels), _channel_vector(what, "b", b, desc.channels)
+    need = ss_groupnorm_workspace_bytes(desc, images, pixels, True)
+    with _on(stream, x.device):
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dw, db = (None if v is None else torch.empty(v.shape, dtype=torch.float32, device=x.device) for v in (w, b))
+        if need > 0 and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    st = _lib.ss_groupnorm_bwd(ctypes.byref(desc), pd, ldd, px, ldx, images, pixels, ps, pw, pb, ctypes.c_void_p(dx.data_ptr()), desc.channels,
+                               _dev_ptr(dw, "dw", allow_none=True), _dev_ptr(db, "db", allow_none=True), _dev_ptr(workspace, "workspace", allow_none=True), _nbytes(workspace),
+                               _stream_ptr(stream))
+    if st != SS_OK:
+        raise SSError(st, what)
+    return GroupNormGrads(dx, dw, db)

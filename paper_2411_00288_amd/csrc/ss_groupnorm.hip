@@ -1,0 +1,230 @@
+// Entry points of the group norm of channels-last images (kernels: ss_groupnorm_kernel.h).
+#include "ss_groupnorm_kernel.h"
+#include "ss_conv_params.h"
+#include <cmath>
+
+namespace ss {
+
+SS_GROUP_LAUNCHES(extern, SS_F16)
+SS_GROUP_LAUNCHES(extern, SS_BF16)
+SS_GROUP_LAUNCHES(extern, SS_F32)
+
+namespace {
+
+// An image's group: its chunks' and channels' moments together.
+__global__ __launch_bounds__(kGroupThreads) void group_stats_kernel(GroupArgs p)
+{
+    __shared__ float shared[kGroupThreads / 64];
+    const int n = (int)(blockIdx.x / (unsigned)p.groups), g = (int)blockIdx.x - n * p.groups;
+    const float2 *const part = p.part + (long long)n * p.chunks * p.C + (long long)g * p.cg;
+    const long long entries = (long long)p.chunks * p.cg;
+    const float m = (float)p.pixels * (float)p.cg;
+    const auto rows_of = [&](int chunk) { return (float)(min(p.pixels, (chunk + 1) * p.per_chunk) - chunk * p.per_chunk); };
+    float s = 0.f;
+    for (long long i = threadIdx.x; i < entries; i += kGroupThreads) {
+        const int chunk = (int)(i / p.cg), c = (int)(i - (long long)chunk * p.cg);
+        s = __builtin_fmaf(part[(long long)chunk * p.C + c].x, rows_of(chunk) / m, s);
+    }
+    const float mean = block_sum(s, shared);
+    s = 0.f;
+    for (long long i = threadIdx.x; i < entries; i += kGroupThreads) {
+        const int chunk = (int)(i / p.cg), c = (int)(i - (long long)chunk * p.cg);
+        const float2 v = part[(long long)chunk * p.C + c];
+        const float d = v.x - mean;
+        s += __builtin_fmaf(d * d, rows_of(chunk), v.y);
+    }
+    const float m2 = block_sum(s, shared);
+    if (threadIdx.x == 0) p.stats[(long long)n * p.groups + g] = float2{mean, reciprocal_root(m2 / m + p.eps)};
+}
+
+// An image's group: its channels' sums over the chunks, and A and B.
+__global__ __launch_bounds__(kGroupThreads) void group_coef_kernel(GroupArgs p)
+{
+    __shared__ float shared[kGroupThreads / 64];
+    const int n = (int)(blockIdx.x / (unsigned)p.groups), g = (int)blockIdx.x - n * p.groups;
+    float a = 0.f, b = 0.f;
+    for (int i = threadIdx.x; i < p.cg; i += kGroupThreads) {
+        const int c = g * p.cg + i;
+        const float2 *part = p.part + (long long)n * p.chunks * p.C + c;
+        float2 s = {0.f, 0.f};
+#pragma unroll 4
+        for (int k = 0; k < p.chunks; k++) {
+            s.x += part[(long long)k * p.C].x;
+            s.y += part[(long long)k * p.C].y;
+        }
+        p.total[(long long)n * p.C + c] = s;
+        const float w = p.w != nullptr ? p.w[c] : 1.f;
+        a = __builtin_fmaf(w, s.x, a);
+        b = __builtin_fmaf(w, s.y, b);
+    }
+    a = block_sum(a, shared);
+    b = block_sum(b, shared);
+    const float m = (float)p.pixels * (float)p.cg;
+    if (threadIdx.x == 0) p.coef[(long long)n * p.groups + g] = float2{a / m, b / m};
+}
+
+// dw and db: the images' sums, 16 channels to the workgroup and 16 slices of the images.
+__global__ __launch_bounds__(256) void group_vectors_kernel(GroupArgs p)
+{
+    __shared__ float2 s[16][17];
+    const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, c = (int)blockIdx.x * 16 + lane;
+    float2 v = {0.f, 0.f};
+    if (c < p.C)
+#pragma unroll 4
+        for (int n = slice; n < p.images; n += 16) {
+            v.x += p.total[(long long)n * p.C + c].x;
+            v.y += p.total[(long long)n * p.C + c].y;
+        }
+    s[slice][lane] = v;
+    __syncthreads();
+    if (slice != 0 || c >= p.C) return;
+    float2 sum = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 16; k++) {
+        sum.x += s[k][lane].x;
+        sum.y += s[k][lane].y;
+    }
+    if (p.dw != nullptr) p.dw[c] = sum.y;
+    if (p.db != nullptr) p.db[c] = sum.x;
+}
+
+constexpr int kMostChannels = 16384;
+constexpr int64_t kMostPixels = 1 << 24;   // (a group's values are counted in fp32)
+
+int check_group(const ss_groupnorm_desc *d, int64_t images, int64_t pixels)
+{
+    if (!d || d->channels <= 0 || d->groups <= 0 || d->channels % d->groups != 0 || d->reserved != 0) return SS_ERR_INVALID_ARG;
+    if (d->dtype != SS_F16 && d->dtype != SS_BF16 && d->dtype != SS_F32) return SS_ERR_INVALID_ARG;
+    if (d->act != SS_ACT_NONE && d->act != SS_ACT_RELU && d->act != SS_ACT_GELU && d->act != SS_ACT_SILU) return SS_ERR_INVALID_ARG;
+    if (!(d->eps >= 0.f) || std::isinf(d->eps) || images < 0 || pixels < 0) return SS_ERR_INVALID_ARG;
+    if (d->channels > kMostChannels || pixels > kMostPixels || images > INT32_MAX || images * std::max<int64_t>(pixels, 1) > INT32_MAX) return SS_ERR_UNSUPPORTED;
+    return SS_OK;
+}
+
+bool rows_ok(const ss_groupnorm_desc *d, const void *p, int64_t ld) { return p && aligned(p, d->dtype == SS_F32 ? 4 : 2) && ld >= d->channels && ld <= INT32_MAX; }
+
+struct GroupPlan {
+    GroupArgs a;
+    size_t total_at, coef_at, stats_at, bytes;
+};
+
+// Chunks: as many as give each compute unit eight workgroups, of at least eight rows to the thread.
+GroupPlan group_plan(const ss_groupnorm_desc *d, long long images, long long pixels, bool backward)
+{
+    GroupPlan g{};
+    GroupArgs &a = g.a;
+    const long long cus = std::max(compute_units(), 1);
+    a.images = (int)images;
+    a.pixels = (int)pixels;
+    a.C = d->channels;
+    a.groups = d->groups;
+    a.cg = d->channels / d->groups;
+    a.act = d->act;
+    a.eps = d->eps;
+    fast_div_setup((unsigned)a.cg, &a.cg_mul, &a.cg_sh);
+    a.lanes = std::min((a.C + 7) / 8, kGroupThreads);
+    a.tiles = ((a.C + 7) / 8 + a.lanes - 1) / a.lanes;
+    a.slots = kGroupThreads / a.lanes;
+    const long long want = std::max(1ll, 8 * cus / (images * a.tiles)), most = std::max(1ll, pixels / (8ll * a.slots));
+    const long long chunks = std::min(want, most);
+    a.per_chunk = (int)((pixels + chunks - 1) / chunks);
+    a.chunks = (int)((pixels + a.per_chunk - 1) / a.per_chunk);
+    const auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
+    g.total_at = up((size_t)images * a.chunks * a.C * sizeof(float2));
+    g.coef_at = g.total_at + (backward ? up((size_t)images * a.C * sizeof(float2)) : 0);
+    g.stats_at = g.coef_at + (backward ? up((size_t)images * a.groups * sizeof(float2)) : 0);
+    g.bytes = g.stats_at + (backward ? 0 : (size_t)images * a.groups * sizeof(float2));
+    return g;
+}
+
+int launch(const GroupArgs &a, int dtype, int stage, hipStream_t s)
+{
+    dtype == SS_F16 ? launch_group<SS_F16>(a, stage, s) : dtype == SS_BF16 ? launch_group<SS_BF16>(a, stage, s) : launch_group<SS_F32>(a, stage, s);
+    return launched();
+}
+
+}  // namespace
+}  // namespace ss
+
+using namespace ss;
+
+extern "C" int ss_groupnorm_workspace_bytes(const ss_groupnorm_desc *d, int64_t images, int64_t pixels, int32_t backward, size_t *bytes)
+{
+    const int st = check_group(d, images, pixels);
+    if (st != SS_OK) return st;
+    if (!bytes || (backward != 0 && backward != 1)) return SS_ERR_INVALID_ARG;
+    *bytes = images == 0 || pixels == 0 ? 0 : group_plan(d, images, pixels, backward != 0).bytes;
+    return SS_OK;
+}
+
+extern "C" int ss_groupnorm_fwd(const ss_groupnorm_desc *d, const void *x, int64_t ldx, int64_t images, int64_t pixels, const float *w, const float *b, void *y, int64_t ldy,
+                                float *stats, void *workspace, size_t ws_bytes, void *stream)
+{
+    const int st = check_group(d, images, pixels);
+    if (st != SS_OK) return st;
+    if (!aligned(w, 4) || !aligned(b, 4) || !aligned(stats, 8)) return SS_ERR_INVALID_ARG;
+    if (images == 0 || pixels == 0) return SS_OK;
+    if (!rows_ok(d, x, ldx) || !rows_ok(d, y, ldy)) return SS_ERR_INVALID_ARG;
+    GroupPlan g = group_plan(d, images, pixels, false);
+    if (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes) return SS_ERR_WORKSPACE;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    char *const ws = static_cast<char *>(workspace);
+    GroupArgs &a = g.a;
+    a.x = static_cast<const char *>(x);
+    a.ldx = ldx;
+    a.out = static_cast<char *>(y);
+    a.ldout = ldy;
+    a.w = w;
+    a.b = b;
+    a.part = reinterpret_cast<float2 *>(ws);
+    a.stats = stats ? reinterpret_cast<float2 *>(stats) : reinterpret_cast<float2 *>(ws + g.stats_at);
+    int done = launch(a, d->dtype, 0, s);
+    if (done != SS_OK) return done;
+    group_stats_kernel<<<dim3((unsigned)(images * a.groups)), dim3(kGroupThreads), 0, s>>>(a);
+    done = launched();
+    return done != SS_OK ? done : launch(a, d->dtype, 1, s);
+}
+
+extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int64_t lddy, const void *x, int64_t ldx, int64_t images, int64_t pixels, const float *stats,
+                                const float *w, const float *b, void *dx, int64_t lddx, float *dw, float *db, void *workspace, size_t ws_bytes, void *stream)
+{
+    const int st = check_group(d, images, pixels);
+    if (st != SS_OK) return st;
+    if (!aligned(w, 4) || !aligned(b, 4) || !aligned(dw, 4) || !aligned(db, 4) || !aligned(stats, 8)) return SS_ERR_INVALID_ARG;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    GroupPlan g = group_plan(d, std::max<int64_t>(images, 1), std::max<int64_t>(pixels, 1), true);
+    GroupArgs &a = g.a;
+    a.dw = dw;
+    a.db = db;
+    const auto vectors = [&] {
+        if (!dw && !db) return (int)SS_OK;
+        group_vectors_kernel<<<dim3((unsigned)((a.C + 15) / 16)), dim3(256), 0, s>>>(a);
+        return launched();
+    };
+    if (images == 0 || pixels == 0) {                       // sums over nothing
+        a.images = 0;
+        return vectors();
+    }
+    if (!stats || !rows_ok(d, x, ldx) || !rows_ok(d, dy, lddy) || !rows_ok(d, dx, lddx)) return SS_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes) return SS_ERR_WORKSPACE;
+    char *const ws = static_cast<char *>(workspace);
+    a.x = static_cast<const char *>(x);
+    a.ldx = ldx;
+    a.dy = static_cast<const char *>(dy);
+    a.lddy = lddy;
+    a.out = static_cast<char *>(dx);
+    a.ldout = lddx;
+    a.w = w;
+    a.b = b;
+    a.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
+    a.part = reinterpret_cast<float2 *>(ws);
+    a.total = reinterpret_cast<float2 *>(ws + g.total_at);
+    a.coef = reinterpret_cast<float2 *>(ws + g.coef_at);
+    int done = launch(a, d->dtype, 2, s);
+    if (done != SS_OK) return done;
+    group_coef_kernel<<<dim3((unsigned)(images * a.groups)), dim3(kGroupThreads), 0, s>>>(a);
+    done = launched();
+    if (done != SS_OK) return done;
+    done = launch(a, d->dtype, 3, s);
+    return done != SS_OK ? done : vectors();
+}

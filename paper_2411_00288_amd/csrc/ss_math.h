@@ -82,9 +82,8 @@ __device__ __forceinline__ float widen(uint16_t bits)
 // 0, the limits.  Elsewhere the difference is the smaller one and keeps its bits.  (One register less than a bounded a, which made the kernels with short MXFP4 reductions
 // spill: 64 -> 64 on 99284 rows 9.7 -> 11.2 us.)
 template <int ODT>
-__device__ __forceinline__ float gelu_cdf(float z)
+__device__ __forceinline__ float log2_upper_tail(float a)
 {
-    const float a = fabsf(z);
     float q;
     if constexpr (ODT == SS_F16) {
         q = -8.120558493747162e-07f;
@@ -109,6 +108,13 @@ __device__ __forceinline__ float gelu_cdf(float z)
         q = __builtin_fmaf(q, a, -1.1511123180389404f);
         q = __builtin_fmaf(q, a, -0.9999998807907104f);
     }
+    return q;
+}
+
+template <int ODT>
+__device__ __forceinline__ float gelu_cdf(float z)
+{
+    const float a = fabsf(z), q = log2_upper_tail<ODT>(a);
     // (the IEEE 754-2019 maximum: fmaxf takes a second instruction, which quiets a signalling NaN first)
     const float positive = floor_at(z, 0.f);
     return __builtin_fminf(__builtin_fmaf(-a, __builtin_amdgcn_exp2f(q), positive), positive);

@@ -681,6 +681,98 @@ PyObject *pw_wgrad(PyObject *const *a, Py_ssize_t n)
     return give_all({give(a[3], out[0]), Py_None});
 }
 
+// Images of channels-last rows: x [images, ..., channels] of a group norm's descriptor.
+bool read_images(PyObject *o, const ss_groupnorm_desc &d, at::ScalarType st, Rows *x, int64_t *images)
+{
+    if (!read_rows(o, x) || x->t->dim() < 2 || x->t->size(-1) != d.channels || x->t->scalar_type() != st) return false;
+    *images = x->t->size(0);
+    return true;
+}
+
+// A workspace of `need` bytes: `o`, or a new one.
+bool workspace_in(PyObject *o, const at::Tensor &like, size_t need, at::Tensor *ws, void **p, size_t *bytes)
+{
+    if (o != Py_None) {
+        const at::Tensor *t = dev_tensor(o);
+        if (!t) return false;
+        *p = t->data_ptr();
+        *bytes = t->nbytes();
+        return true;
+    }
+    *ws = at::detail::empty_cuda({(int64_t)need}, at::kByte, like.device(), c10::nullopt);
+    *p = ws->data_ptr();
+    *bytes = need;
+    return true;
+}
+
+// groupnorm_fwd(desc, x, w, b, y, stats, workspace) -> (y, stats), (status, row, block) or None
+PyObject *groupnorm_fwd(PyObject *const *a, Py_ssize_t n)
+{
+    ss_groupnorm_desc d;
+    at::ScalarType st;
+    Rows x;
+    int64_t images, ldy;
+    const float *w, *b;
+    size_t need = 0, ws_bytes = 0;
+    void *wsp = nullptr;
+    if (n != 7 || !read_named(a[0], "ss_groupnorm_desc", &d) || !row_type(d.dtype, &st) || !read_images(a[1], d, st, &x, &images) ||
+        !read_channels(a[2], d.channels, &w) || !read_channels(a[3], d.channels, &b) || ss_groupnorm_workspace_bytes(&d, images, x.rows / images, 0, &need) != SS_OK)
+        Py_RETURN_NONE;
+    at::Tensor y, stats, ws;
+    if (!rows_out(a[4], *x.t, x.rows, d.channels, st, &y, &ldy)) Py_RETURN_NONE;
+    if (a[5] == Py_None) {
+        stats = at::detail::empty_cuda({images, (int64_t)d.groups, 2}, at::kFloat, x.t->device(), c10::nullopt);
+    } else {
+        const at::Tensor *t = dev_tensor(a[5]);
+        if (!t || t->scalar_type() != at::kFloat || t->numel() != images * d.groups * 2) Py_RETURN_NONE;
+        stats = *t;
+    }
+    if (!workspace_in(a[6], *x.t, need, &ws, &wsp, &ws_bytes)) Py_RETURN_NONE;
+    const void *xp = x.t->const_data_ptr();
+    void *yp = y.data_ptr();
+    float *sp = static_cast<float *>(stats.data_ptr());
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status = unlocked([&] { return ss_groupnorm_fwd(&d, xp, x.ld, images, x.rows / images, w, b, yp, ldy, sp, wsp, ws_bytes, s); });
+    return status == SS_OK ? give_all({give(a[4], y), give(a[5], stats)}) : refuse(status);
+}
+
+// groupnorm_bwd(desc, dy, x, stats, w, b, workspace) -> (dx, dw | None, db | None), (status, row, block) or None
+PyObject *groupnorm_bwd(PyObject *const *a, Py_ssize_t n)
+{
+    ss_groupnorm_desc d;
+    at::ScalarType st;
+    Rows x, dy;
+    int64_t images, lddx;
+    const float *w, *b;
+    size_t need = 0, ws_bytes = 0;
+    void *wsp = nullptr;
+    if (n != 7 || !read_named(a[0], "ss_groupnorm_desc", &d) || !row_type(d.dtype, &st) || !read_images(a[2], d, st, &x, &images) || !read_rows(a[1], x.rows, d.channels, st, &dy) ||
+        dy.t->dim() < 2 || dy.t->size(0) != images || !read_channels(a[4], d.channels, &w) || !read_channels(a[5], d.channels, &b) ||
+        ss_groupnorm_workspace_bytes(&d, images, x.rows / images, 1, &need) != SS_OK)
+        Py_RETURN_NONE;
+    const at::Tensor *stats = dev_tensor(a[3]);
+    if (!stats || stats->scalar_type() != at::kFloat || stats->numel() != images * d.groups * 2) Py_RETURN_NONE;
+    at::Tensor dx, dw, db, ws;
+    if (!rows_out(Py_None, *x.t, x.rows, d.channels, st, &dx, &lddx)) Py_RETURN_NONE;
+    if (w) dw = at::detail::empty_cuda(THPVariable_Unpack(a[4]).sizes(), at::kFloat, x.t->device(), c10::nullopt);
+    if (b) db = at::detail::empty_cuda(THPVariable_Unpack(a[5]).sizes(), at::kFloat, x.t->device(), c10::nullopt);
+    if (!workspace_in(a[6], *x.t, need, &ws, &wsp, &ws_bytes)) Py_RETURN_NONE;
+    const void *xp = x.t->const_data_ptr(), *gp = dy.t->const_data_ptr();
+    const float *sp = static_cast<const float *>(stats->const_data_ptr());
+    void *dxp = dx.data_ptr();
+    float *dwp = w ? static_cast<float *>(dw.data_ptr()) : nullptr, *dbp = b ? static_cast<float *>(db.data_ptr()) : nullptr;
+    const hipStream_t s = c10::hip::getCurrentHIPStream().stream();
+    const int status =
+        unlocked([&] { return ss_groupnorm_bwd(&d, gp, dy.ld, xp, x.ld, images, x.rows / images, sp, w, b, dxp, lddx, dwp, dbp, wsp, ws_bytes, s); });
+    if (status != SS_OK) return refuse(status);
+    const auto made = [](const at::Tensor &t) {
+        if (t.defined()) return give(Py_None, t);
+        Py_INCREF(Py_None);
+        return Py_None;
+    };
+    return give_all({made(dx), made(dw), made(db)});
+}
+
 // The gate of a norm call: [..., 1 or cols], dense, of the activations' type.
 bool read_gate(PyObject *o, int64_t cols, at::ScalarType st, const at::Tensor **t, int64_t *groups, int32_t *gate_cols)
 {
@@ -982,6 +1074,8 @@ PyMethodDef methods[] = {
     {"pw_mx4", reinterpret_cast<PyCFunction>(entry<block_pw<Mx4>>), METH_FASTCALL, nullptr},
     {"pw_f8", reinterpret_cast<PyCFunction>(entry<block_pw<F8>>), METH_FASTCALL, nullptr},
     {"pw_wgrad", reinterpret_cast<PyCFunction>(entry<pw_wgrad>), METH_FASTCALL, nullptr},
+    {"groupnorm_fwd", reinterpret_cast<PyCFunction>(entry<groupnorm_fwd>), METH_FASTCALL, nullptr},
+    {"groupnorm_bwd", reinterpret_cast<PyCFunction>(entry<groupnorm_bwd>), METH_FASTCALL, nullptr},
     {"norm_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd<false>>), METH_FASTCALL, nullptr},
     {"norm_mx4_fwd", reinterpret_cast<PyCFunction>(entry<norm_fwd<true>>), METH_FASTCALL, nullptr},
     {"norm_bwd", reinterpret_cast<PyCFunction>(entry<norm_bwd>), METH_FASTCALL, nullptr},
