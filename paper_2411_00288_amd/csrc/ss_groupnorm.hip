@@ -1,5 +1,5 @@
-// Entry points of the group norm of channels-last images (kernels: ss_groupnorm_kernel.h).
-#include "ss_groupnorm_kernel.h"
+// Entry points of the group norm of channels-last images (kernels: ss_groupnorm_kernel.h and, where a workgroup holds its data, ss_groupnorm_held.h).
+#include "ss_groupnorm_held.h"
 #include "ss_conv_params.h"
 #include <cmath>
 
@@ -8,6 +8,9 @@ namespace ss {
 SS_GROUP_LAUNCHES(extern, SS_F16)
 SS_GROUP_LAUNCHES(extern, SS_BF16)
 SS_GROUP_LAUNCHES(extern, SS_F32)
+SS_HELD_LAUNCHES(extern, SS_F16)
+SS_HELD_LAUNCHES(extern, SS_BF16)
+SS_HELD_LAUNCHES(extern, SS_F32)
 
 namespace {
 
@@ -103,8 +106,42 @@ int check_group(const ss_groupnorm_desc *d, int64_t images, int64_t pixels)
 
 bool rows_ok(const ss_groupnorm_desc *d, const void *p, int64_t ld) { return p && aligned(p, d->dtype == SS_F32 ? 4 : 2) && ld >= d->channels && ld <= INT32_MAX; }
 
+// The kernels, by the ids of the test hook.
+enum { GROUP_HELD = 95, GROUP_PASSES };
+
+// A workgroup's share of an image where it can be held; threads = 0: it cannot.
+HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pixels, bool backward)
+{
+    HeldShape h{};
+    const int C = d->channels, cg = C / d->groups, item = d->dtype == SS_F32 ? 4 : 2, most_rows = held_most_rows(d->dtype);
+    const long long cus = std::max(compute_units(), 1);
+    if (C < 8 || forced_tile() == GROUP_PASSES) return h;
+    for (int segment = 64; segment >= 16; segment /= 2) {
+        HeldShape s{};
+        s.groups = std::min(d->groups, std::max(1, (segment + cg * item - 1) / (cg * item)));
+        s.width = s.groups * cg;
+        s.bundles = (d->groups + s.groups - 1) / s.groups;
+        s.lanes = (s.width + 7) / 8;
+        for (int threads = 256; threads <= held_most_threads(backward); threads *= 2) {
+            if (s.lanes > threads) continue;
+            const int slots = threads / s.lanes;
+            const long long rows = (pixels + slots - 1) / slots;
+            if (rows > most_rows) continue;
+            s.threads = threads;
+            s.slots = slots;
+            s.rows = (int)rows;
+            if (rows <= 4) break;                           // (fewer rows to the thread gain nothing)
+        }
+        if (s.threads == 0 || (h.threads != 0 && s.groups == h.groups)) continue;
+        h = s;
+        if (images * s.bundles >= cus) break;
+    }
+    return h;
+}
+
 struct GroupPlan {
     GroupArgs a;
+    HeldShape held;
     size_t total_at, coef_at, stats_at, bytes;
 };
 
@@ -134,6 +171,11 @@ GroupPlan group_plan(const ss_groupnorm_desc *d, long long images, long long pix
     g.coef_at = g.total_at + (backward ? up((size_t)images * a.C * sizeof(float2)) : 0);
     g.stats_at = g.coef_at + (backward ? up((size_t)images * a.groups * sizeof(float2)) : 0);
     g.bytes = g.stats_at + (backward ? 0 : (size_t)images * a.groups * sizeof(float2));
+    g.held = held_shape(d, images, pixels, backward);
+    if (g.held.threads != 0) {                              // only the images' sums, of several images
+        g.total_at = 0;
+        g.bytes = backward && images > 1 ? (size_t)images * a.C * sizeof(float2) : 0;
+    }
     return g;
 }
 
@@ -141,6 +183,11 @@ int launch(const GroupArgs &a, int dtype, int stage, hipStream_t s)
 {
     dtype == SS_F16 ? launch_group<SS_F16>(a, stage, s) : dtype == SS_BF16 ? launch_group<SS_BF16>(a, stage, s) : launch_group<SS_F32>(a, stage, s);
     return launched();
+}
+
+int launch(const GroupArgs &a, const HeldShape &h, int dtype, bool backward, hipStream_t s)
+{
+    return dtype == SS_F16 ? launch_held<SS_F16>(a, h, backward, s) : dtype == SS_BF16 ? launch_held<SS_BF16>(a, h, backward, s) : launch_held<SS_F32>(a, h, backward, s);
 }
 
 }  // namespace
@@ -166,7 +213,7 @@ extern "C" int ss_groupnorm_fwd(const ss_groupnorm_desc *d, const void *x, int64
     if (images == 0 || pixels == 0) return SS_OK;
     if (!rows_ok(d, x, ldx) || !rows_ok(d, y, ldy)) return SS_ERR_INVALID_ARG;
     GroupPlan g = group_plan(d, images, pixels, false);
-    if (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes) return SS_ERR_WORKSPACE;
+    if (g.bytes > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes)) return SS_ERR_WORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     char *const ws = static_cast<char *>(workspace);
     GroupArgs &a = g.a;
@@ -177,7 +224,9 @@ extern "C" int ss_groupnorm_fwd(const ss_groupnorm_desc *d, const void *x, int64
     a.w = w;
     a.b = b;
     a.part = reinterpret_cast<float2 *>(ws);
-    a.stats = stats ? reinterpret_cast<float2 *>(stats) : reinterpret_cast<float2 *>(ws + g.stats_at);
+    a.stats = reinterpret_cast<float2 *>(stats);
+    if (g.held.threads != 0) return launch(a, g.held, d->dtype, false, s);
+    if (!stats) a.stats = reinterpret_cast<float2 *>(ws + g.stats_at);
     int done = launch(a, d->dtype, 0, s);
     if (done != SS_OK) return done;
     group_stats_kernel<<<dim3((unsigned)(images * a.groups)), dim3(kGroupThreads), 0, s>>>(a);
@@ -206,7 +255,7 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
         return vectors();
     }
     if (!stats || !rows_ok(d, x, ldx) || !rows_ok(d, dy, lddy) || !rows_ok(d, dx, lddx)) return SS_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes) return SS_ERR_WORKSPACE;
+    if (g.bytes > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes)) return SS_ERR_WORKSPACE;
     char *const ws = static_cast<char *>(workspace);
     a.x = static_cast<const char *>(x);
     a.ldx = ldx;
@@ -220,6 +269,10 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
     a.part = reinterpret_cast<float2 *>(ws);
     a.total = reinterpret_cast<float2 *>(ws + g.total_at);
     a.coef = reinterpret_cast<float2 *>(ws + g.coef_at);
+    if (g.held.threads != 0) {
+        const int held = launch(a, g.held, d->dtype, true, s);
+        return held != SS_OK || images == 1 ? held : vectors();
+    }
     int done = launch(a, d->dtype, 2, s);
     if (done != SS_OK) return done;
     group_coef_kernel<<<dim3((unsigned)(images * a.groups)), dim3(kGroupThreads), 0, s>>>(a);

@@ -1,0 +1,318 @@
+// Group norm of images that a workgroup can hold: one pass over the data.
+//
+// A workgroup takes one image's bundle of neighbouring groups, so many that a pixel's share is worth a memory access, and keeps it in registers from its only read to its only write: a
+// thread holds eight channels of every R-th pixel.  The mean is found first and the squares of the differences from it then.  Sums go over the threads in LDS:
+// first each channel's over the threads that hold it, then each group's over its channels.  Bundles of an image follow each other on one XCD, so that a line whose channels several
+// of them share is read and written once.
+#ifndef SS_GROUPNORM_HELD_H_
+#define SS_GROUPNORM_HELD_H_
+#include "ss_groupnorm_kernel.h"
+#include "ss_lds.h"
+
+namespace ss {
+
+// The shape of a workgroup: its groups, their channels, threads of a pixel, pixels at a time, pixels of a thread.
+struct HeldShape {
+    int groups, width, lanes, slots, rows, threads, bundles;
+};
+
+constexpr int held_most_threads(bool backward) { return backward ? 512 : 1024; }
+// Registers of a thread for data, in values of 16 bits: 16 rows of 8 values forward, and of two tensors backward.
+constexpr int held_most_rows(int dt) { return dt == SS_F32 ? 8 : 16; }
+
+// LDS of a workgroup, in floats, behind each other: the threads' values, the channels', the groups'.
+inline size_t held_lds(const HeldShape &h, int values) { return ((size_t)values * (8 * (size_t)h.threads + (size_t)h.lanes * 8 + h.groups)) * sizeof(float); }
+
+// N sums over the workgroup at once: v[i][e] of every thread -> channel[i * lanes * 8 + c] and group[i * groups + g], weighted by the channel's `weight`.  Entered and left behind a barrier.
+template <int N, typename Weight>
+__device__ __forceinline__ void held_sums(const HeldShape &h, int cg, const float (&v)[N][8], float *shared, float *channel, float *group, Weight &&weight)
+{
+    const int t = threadIdx.x, T = h.threads, lane = t % 64, wave = t / 64, waves = T / 64;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) shared[(i * 8 + e) * T + t] = v[i][e];
+    __syncthreads();
+    if (h.slots >= 32) {
+        // a wave to the channel
+        for (int c = wave; c < h.width; c += waves) {
+            float s[N] = {};
+            const float *const from = shared + (c % 8) * T + c / 8;
+            for (int k = lane; k < h.slots; k += 64)
+#pragma unroll
+                for (int i = 0; i < N; i++) s[i] += from[i * 8 * T + k * h.lanes];
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const float sum = lanes_sum<64>(s[i]);
+                if (lane == 0) channel[i * h.lanes * 8 + c] = sum;
+            }
+        }
+    } else {
+        for (int c = t; c < h.width; c += T) {
+            float s[N] = {};
+            const float *const from = shared + (c % 8) * T + c / 8;
+            for (int k = 0; k < h.slots; k++)
+#pragma unroll
+                for (int i = 0; i < N; i++) s[i] += from[i * 8 * T + k * h.lanes];
+#pragma unroll
+            for (int i = 0; i < N; i++) channel[i * h.lanes * 8 + c] = s[i];
+        }
+    }
+    __syncthreads();
+    if (cg <= 16) {
+        for (int g = t; g < h.groups; g += T) {
+            float s[N] = {};
+            for (int c = g * cg; c < (g + 1) * cg; c++)
+#pragma unroll
+                for (int i = 0; i < N; i++) s[i] = __builtin_fmaf(weight(c), channel[i * h.lanes * 8 + c], s[i]);
+#pragma unroll
+            for (int i = 0; i < N; i++) group[i * h.groups + g] = s[i];
+        }
+    } else {
+        for (int g = wave; g < h.groups; g += waves) {
+            float s[N] = {};
+            for (int c = g * cg + lane; c < (g + 1) * cg; c += 64)
+#pragma unroll
+                for (int i = 0; i < N; i++) s[i] = __builtin_fmaf(weight(c), channel[i * h.lanes * 8 + c], s[i]);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const float sum = lanes_sum<64>(s[i]);
+                if (lane == 0) group[i * h.groups + g] = sum;
+            }
+        }
+    }
+    __syncthreads();
+}
+
+struct HeldPlace {
+    int n, c0, c, slot, left, rows;        // image, the bundle's first channel, the thread's, its pixel, its channels in the bundle, its pixels
+};
+
+__device__ __forceinline__ HeldPlace held_place(const GroupArgs &p, const HeldShape &h)
+{
+    HeldPlace q;
+    const int total = (int)gridDim.x, xcd = (int)blockIdx.x % 8, id = xcd * (total / 8) + min(xcd, total % 8) + (int)blockIdx.x / 8;
+    q.n = id / h.bundles;
+    q.c0 = (id - q.n * h.bundles) * h.width;
+    q.slot = (int)threadIdx.x / h.lanes;
+    const int run = ((int)threadIdx.x - q.slot * h.lanes) * 8;
+    q.c = q.c0 + run;
+    q.left = min(h.width - run, p.C - q.c);                // (a last bundle may be narrower)
+    q.rows = q.slot < h.slots && q.left > 0 ? max(0, (p.pixels - q.slot + h.slots - 1) / h.slots) : 0;
+    return q;
+}
+
+// act over all of a thread's rows: the choice stands outside of them.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F &&f)
+{
+    if (act == SS_ACT_RELU)
+        f(std::integral_constant<int, SS_ACT_RELU>{});
+    else if (act == SS_ACT_SILU)
+        f(std::integral_constant<int, SS_ACT_SILU>{});
+    else if (act == SS_ACT_GELU)
+        f(std::integral_constant<int, SS_ACT_GELU>{});
+    else
+        f(std::integral_constant<int, SS_ACT_NONE>{});
+}
+
+// ONE: a thread's eight channels are of one group.
+template <int DT, int NR, int MODE, bool ONE>
+__global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(GroupArgs p, HeldShape h)
+{
+    constexpr int B = item_bytes<DT>(), G = ONE ? 1 : 8;
+    extern __shared__ float smem[];
+    const HeldPlace q = held_place(p, h);
+    float *const channel = smem + 8 * h.threads, *const group = channel + h.lanes * 8;
+    const long long first = (long long)q.n * p.pixels + q.slot;
+    Run<DT> raw[NR];
+#pragma unroll
+    for (int i = 0; i < NR; i++)
+        if (q.rows > 0) raw[i] = row_run<DT, MODE>(p.x + (first + (long long)min(i, q.rows - 1) * h.slots) * p.ldx * B, q.c, q.left, p.C);
+    float w[8], b[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const int c = min(q.c + e, p.C - 1);
+        w[e] = p.w != nullptr ? p.w[c] : 1.f;
+        b[e] = p.b != nullptr ? p.b[c] : 0.f;
+    }
+    const auto values = [&](int i, float (&v)[8]) { row_values<DT, MODE>(raw[i], q.c, i < q.rows ? q.left : 0, p.C, v); };
+    int g[G];                                              // groups in the bundle
+#pragma unroll
+    for (int e = 0; e < G; e++) g[e] = min(group_of(p, max(min(q.c + e, p.C - 1) - q.c0, 0)), h.groups - 1);
+    const auto one = [](int) { return 1.f; };
+    const float inv = 1.f / ((float)p.pixels * (float)p.cg);
+    float s[1][8] = {};
+#pragma unroll
+    for (int i = 0; i < NR; i++)
+        if (i < q.rows) {
+            float v[8];
+            values(i, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++) s[0][e] += v[e];
+        }
+    held_sums<1>(h, p.cg, s, smem, channel, group, one);
+    float mean[G];
+#pragma unroll
+    for (int e = 0; e < G; e++) mean[e] = group[g[e]] * inv;
+    const int mine = (int)threadIdx.x;
+    const float mean_out = mine < h.groups ? group[mine] * inv : 0.f;         // (a bundle has at most 32 groups)
+#pragma unroll
+    for (int e = 0; e < 8; e++) s[0][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NR; i++)
+        if (i < q.rows) {
+            float v[8];
+            values(i, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float d = v[e] - mean[e % G];
+                s[0][e] = __builtin_fmaf(d, d, s[0][e]);
+            }
+        }
+    held_sums<1>(h, p.cg, s, smem, channel, group, one);
+    if (p.stats != nullptr && mine < h.groups) {
+        const int at = group_of(p, q.c0) + mine;
+        if (at < p.groups) p.stats[(long long)q.n * p.groups + at] = float2{mean_out, reciprocal_root(group[mine] * inv + p.eps)};
+    }
+    float r[G];
+#pragma unroll
+    for (int e = 0; e < G; e++) r[e] = reciprocal_root(group[g[e]] * inv + p.eps);
+#pragma unroll
+    for (int e = 0; e < 8; e++) w[e] *= r[e % G];
+    with_act(p.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+#pragma unroll
+        for (int i = 0; i < NR; i++)
+            if (i < q.rows) {
+                float v[8];
+                values(i, v);
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] = activate<DT>(__builtin_fmaf(v[e] - mean[e % G], w[e], b[e]), ACT);
+                store8<DT>(p.out + ((first + (long long)i * h.slots) * p.ldout + q.c) * B, q.left, v);
+            }
+    });
+}
+
+template <int DT, int NR, int MODE, bool ONE>
+__global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kernel(GroupArgs p, HeldShape h)
+{
+    constexpr int B = item_bytes<DT>(), G = ONE ? 1 : 8;
+    extern __shared__ float smem[];
+    const HeldPlace q = held_place(p, h);
+    float *const channel = smem + 16 * h.threads, *const group = channel + 2 * h.lanes * 8;
+    const long long first = (long long)q.n * p.pixels + q.slot;
+    Run<DT> rx[NR], rd[NR];
+#pragma unroll
+    for (int i = 0; i < NR; i++)
+        if (q.rows > 0) {
+            const long long row = first + (long long)min(i, q.rows - 1) * h.slots;
+            rx[i] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, q.left, p.C);
+            rd[i] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, q.left, p.C);
+        }
+    float w[8], b[8], mean[G], r[G];
+    int g[G];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const int c = min(q.c + e, p.C - 1);
+        w[e] = p.w != nullptr ? p.w[c] : 1.f;
+        b[e] = p.b != nullptr ? p.b[c] : 0.f;
+        if (e < G) {
+            const float2 st = p.stats[(long long)q.n * p.groups + group_of(p, c)];
+            mean[e % G] = st.x;
+            r[e % G] = st.y;
+            g[e % G] = min(group_of(p, max(c - q.c0, 0)), h.groups - 1);
+        }
+    }
+    // t and xh of row i
+    const auto gradient = [&](int i, auto act, float (&t)[8], float (&xh)[8]) {
+        constexpr int ACT = decltype(act)::value;
+        float x[8], d[8];
+        row_values<DT, MODE>(rx[i], q.c, q.left, p.C, x);
+        row_values<DT, MODE>(rd[i], q.c, q.left, p.C, d);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            xh[e] = (x[e] - mean[e % G]) * r[e % G];
+            t[e] = gradient_before<DT>(d[e], xh[e], x[e], mean[e % G], r[e % G], w[e], b[e], ACT);
+        }
+    };
+    float s[2][8] = {};
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < NR; i++)
+            if (i < q.rows) {
+                float t[8], xh[8];
+                gradient(i, act, t, xh);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    s[0][e] += t[e];
+                    s[1][e] = __builtin_fmaf(t[e], xh[e], s[1][e]);
+                }
+            }
+    });
+    held_sums<2>(h, p.cg, s, smem, channel, group, [&](int c) { return p.w != nullptr ? p.w[min(q.c0 + c, p.C - 1)] : 1.f; });
+    for (int c = threadIdx.x; c < h.width && q.c0 + c < p.C; c += h.threads) {
+        const float s0 = channel[c], s1 = channel[h.lanes * 8 + c];
+        if (p.images > 1) {
+            p.total[(long long)q.n * p.C + q.c0 + c] = float2{s0, s1};
+        } else {
+            if (p.dw != nullptr) p.dw[q.c0 + c] = s1;
+            if (p.db != nullptr) p.db[q.c0 + c] = s0;
+        }
+    }
+    const float inv = 1.f / ((float)p.pixels * (float)p.cg);
+    float A[G], K[G];
+#pragma unroll
+    for (int e = 0; e < G; e++) {
+        A[e] = group[g[e]] * inv;
+        K[e] = group[h.groups + g[e]] * inv;
+    }
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < NR; i++)
+            if (i < q.rows) {
+                float t[8], xh[8];
+                gradient(i, act, t, xh);
+#pragma unroll
+                for (int e = 0; e < 8; e++) t[e] = r[e % G] * __builtin_fmaf(-xh[e], K[e % G], __builtin_fmaf(w[e], t[e], -A[e % G]));
+                store8<DT>(p.out + ((first + (long long)i * h.slots) * p.ldout + q.c) * B, q.left, t);
+            }
+    });
+}
+
+template <auto KERNEL>
+int launch_held_kernel(const GroupArgs &a, const HeldShape &h, size_t lds, hipStream_t s)
+{
+    const int st = allow_lds<KERNEL>(lds);
+    if (st != SS_OK) return st;
+    KERNEL<<<dim3((unsigned)(a.images * h.bundles)), dim3(h.threads), lds, s>>>(a, h);
+    return launched();
+}
+
+template <int DT>
+int launch_held(const GroupArgs &a, const HeldShape &h, bool backward, hipStream_t s)
+{
+    const size_t lds = held_lds(h, backward ? 2 : 1);
+    const auto rows = [&](auto nr) {
+        constexpr int NR = decltype(nr)::value;
+        const auto pick = [&](auto md, auto one) -> int {
+            constexpr int MODE = decltype(md)::value;
+            constexpr bool ONE = decltype(one)::value;
+            return backward ? launch_held_kernel<group_held_grad_kernel<DT, NR, MODE, ONE>>(a, h, lds, s) : launch_held_kernel<group_held_kernel<DT, NR, MODE, ONE>>(a, h, lds, s);
+        };
+        if (a.C % 8 || h.width % 8) return pick(Mode<CUT>{}, std::false_type{});
+        return a.cg % 8 ? pick(Mode<EVEN>{}, std::false_type{}) : pick(Mode<EVEN>{}, std::true_type{});
+    };
+    if (h.rows <= 1) return rows(Mode<1>{});
+    if (h.rows <= 2) return rows(Mode<2>{});
+    if (h.rows <= 4) return rows(Mode<4>{});
+    if (h.rows <= 8) return rows(Mode<8>{});
+    if constexpr (held_most_rows(DT) >= 16) return rows(Mode<16>{});
+    return SS_ERR_UNSUPPORTED;
+}
+
+#define SS_HELD_LAUNCHES(X, DT) X template int launch_held<DT>(const GroupArgs &, const HeldShape &, bool, hipStream_t);
+
+}  // namespace ss
+
+#endif

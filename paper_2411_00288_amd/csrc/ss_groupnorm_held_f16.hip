@@ -1,0 +1,6 @@
+// Group norm kernels that hold their data: SS_F16.
+#include "ss_groupnorm_held.h"
+
+namespace ss {
+SS_HELD_LAUNCHES(, SS_F16)
+}

@@ -238,6 +238,16 @@ __global__ __launch_bounds__(kGroupThreads) void group_apply_kernel(GroupArgs p)
 // ---------------------------------------------------------------------------------------------
 // gradient
 // ---------------------------------------------------------------------------------------------
+// t, the gradient before the activation, from dy.
+template <int DT>
+__device__ __forceinline__ float gradient_before(float dy, float xh, float x, float mean, float r, float w, float b, int act)
+{
+    if (act == SS_ACT_NONE) return dy;
+    const float z = __builtin_fmaf(xh, w, b);
+    if (act == SS_ACT_RELU) return above_corner(z, x, mean, r, w, b) ? dy : z != z ? z : 0.f;
+    return dy * slope<DT>(z, act);
+}
+
 // t and xh of eight channels of a pixel.
 template <int DT>
 __device__ __forceinline__ void group_gradient(const Channels &k, const float (&x)[8], const float (&dy)[8], int act, float (&t)[8], float (&xh)[8])
@@ -245,13 +255,7 @@ __device__ __forceinline__ void group_gradient(const Channels &k, const float (&
 #pragma unroll
     for (int e = 0; e < 8; e++) {
         xh[e] = (x[e] - k.mean[e]) * k.r[e];
-        t[e] = dy[e];
-        if (act == SS_ACT_NONE) continue;
-        const float z = __builtin_fmaf(xh[e], k.w[e], k.b[e]);
-        if (act == SS_ACT_RELU)
-            t[e] = above_corner(z, x[e], k.mean[e], k.r[e], k.w[e], k.b[e]) ? dy[e] : z != z ? z : 0.f;
-        else
-            t[e] *= slope<DT>(z, act);
+        t[e] = gradient_before<DT>(dy[e], xh[e], x[e], k.mean[e], k.r[e], k.w[e], k.b[e], act);
     }
 }
 

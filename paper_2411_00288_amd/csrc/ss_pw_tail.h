@@ -2,7 +2,7 @@
 #ifndef SS_PW_TAIL_H_
 #define SS_PW_TAIL_H_
 #include "ss_mx4.h"
-#include <atomic>
+#include "ss_lds.h"
 #include <type_traits>
 
 namespace ss {
@@ -192,22 +192,6 @@ __device__ __forceinline__ void wait_loads()
 {
     __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
 }
-// A kernel's shared memory may pass 64 KB once its limit is raised, which is done at its first such launch on a device.
-template <auto KERNEL>
-int allow_lds(size_t bytes)
-{
-    if (bytes <= 65536) return SS_OK;
-    static std::atomic<unsigned long long> done{0};
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return SS_ERR_HIP;
-    const unsigned long long bit = 1ull << (dev & 63);
-    if (dev >= 64 || !(done.load(std::memory_order_acquire) & bit)) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return SS_ERR_HIP;
-        if (dev < 64) done.fetch_or(bit, std::memory_order_release);
-    }
-    return SS_OK;
-}
-
 template <auto KERNEL>
 int launch_lds(long long blocks, int threads, size_t bytes, hipStream_t s, const PwArgs &a, const PwRowsArgs &r)
 {

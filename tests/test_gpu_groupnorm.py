@@ -80,9 +80,15 @@ def check_forward(x, w, b, groups, kind, y, stats):
     assert ((y.cpu().double().view(n, -1, c) - want).abs() <= tol).all()
 
 
+@pytest.fixture(params=[None, 96], ids=["chosen", "passes"])
+def kernel(request, force_tile):
+    """The library's choice (the kernels that hold an image's groups, for most of these), or the passes over images of any size."""
+    force_tile(request.param)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
-def test_forward(ss, shape, dtype):
+def test_forward(ss, kernel, shape, dtype):
     kind = list(ACTS)[sum(shape) % 4]
     n, h, wd, c, groups = shape
     x, _, w, b = data(sum(shape), (n, h, wd, c), dtype)
@@ -96,7 +102,7 @@ def test_forward(ss, shape, dtype):
 
 @pytest.mark.parametrize("kind", ACTS)
 @pytest.mark.parametrize("dtype", TYPES)
-def test_forward_activations(ss, kind, dtype):
+def test_forward_activations(ss, kernel, kind, dtype):
     x, _, w, b = data(3, (2, 9, 11, 48), dtype)
     w = w * 4
     desc = ss.make_groupnorm_desc(48, 6, CODES[dtype], ACTS[kind], EPS)
@@ -106,7 +112,7 @@ def test_forward_activations(ss, kind, dtype):
 
 
 @pytest.mark.parametrize("pixels", [40, 5000])
-def test_far_from_zero(ss, pixels):
+def test_far_from_zero(ss, kernel, pixels):
     """Values whose mean is a thousand times their deviation: the sum of squares is no difference of large sums."""
     g = torch.Generator().manual_seed(9)
     x = 1000 + torch.randn((2, pixels, 32), generator=g)
@@ -155,7 +161,7 @@ def check_backward(x, dy, w, b, groups, kind, stats, grads):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
-def test_backward(ss, shape, dtype):
+def test_backward(ss, kernel, shape, dtype):
     kind = list(ACTS)[(sum(shape) + 1) % 4]
     n, h, wd, c, groups = shape
     x, dy, w, b = data(sum(shape) + 1, (n, h, wd, c), dtype)
@@ -170,7 +176,7 @@ def test_backward(ss, shape, dtype):
 
 @pytest.mark.parametrize("kind", ACTS)
 @pytest.mark.parametrize("dtype", TYPES)
-def test_backward_activations(ss, kind, dtype):
+def test_backward_activations(ss, kernel, kind, dtype):
     x, dy, w, b = data(4, (2, 9, 11, 48), dtype)
     w = w * 3
     desc = ss.make_groupnorm_desc(48, 6, CODES[dtype], ACTS[kind], EPS)
@@ -180,7 +186,7 @@ def test_backward_activations(ss, kind, dtype):
         check_backward(x, dy, *vectors, 6, kind, stats, grads)
 
 
-def test_corner(ss):
+def test_corner(ss, kernel):
     """The values that a ReLU's corner falls on: those whose sum in 32 bits rounds to the other side."""
     x = torch.randn((1, 64, 64, 8), generator=torch.Generator().manual_seed(8))
     desc = ss.make_groupnorm_desc(8, 2, ss.SS_F32, ss.SS_ACT_RELU, EPS)
@@ -219,7 +225,7 @@ def test_differences(ss):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_views(ss, dtype):
+def test_views(ss, kernel, dtype):
     """Channels of a wider tensor, from any element on; outputs that are the input; what lies beside them stays."""
     wide, dwide, w, b = data(31, (3, 6, 5, 50), dtype)
     wide, dwide, w, b = wide.cuda(), dwide.cuda(), w[:33].cuda(), b[:33].cuda()
@@ -236,7 +242,7 @@ def test_views(ss, dtype):
     assert torch.equal(wide[..., :5], before[..., :5]) and torch.equal(wide[..., 38:], before[..., 38:])
 
 
-def test_streams_and_graphs(ss):
+def test_streams_and_graphs(ss, kernel):
     """Another stream; a captured pass, both ways, replayed with other data between eager calls."""
     x, dy, w, b = (t.cuda() for t in data(41, (2, 20, 20, 64), "bf16"))
     desc = ss.make_groupnorm_desc(64, 8, ss.SS_BF16, ss.SS_ACT_GELU, EPS)
@@ -267,7 +273,7 @@ def test_streams_and_graphs(ss):
             assert torch.equal(one, other)
 
 
-def test_nan_stays_in_its_group(ss):
+def test_nan_stays_in_its_group(ss, kernel):
     x, dy, w, b = data(61, (3, 10, 9, 40), "f32")
     x[1, 4, 4, 13] = float("nan")
     x[2, 0, 0, 39] = float("inf")
