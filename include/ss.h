@@ -544,7 +544,7 @@ int ss_pw_f8_q_fwd(const ss_weight_desc *desc, const void *codes, const void *sc
  *     dw[o][c] = sum_r dy[r][o] x[r][c]          db[o] = sum_r dy[r][o]
  * from 16-bit operands as they are, whatever the type of the forward product: the sums are 32 bits wide, which those of 8-bit matrix instructions are not.  A mask
  * is the caller's to apply.
- *   dy [rows][cout], x [rows][cin] of desc->dtype (SS_F16 or SS_BF16, a 1x1 kernel: anything else SS_ERR_UNSUPPORTED), pitches in elements, rows from any element on
+ *   dy [rows][cout], x [rows][cin] of desc->dtype (SS_F16 or SS_BF16, a 1x1 kernel: anything else SS_ERR_UNSUPPORTED), pitches in elements, at most 2^23, rows from any element on
  *   dw [cout][cin]; db [cout] or NULL
  *   workspace ss_pw_wgrad_workspace_bytes bytes, 16-byte aligned, not initialised; not shared by calls that may run at the same time
  * Sums are made in a fixed order: the same call gives the same bits.  rows from 0 (zeros) to 2^31 - 1.  Asynchronous on `stream`.
