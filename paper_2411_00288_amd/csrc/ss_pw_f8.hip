@@ -178,17 +178,181 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_f8_tile_kernel(
         pw_store<DT, MI, NI, false, true, KEPT>(p, acc, mt0, row0 + px0, lane);
 }
 
-// Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
-// the reduction, a block of 128 each in turn, and join their sums in LDS.
-template <int DT, int NW, int NI>
-__global__ __launch_bounds__(NW * 64) void pw_f8_few_kernel(PwArgs p, PwRowsArgs)
+// 16-bit input rows of a workgroup, quantised into LDS.  Piece b (16 channels) of row r stands at ((b * pad + r) * 16): the lanes of a fragment read consecutive
+// pieces.  WIDE: K is at least 8.  The scale of block k is byte k % 4 of word (k / 4) * pad + r.  Pieces 0 .. 4 Ks - 1, rows 0 .. count - 1; what is past the
+// matrix is zero.
+template <int DT, int THREADS, int U, bool WIDE>
+__device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row0, int rows, int count, int K, int Ks, int pad, uint8_t *codes_s, uint8_t *scales_s)
+{
+    const int runs = (Ks + 1) / 2 * 16, total = count * runs;
+    const uint16_t *const x = r.x + row0 * r.ldx;
+    int row = (int)(((unsigned long long)threadIdx.x * r.mul) >> r.sh), run = (int)threadIdx.x - row * runs;
+    for (int base = 0; base < total; base += THREADS * U) {
+        Run<DT> raw[U];
+        int rw[U], rn[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            rw[u] = row;
+            rn[u] = run;
+            if (base + u * THREADS < total) {              // uniform
+                if constexpr (WIDE)
+                    raw[u] = load_wide<DT, false>(x + (long long)min(row, rows - 1) * (int)r.ldx, run * 8, K);
+                else
+                    raw[u] = load_run<DT>(x + (long long)row * (int)r.ldx + run * 8, row < rows ? K - run * 8 : 0);
+            }
+            row += r.step_row;
+            run += r.step_run;
+            if (run >= runs) {
+                run -= runs;
+                row++;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (base + u * THREADS >= total) break;        // uniform
+            const int b = rn[u] / 2, k = rn[u] / 16;
+            if constexpr (WIDE) place_wide<DT>(raw[u], rn[u] * 8, K, rw[u] < rows);
+            const uint32_t byte = f8_scale(row16_max(magnitude<DT>(raw[u])));
+            const u32x2 c = f8_codes<DT>(raw[u], byte);
+            if (rw[u] >= count) continue;
+            if (b < 4 * Ks) *reinterpret_cast<u32x2 *>(codes_s + (__umul24(b, pad) + rw[u]) * 16 + rn[u] % 2 * 8) = c;
+            if (rn[u] % 16 == 0) scales_s[(__umul24(k / 4, pad) + rw[u]) * 4 + k % 4] = (uint8_t)byte;
+        }
+    }
+}
+
+// Layers on 16-bit input whose reduction fits LDS: a workgroup quantises its 32 NT rows once, and its waves take units of output channels and 32 rows in turn (the
+// units of the same channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels, unless there are few
+// rows: then several workgroups share the channels of one's rows.  The next weights are on their way from the L2 while the current ones are multiplied or, with a
+// reduction of one block (SHORT), while the sums are finished.  One block: units of 64 channels; longer: units of 32.
+template <int DT, int NT, bool SHORT, bool WIDE, int THREADS>
+__global__ __launch_bounds__(THREADS, SHORT && NT == 1 ? 3 : 4) void pw_f8_rows_kernel(PwArgs p, PwRowsArgs r)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    constexpr int PX = 32 * NT, PAD = PX + 1, WAVES = THREADS / 64, MI = SHORT ? 2 : 1;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int Ks = (p.K + 63) / 64, KB = SHORT ? 1 : (p.K + 127) / 128, Kq = (KB + 3) / 4, Mt = (p.cout + 31) / 32;
+    const unsigned part = blockIdx.x / r.blocks;
+    const int first = (int)part * r.units * NT, units = min((Mt + MI - 1) / MI, ((int)part + 1) * r.units) * NT;
+    const long long row0 = (long long)(blockIdx.x - part * r.blocks) * PX;
+    uint8_t *const codes_s = smem, *const scales_s = smem + 4 * Ks * PAD * 16;
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w), 0, (int)((unsigned)Mt * Ks * 2048u), 0x00020000);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales), 0, Mt * Kq * 128, 0x00020000);
+    u32x4 wa[2][MI][2], wn[2][MI][2];
+    uint32_t sa[MI], sn[MI];
+    auto fetch = [&](int mt, int q, u32x4 (&w)[2][MI][2], uint32_t (&sc)[MI]) {
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const int m = min(mt + i, Mt - 1);
+            sc[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ra, (lane % 32) * 4, (m * Kq + q / 4) * 128, 0) >> (8 * (q % 4));
+#pragma unroll
+            for (int s = 0; s < 2; s++)
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+                    w[s][i][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, ((m * Ks + min(q * 2 + s, Ks - 1)) * 2 + h) * 1024, 0));
+        }
+    };
+    auto multiply = [&](int at, int q, f32x16 (&acc)[MI][1]) {
+        const uint32_t sb[1] = {*reinterpret_cast<const uint32_t *>(scales_s + ((q / 4) * PAD + at + lane % 32) * 4) >> (8 * (q % 4))};
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            if (q * 2 + s < Ks) {
+                u32x4 xb[1][2];
+#pragma unroll
+                for (int h = 0; h < 2; h++) xb[0][h] = *reinterpret_cast<const u32x4 *>(codes_s + ((8 * q + 4 * s + 2 * half + h) * PAD + at + lane % 32) * 16);
+                step_f8<0, 0>(wa[s], xb, acc, sa, sb);
+            }
+        }
+    };
+    // The sums start from the bias, which waits in LDS: a load behind the last unit's stores would wait for those, too.
+    float *const bias_s = reinterpret_cast<float *>(scales_s + (Kq * PAD * 4 + 15) / 16 * 16);
+    auto start = [&](int mt, f32x16 (&acc)[MI][1]) {
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(bias_s + min(mt + i, Mt - 1) * 32 + 8 * g + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; e++) acc[i][0][4 * g + e] = b[e];
+            }
+    };
+    for (int o = threadIdx.x; o < Mt * 32; o += THREADS) bias_s[o] = p.bias != nullptr && o < p.cout ? p.bias[o] : 0.f;
+    if constexpr (SHORT)
+        fetch(min((first + wave) / NT * MI, Mt - 1), 0, wa, sa);
+    else
+        fetch(min((first + wave) / NT * MI, Mt - 1), 0, wn, sn);
+    quantise_rows<DT, THREADS, SHORT ? 4 : 8, WIDE>(r, row0, (int)min((long long)PX, p.P - row0), PX, p.K, Ks, PAD, codes_s, scales_s);
+    __syncthreads();
+    // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
+    // through the loop for it, so that tiles with fewer stores would have every wave wait for the stores of the others.
+    __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt 0, the first weights: so that the loop is entered with none on their way)
+    const auto walk = [&](auto whole, auto out, auto with) {
+        constexpr bool ALL = decltype(whole)::value;
+        constexpr int OUT = decltype(out)::value, WITH = decltype(with)::value;
+        f32x16 acc[MI][1];
+        int unit = first + wave, q = 0;
+        start(unit / NT * MI, acc);
+        while (unit < units) {
+            const int mt = unit / NT * MI, at = unit % NT * 32;
+            if constexpr (SHORT) {
+                multiply(at, 0, acc);
+                unit += WAVES;
+                fetch(min(unit / NT * MI, Mt - 1), 0, wa, sa);
+                pw_store<DT, MI, 1, ALL, false, OUT, WITH>(p, acc, mt, row0 + at, lane);
+                __builtin_amdgcn_sched_barrier(0);
+                start(unit / NT * MI, acc);
+            } else {
+#pragma unroll
+                for (int i = 0; i < MI; i++) {
+                    sa[i] = sn[i];
+#pragma unroll
+                    for (int s = 0; s < 2; s++)
+#pragma unroll
+                        for (int h = 0; h < 2; h++) wa[s][i][h] = wn[s][i][h];
+                }
+                const bool done = q + 1 == KB;
+                const int next = done ? unit + WAVES : unit, nq = done ? 0 : q + 1;
+                fetch(min(next / NT * MI, Mt - 1), nq, wn, sn);
+                multiply(at, q, acc);
+                if (done) {
+                    pw_store<DT, MI, 1, ALL, false, OUT, WITH>(p, acc, mt, row0 + at, lane);
+                    start(next / NT * MI, acc);
+                }
+                unit = next;
+                q = nq;
+            }
+        }
+    };
+    // (a residual takes registers: in a loop that looks for one the others' sums are spilled, 401408 x 96 -> 384 in 4 bits 78 -> 86 us)
+    const auto ways = [&](auto with) {
+        if (p.cout % 64 != 0 || row0 + PX > p.P)
+            walk(std::false_type{}, Int<KEPT>{}, with);
+        else if (!p.stream)
+            walk(std::true_type{}, Int<KEPT>{}, with);
+        else if (!SHORT || p.act == SS_ACT_GELU)
+            walk(std::true_type{}, Int<PAST>{}, with);
+        else if constexpr (SHORT)
+            walk(std::true_type{}, Int<LINES>{}, with);
+    };
+    if (p.residual == nullptr)
+        ways(Int<NO_RES>{});
+    else
+        ways(Int<RES>{});
+}
+
+// Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share
+// the reduction, a block of 128 each in turn, and join their sums in LDS.  QUANT: the rows are quantised into LDS first, by all threads, while the first
+// weights are on their way.
+template <int DT, int NW, int NI, bool QUANT, bool WIDE>
+__global__ __launch_bounds__(NW * 64) void pw_f8_few_kernel(PwArgs p, PwRowsArgs r)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    static_assert(!QUANT || NI == 1, "rows in LDS");
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const int Ks = (p.K + 63) / 64, KB = (p.K + 127) / 128, S = (KB + 3) / 4 * 4, Kq = S / 4, Mt = (p.cout + 31) / 32;
     const int mt = blockIdx.x % Mt;
     const long long row0 = (long long)(blockIdx.x / Mt) * (32 * NI);
-    const int rows = (int)min((long long)(32 * NI), p.P - row0);
+    const int rows = (int)min((long long)(32 * NI), p.P - row0), pad = rows | 1;
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w) + (size_t)mt * Ks * 2048, 0, Ks * 2048, 0x00020000);
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w_scales) + (size_t)mt * Kq * 128, 0, Kq * 128, 0x00020000);
     // (the offsets are the lanes' own: only those are held against the buffer's end, which a step past the last reads zeros behind)
@@ -203,14 +367,20 @@ __global__ __launch_bounds__(NW * 64) void pw_f8_few_kernel(PwArgs p, PwRowsArgs
     uint32_t word_a, word_n;
     weights(wave, wa, word_a);
     weights(wave + NW, wn, word_n);
+    uint8_t *const scales_s = smem + 4 * Ks * pad * 16;
+    if constexpr (QUANT) {
+        quantise_rows<DT, NW * 64, 8, WIDE>(r, row0, rows, rows, p.K, Ks, pad, smem, scales_s);
+        __syncthreads();
+    }
     f32x16 acc[1][NI] = {};
     const uint8_t *px[NI], *ps[NI];
 #pragma unroll
     for (int j = 0; j < NI; j++) {
-        const long long at = row0 + min(j * 32 + lane % 32, rows - 1);         // (lanes past the last row repeat it)
-        px[j] = p.codes + at * (Ks * 64) + half * 32;
-        ps[j] = p.scales + at * S;
+        const int row = min(j * 32 + lane % 32, rows - 1);                     // (lanes past the last row repeat it)
+        px[j] = QUANT ? smem + (2 * half * pad + row) * 16 : p.codes + (row0 + row) * (Ks * 64) + half * 32;
+        ps[j] = QUANT ? scales_s + row * 4 : p.scales + (row0 + row) * S;
     }
+    const int step_at = QUANT ? 4 * pad * 16 : 64, piece_at = QUANT ? pad * 16 : 16, word_at = QUANT ? pad * 4 : 4;
     for (int q = wave; q < KB; q += NW) {
         u32x4 xb[2][NI][2];
         uint32_t sa[1], sb[NI];
@@ -218,11 +388,11 @@ __global__ __launch_bounds__(NW * 64) void pw_f8_few_kernel(PwArgs p, PwRowsArgs
         sa[0] = word_a >> turn;
 #pragma unroll
         for (int j = 0; j < NI; j++) {
-            sb[j] = *reinterpret_cast<const uint32_t *>(ps[j] + q / 4 * 4) >> turn;
+            sb[j] = *reinterpret_cast<const uint32_t *>(ps[j] + q / 4 * word_at) >> turn;
 #pragma unroll
             for (int s = 0; s < 2; s++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) xb[s][j][h] = *reinterpret_cast<const u32x4 *>(px[j] + min(2 * q + s, Ks - 1) * 64 + h * 16);
+                for (int h = 0; h < 2; h++) xb[s][j][h] = *reinterpret_cast<const u32x4 *>(px[j] + min(2 * q + s, Ks - 1) * step_at + h * piece_at);
         }
         // (a step past the last has zero weights, and the last step's pixels again)
         step_f8<0, 0>(wa[0], xb[0], acc, sa, sb);
@@ -309,6 +479,13 @@ F8Kernel codes_kernel(const F8Dims &t, long long rows)
     return choose_f8_codes(t, rows, std::max(compute_units(), 1));
 }
 
+F8Kernel kernel16(const F8Dims &t, long long rows)
+{
+    const int forced = forced_tile();
+    if (forced >= F816_FEW && forced <= F816_CODES && f8_fits16(t, rows, (F8Kernel)forced)) return (F8Kernel)forced;
+    return choose_f8_16(t, rows, std::max(compute_units(), 1));
+}
+
 template <int DT, int MI, int NI, int WM, int OUT>
 int launch_tile(const PwArgs &a, const F8Dims &t, hipStream_t s)
 {
@@ -320,7 +497,7 @@ int launch_tile(const PwArgs &a, const F8Dims &t, hipStream_t s)
 }
 
 template <int DT>
-int product_codes(const PwArgs &a, const F8Dims &t, hipStream_t s)
+int product_codes(const PwArgs &a, const F8Dims &t, F8Kernel kernel, hipStream_t s)
 {
     const auto tile = [&](auto mi, auto ni, auto wm) -> int {
         constexpr int MI = decltype(mi)::value, NI = decltype(ni)::value, WM = decltype(wm)::value;
@@ -330,12 +507,12 @@ int product_codes(const PwArgs &a, const F8Dims &t, hipStream_t s)
         constexpr int NI = decltype(ni)::value;
         const long long blocks = ((long long)a.P + 32 * NI - 1) / (32 * NI) * t.Mt;
         if (blocks > 0x3FFFFFll) return SS_ERR_UNSUPPORTED;
-        if (NI == 2 || t.KB > 8) return launch_lds<pw_f8_few_kernel<DT, 16, NI>>(blocks, 1024, f8_few_lds(16), s, a, PwRowsArgs{});
+        if (NI == 2 || t.KB > 8) return launch_lds<pw_f8_few_kernel<DT, 16, NI, false, false>>(blocks, 1024, f8_few_lds(t, 16, 0), s, a, PwRowsArgs{});
         if constexpr (NI == 1)              // (two tiles of rows are for long reductions)
-            return t.KB > 4 ? launch_lds<pw_f8_few_kernel<DT, 8, NI>>(blocks, 512, f8_few_lds(8), s, a, PwRowsArgs{})
-                            : launch_lds<pw_f8_few_kernel<DT, 4, NI>>(blocks, 256, f8_few_lds(4), s, a, PwRowsArgs{});
+            return t.KB > 4 ? launch_lds<pw_f8_few_kernel<DT, 8, NI, false, false>>(blocks, 512, f8_few_lds(t, 8, 0), s, a, PwRowsArgs{})
+                            : launch_lds<pw_f8_few_kernel<DT, 4, NI, false, false>>(blocks, 256, f8_few_lds(t, 4, 0), s, a, PwRowsArgs{});
     };
-    switch (codes_kernel(t, a.P)) {
+    switch (kernel) {
         case F8_TILE_64: return tile(Int<1>{}, Int<1>{}, Int<2>{});
         case F8_TILE_128: return tile(Int<1>{}, Int<4>{}, Int<4>{});
         case F8_TILE_256: return tile(Int<2>{}, Int<8>{}, Int<4>{});
@@ -344,22 +521,67 @@ int product_codes(const PwArgs &a, const F8Dims &t, hipStream_t s)
     }
 }
 
-// The layer in pieces of rows, so that no launch has 2^32 threads: tiles of 64 x 64 have 4 threads to the row and 64 channels, few-row kernels 32 to the row and 32 channels.
-int product(const ss_weight_desc *d, const PwArgs &all, const uint8_t *codes, const uint8_t *scales, hipStream_t s)
+template <int DT>
+int product16(const PwArgs &a, const F8Dims &t, F8Kernel kernel, const void *x, int64_t ldx, hipStream_t s)
 {
-    const F8Dims t = f8_dims(d->cout, d->cin);
-    const long long piece = piece_rows(4ll * ((t.Mt + 1) / 2));
+    PwRowsArgs r{};
+    r.x = static_cast<const uint16_t *>(x);
+    r.ldx = ldx;
+    const int runs = t.KB * 16;
+    fast_div_setup((unsigned)runs, &r.mul, &r.sh);
+    const auto go = [&](auto wide) -> int {
+        constexpr bool WIDE = decltype(wide)::value;
+        const auto few = [&](auto nw) -> int {
+            constexpr int NW = decltype(nw)::value;
+            r.step_row = NW * 64 / runs;
+            r.step_run = NW * 64 % runs;
+            return launch_lds<pw_f8_few_kernel<DT, NW, 1, true, WIDE>>(t.Mt, NW * 64, f8_few_lds(t, NW, a.P), s, a, r);
+        };
+        const auto rows = [&](auto nt, auto brief, auto threads) -> int {
+            constexpr int NT = decltype(nt)::value, THREADS = decltype(threads)::value;
+            r.step_row = THREADS / runs;
+            r.step_run = THREADS % runs;
+            const long long blocks = ((long long)a.P + 32 * NT - 1) / (32 * NT);
+            const int splits = NT == 1 ? f8_rows_splits(t, a.P, std::max(compute_units(), 1)) : 1;
+            r.blocks = (unsigned)blocks;
+            r.units = ((decltype(brief)::value ? (t.Mt + 1) / 2 : t.Mt) + splits - 1) / splits;
+            return launch_lds<pw_f8_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, f8_rows_lds(t, 32 * NT), s, a, r);
+        };
+        if (kernel == F816_FEW) {
+            const int waves = f8_few16_waves(t, a.P, a.K);
+            return waves == 16 ? few(Int<16>{}) : waves == 8 ? few(Int<8>{}) : few(Int<4>{});
+        }
+        if (kernel == F816_ROWS_128) return rows(Int<4>{}, std::true_type{}, Int<256>{});
+        if (t.KB == 1) return rows(Int<1>{}, std::true_type{}, Int<256>{});
+        return f8_rows_waves(t, a.P, std::max(compute_units(), 1)) == 4 ? rows(Int<1>{}, std::false_type{}, Int<256>{}) : rows(Int<1>{}, std::false_type{}, Int<512>{});
+    };
+    return a.K >= 8 ? go(std::true_type{}) : go(std::false_type{});
+}
+
+// The layer in pieces of `piece` rows, so that no launch has 2^32 threads: launch(arguments, first row).
+template <typename F>
+int in_pieces(const PwArgs &all, long long piece, F &&launch)
+{
     for (long long at = 0; at < all.P; at += piece) {
         PwArgs a = all;
         a.P = (int)std::min(piece, all.P - at);
         a.y += at * a.ldy;
         if (a.residual != nullptr) a.residual += at * a.ldr;
-        a.codes = codes + at * t.P;
-        a.scales = scales + at * t.S;
-        const int st = d->dtype == SS_F16 ? product_codes<SS_F16>(a, t, s) : product_codes<SS_BF16>(a, t, s);
+        const int st = launch(a, at);
         if (st != SS_OK) return st;
     }
     return SS_OK;
+}
+
+int product(const ss_weight_desc *d, const PwArgs &all, const uint8_t *codes, const uint8_t *scales, hipStream_t s)
+{
+    const F8Dims t = f8_dims(d->cout, d->cin);
+    return in_pieces(all, piece_rows(4ll * ((t.Mt + 1) / 2)), [&](PwArgs &a, long long at) {       // (tiles of 64 x 64 have the most threads)
+        a.codes = codes + at * t.P;
+        a.scales = scales + at * t.S;
+        const F8Kernel kernel = codes_kernel(t, a.P);
+        return d->dtype == SS_F16 ? product_codes<SS_F16>(a, t, kernel, s) : product_codes<SS_BF16>(a, t, kernel, s);
+    });
 }
 
 }  // namespace
@@ -385,7 +607,7 @@ extern "C" int ss_pw_f8_workspace_bytes(const ss_weight_desc *desc, int64_t rows
     if (!bytes || rows < 0) return SS_ERR_INVALID_ARG;
     if (rows > INT32_MAX) return SS_ERR_UNSUPPORTED;
     const F8Dims t = f8_dims(desc->cout, desc->cin);
-    *bytes = rows > 0 ? to256((size_t)rows * t.P) + (size_t)rows * t.S : 0;
+    *bytes = rows > 0 && kernel16(t, rows) == F816_CODES ? to256((size_t)rows * t.P) + (size_t)rows * t.S : 0;
     return SS_OK;
 }
 
@@ -398,14 +620,19 @@ extern "C" int ss_pw_f8_fwd(const ss_weight_desc *desc, const void *x, int64_t r
     if (ldx > INT32_MAX) return SS_ERR_UNSUPPORTED;
     if (rows == 0) return SS_OK;
     if (!x || !aligned(x, 2)) return SS_ERR_INVALID_ARG;
-    size_t need = 0;
-    st = ss_pw_f8_workspace_bytes(desc, rows, &need);
-    if (st != SS_OK) return st;
-    if (need > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < need)) return SS_ERR_WORKSPACE;
     const F8Dims t = f8_dims(desc->cout, desc->cin);
+    const F8Kernel kernel = kernel16(t, rows);
+    const size_t codes_bytes = to256((size_t)rows * t.P);
+    if (kernel == F816_CODES && (!workspace || !aligned(workspace, 16) || ws_bytes < codes_bytes + (size_t)rows * t.S)) return SS_ERR_WORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    uint8_t *codes = static_cast<uint8_t *>(workspace), *scales = codes + to256((size_t)rows * t.P);
+    const PwArgs a = pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy);
+    if (kernel != F816_CODES)
+        return in_pieces(a, piece_rows(16), [&](const PwArgs &part, long long at) {                // (eight waves to 32 rows)
+            const void *const first = static_cast<const uint16_t *>(x) + at * ldx;
+            return desc->dtype == SS_F16 ? product16<SS_F16>(part, t, kernel, first, ldx, s) : product16<SS_BF16>(part, t, kernel, first, ldx, s);
+        });
+    uint8_t *codes = static_cast<uint8_t *>(workspace), *scales = codes + codes_bytes;
     st = f8_quantize(x, rows, desc->cin, ldx, desc->dtype, codes, scales, s);
     if (st != SS_OK) return st;
-    return product(desc, pw_args(desc, rows, packed, bias, residual, ldr, act, y, ldy), codes, scales, s);
+    return product(desc, a, codes, scales, s);
 }

@@ -294,9 +294,9 @@ __global__ __launch_bounds__(THREADS, 4) void pw_mx4_rows_kernel(PwArgs p, PwRow
     // Whole tiles have a loop of their own: a load is waited for by the number of memory instructions behind it, and the compiler takes the least of any way
     // through the loop for it, so that tiles with fewer stores had every wave wait for the stores of the others (401408 x 96 -> 384: 126 -> 95 us, then).
     __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt 0, the first weights: so that the loop is entered with none on their way)
-    const auto walk = [&](auto whole, auto out) {
+    const auto walk = [&](auto whole, auto out, auto with) {
         constexpr bool ALL = decltype(whole)::value;
-        constexpr int OUT = decltype(out)::value;
+        constexpr int OUT = decltype(out)::value, WITH = decltype(with)::value;
         f32x16 acc[MI][1];
         int unit = first + wave, q = 0;
         start(unit / NT * MI, acc);
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(THREADS, 4) void pw_mx4_rows_kernel(PwArgs p, PwRow
                 multiply(at, 0, acc);
                 unit += WAVES;
                 fetch(min(unit / NT * MI, Mt - 1), 0, wa, sa);
-                pw_store<DT, MI, 1, ALL, false, OUT>(p, acc, mt, row0 + at, lane);
+                pw_store<DT, MI, 1, ALL, false, OUT, WITH>(p, acc, mt, row0 + at, lane);
                 __builtin_amdgcn_sched_barrier(0);
                 start(unit / NT * MI, acc);
             } else {
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(THREADS, 4) void pw_mx4_rows_kernel(PwArgs p, PwRow
                 fetch(min(next / NT * MI, Mt - 1), nq, wn, sn);
                 multiply(at, q, acc);
                 if (done) {
-                    pw_store<DT, MI, 1, ALL, false, OUT>(p, acc, mt, row0 + at, lane);
+                    pw_store<DT, MI, 1, ALL, false, OUT, WITH>(p, acc, mt, row0 + at, lane);
                     start(next / NT * MI, acc);
                 }
                 unit = next;
@@ -329,14 +329,21 @@ __global__ __launch_bounds__(THREADS, 4) void pw_mx4_rows_kernel(PwArgs p, PwRow
             }
         }
     };
-    if (p.cout % 64 != 0 || row0 + PX > p.P)
-        walk(std::false_type{}, Int<KEPT>{});
-    else if (!p.stream)
-        walk(std::true_type{}, Int<KEPT>{});
-    else if (!SHORT || p.act == SS_ACT_GELU)
-        walk(std::true_type{}, Int<PAST>{});
-    else if constexpr (SHORT)
-        walk(std::true_type{}, Int<LINES>{});
+    // (a residual takes registers: in a loop that looks for one the others' sums are spilled, 401408 x 96 -> 384 in 4 bits 78 -> 86 us)
+    const auto ways = [&](auto with) {
+        if (p.cout % 64 != 0 || row0 + PX > p.P)
+            walk(std::false_type{}, Int<KEPT>{}, with);
+        else if (!p.stream)
+            walk(std::true_type{}, Int<KEPT>{}, with);
+        else if (!SHORT || p.act == SS_ACT_GELU)
+            walk(std::true_type{}, Int<PAST>{}, with);
+        else if constexpr (SHORT)
+            walk(std::true_type{}, Int<LINES>{}, with);
+    };
+    if (p.residual == nullptr)
+        ways(Int<NO_RES>{});
+    else
+        ways(Int<RES>{});
 }
 
 // Few rows: bound by reading the weights once, or by a memory latency or two.  A workgroup makes 32 output channels of 32 NI rows; its NW waves share

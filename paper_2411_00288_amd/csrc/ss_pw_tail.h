@@ -49,33 +49,60 @@ __device__ __forceinline__ f32x16 tile_bias(const PwArgs &p, int o0, int half)
     return s;
 }
 
+// Is there a residual, is there none, or do the arguments tell?
+enum { NO_RES = 0, RES = 1, MAYBE_RES = 2 };
+
+// A tile's residual, as its output leaves: 16 bytes of a pixel to the lane.  (As runs of four channels, 8 bytes here and there: 96 -> 384 in 4 bits on 401408 rows 198 us instead of 153.)
+template <bool ALL>
+__device__ __forceinline__ void load_residual(const PwArgs &p, int o0, long long px0, int half, u32x4 (&from)[2])
+{
+    const int o = o0 + (int)(threadIdx.x / 16 % 2) * 16 + half * 8;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        from[q] = u32x4{};
+        const long long at = px0 + 16 * q + threadIdx.x % 16;
+        if (!ALL && at >= p.P) continue;
+        const uint16_t *const src = p.residual + at * p.ldr + o;
+        if (ALL || o + 8 <= p.cout)
+            from[q] = reinterpret_cast<const Vec16 *>(src)->v;
+        else
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (o + e < p.cout) from[q][e / 2] |= (uint32_t)src[e] << (16 * (e % 2));
+    }
+}
+
 // A 32 x 32 tile of sums, finished: residual, activation, rounding.  A lane gets channels lane / 16 % 2 * 16 + half * 8 to 7 more of pixels lane % 16 and 16 more.  ALL: the
 // tile ends within the matrix.  BIAS: it is not in the sums yet.
-template <int DT, bool ALL, bool BIAS>
+template <int DT, bool ALL, bool BIAS, int WITH>
 __device__ __forceinline__ void finish_tile(const PwArgs &p, const f32x16 &acc, const f32x16 &bias, int o0, long long px0, int half, u32x4 (&run)[2])
 {
-    const long long px = px0 + threadIdx.x % 32;
-    const bool in = ALL || px < p.P;
     float z[16];
 #pragma unroll
     for (int v = 0; v < 16; v++) z[v] = BIAS ? acc[v] + bias[v] : acc[v];
-    if (p.residual != nullptr && in) {
+    if (WITH == RES || (WITH == MAYBE_RES && p.residual != nullptr)) {
+        u32x4 from[2];
+        load_residual<ALL>(p, o0, px0, half, from);
+        // (the way back of the stores' trades, to the lane that has the sums)
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-            const int o = o0 + 8 * q + 4 * half;
-            const uint16_t *src = p.residual + px * p.ldr + o;
-            if (ALL || o + 4 <= p.cout) {
-                const u32x2 r = reinterpret_cast<const Half16 *>(src)->v;
-                z[4 * q] += widen<DT>((uint16_t)r[0]);
-                z[4 * q + 1] += widen<DT>((uint16_t)(r[0] >> 16));
-                z[4 * q + 2] += widen<DT>((uint16_t)r[1]);
-                z[4 * q + 3] += widen<DT>((uint16_t)(r[1] >> 16));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (o + e < p.cout) z[4 * q + e] += widen<DT>(src[e]);
-            }
+        for (int e = 0; e < 4; e++) {
+            const uint32_t a = from[0][e], b = from[1][e];
+            const auto s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+            from[0][e] = s[0];
+            from[1][e] = s[1];
         }
+#pragma unroll
+        for (int q = 0; q < 2; q++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const uint32_t a = from[q][e], b = from[q][2 + e];
+                const auto s = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    z[8 * q + 4 * k + 2 * e] += widen<DT>((uint16_t)s[k]);
+                    z[8 * q + 4 * k + 2 * e + 1] += widen<DT>((uint16_t)(s[k] >> 16));
+                }
+            }
     }
     if (p.act == SS_ACT_RELU) {
 #pragma unroll
@@ -163,7 +190,7 @@ __device__ __forceinline__ void store_pair(const PwArgs &p, const u32x4 (&left)[
 }
 
 // A wave's MI x NI tiles, from row tile mt0 and pixel px0 on.  BIAS: it is not in the sums yet.
-template <int DT, int MI, int NI, bool ALL, bool BIAS, int OUT>
+template <int DT, int MI, int NI, bool ALL, bool BIAS, int OUT, int WITH = MAYBE_RES>
 __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI][NI], int mt0, long long px0, int lane)
 {
     constexpr bool lines = MI == 2 && ALL && OUT == LINES;
@@ -179,7 +206,7 @@ __device__ __forceinline__ void pw_store(const PwArgs &p, const f32x16 (&acc)[MI
             __builtin_amdgcn_sched_barrier(0);
             const int o0 = (mt0 + i) * 32;
             if (!ALL && o0 >= p.cout) break;
-            finish_tile<DT, ALL, BIAS>(p, acc[i][j], bias[i], o0, px0 + j * 32, lane / 32, run[i]);
+            finish_tile<DT, ALL, BIAS, WITH>(p, acc[i][j], bias[i], o0, px0 + j * 32, lane / 32, run[i]);
             if constexpr (!lines) store_tile<DT, ALL, OUT != KEPT>(p, run[i], o0, px0 + j * 32, lane);
         }
         if constexpr (lines) store_pair(p, run[0], run[1], mt0 * 32, px0 + j * 32, lane);

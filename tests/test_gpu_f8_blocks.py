@@ -111,7 +111,7 @@ def bound(W, x, out, dtype, K):
     return out.abs() * torch.finfo(dtype).eps / 2 + (K / 64 + 70) * 2.0 ** -23 * size + dropped + 2.0 ** -25
 
 
-KERNELS = {"tile_64": 80, "tile_128": 81, "tile_256": 82, "few_32": 83, "few_64": 84}
+KERNELS = {"tile_64": 80, "tile_128": 81, "tile_256": 82, "few_32": 83, "few_64": 84, "few16": 85, "rows": 86, "rows_128": 87, "codes": 88}
 
 
 @pytest.mark.parametrize("kernel", [None, *KERNELS])
