@@ -116,9 +116,13 @@ HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pix
     const int C = d->channels, cg = C / d->groups, item = d->dtype == SS_F32 ? 4 : 2, most_rows = held_most_rows(d->dtype);
     const long long cus = std::max(compute_units(), 1);
     if (C < 8 || forced_tile() == GROUP_PASSES) return h;
+    // (bundles whose widths are whole runs of eight channels, where the groups allow it)
+    int unit = 8;
+    while (unit > 1 && cg * (unit / 2) % 8 == 0) unit /= 2;
     for (int segment = 64; segment >= 16; segment /= 2) {
         HeldShape s{};
-        s.groups = std::min(d->groups, std::max(1, (segment + cg * item - 1) / (cg * item)));
+        s.groups = std::max(1, (segment + cg * item - 1) / (cg * item));
+        s.groups = std::min(d->groups, (s.groups + unit - 1) / unit * unit);
         s.width = s.groups * cg;
         s.bundles = (d->groups + s.groups - 1) / s.groups;
         s.lanes = (s.width + 7) / 8;
@@ -130,7 +134,7 @@ HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pix
             s.threads = threads;
             s.slots = slots;
             s.rows = (int)rows;
-            if (rows <= 4) break;                           // (fewer rows to the thread gain nothing)
+            if (rows <= 4 || images * s.bundles >= cus) break;
         }
         if (s.threads == 0 || (h.threads != 0 && s.groups == h.groups)) continue;
         h = s;

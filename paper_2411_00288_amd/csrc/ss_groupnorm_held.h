@@ -102,20 +102,6 @@ __device__ __forceinline__ HeldPlace held_place(const GroupArgs &p, const HeldSh
     return q;
 }
 
-// act over all of a thread's rows: the choice stands outside of them.
-template <typename F>
-__device__ __forceinline__ void with_act(int act, F &&f)
-{
-    if (act == SS_ACT_RELU)
-        f(std::integral_constant<int, SS_ACT_RELU>{});
-    else if (act == SS_ACT_SILU)
-        f(std::integral_constant<int, SS_ACT_SILU>{});
-    else if (act == SS_ACT_GELU)
-        f(std::integral_constant<int, SS_ACT_GELU>{});
-    else
-        f(std::integral_constant<int, SS_ACT_NONE>{});
-}
-
 // ONE: a thread's eight channels are of one group.
 template <int DT, int NR, int MODE, bool ONE>
 __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(GroupArgs p, HeldShape h)
@@ -210,46 +196,43 @@ __global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kerne
             rx[i] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, q.left, p.C);
             rd[i] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, q.left, p.C);
         }
-    float w[8], b[8], mean[G], r[G];
+    const Channels<G> k(p, q.n, min(q.c, p.C - 1));
     int g[G];
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        const int c = min(q.c + e, p.C - 1);
-        w[e] = p.w != nullptr ? p.w[c] : 1.f;
-        b[e] = p.b != nullptr ? p.b[c] : 0.f;
-        if (e < G) {
-            const float2 st = p.stats[(long long)q.n * p.groups + group_of(p, c)];
-            mean[e % G] = st.x;
-            r[e % G] = st.y;
-            g[e % G] = min(group_of(p, max(c - q.c0, 0)), h.groups - 1);
-        }
-    }
-    // t and xh of row i
-    const auto gradient = [&](int i, auto act, float (&t)[8], float (&xh)[8]) {
-        constexpr int ACT = decltype(act)::value;
-        float x[8], d[8];
+    for (int e = 0; e < G; e++) g[e] = min(group_of(p, max(min(q.c + e, p.C - 1) - q.c0, 0)), h.groups - 1);
+    const auto row_of = [&](int i, float (&x)[8], float (&d)[8]) {
         row_values<DT, MODE>(rx[i], q.c, q.left, p.C, x);
-        row_values<DT, MODE>(rd[i], q.c, q.left, p.C, d);
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            xh[e] = (x[e] - mean[e % G]) * r[e % G];
-            t[e] = gradient_before<DT>(d[e], xh[e], x[e], mean[e % G], r[e % G], w[e], b[e], ACT);
-        }
+        for (int e = 0; e < 8; e++) d[e] = x[e] - k.mean[e % G];
     };
     float s[2][8] = {};
     with_act(p.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
 #pragma unroll
         for (int i = 0; i < NR; i++)
             if (i < q.rows) {
-                float t[8], xh[8];
-                gradient(i, act, t, xh);
+                float x[8], d[8], dy[8], t[8];
+                row_of(i, x, d);
+                row_values<DT, MODE>(rd[i], q.c, q.left, p.C, dy);
+                before_act<DT, ACT>(k, d, x, dy, t);
+                if constexpr (ACT == SS_ACT_RELU) {        // (dy or nothing: it takes dy's place, its channels in theirs)
+#pragma unroll
+                    for (int e = 0; e < (DT == SS_F32 ? 8 : 4); e++) {
+                        if constexpr (DT == SS_F32)
+                            rd[i].v[e / 4][e % 4] = as_bits(t[e]);
+                        else
+                            rd[i].v[0][e] = cvt_pack2<DT>(t[2 * e], t[2 * e + 1]);
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     s[0][e] += t[e];
-                    s[1][e] = __builtin_fmaf(t[e], xh[e], s[1][e]);
+                    s[1][e] = __builtin_fmaf(t[e], d[e], s[1][e]);
                 }
             }
     });
+#pragma unroll
+    for (int e = 0; e < 8; e++) s[1][e] *= k.r[e % G];
     held_sums<2>(h, p.cg, s, smem, channel, group, [&](int c) { return p.w != nullptr ? p.w[min(q.c0 + c, p.C - 1)] : 1.f; });
     for (int c = threadIdx.x; c < h.width && q.c0 + c < p.C; c += h.threads) {
         const float s0 = channel[c], s1 = channel[h.lanes * 8 + c];
@@ -261,20 +244,27 @@ __global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kerne
         }
     }
     const float inv = 1.f / ((float)p.pixels * (float)p.cg);
-    float A[G], K[G];
+    float c0[G], c1[G];                                    // dx = a t - r A - (r B) xh = a t + c0 + c1 d
 #pragma unroll
     for (int e = 0; e < G; e++) {
-        A[e] = group[g[e]] * inv;
-        K[e] = group[h.groups + g[e]] * inv;
+        c0[e] = -k.r[e] * (group[g[e]] * inv);
+        c1[e] = -k.r[e] * k.r[e] * (group[h.groups + g[e]] * inv);
     }
     with_act(p.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
 #pragma unroll
         for (int i = 0; i < NR; i++)
             if (i < q.rows) {
-                float t[8], xh[8];
-                gradient(i, act, t, xh);
+                float x[8], d[8], dy[8], t[8];
+                row_of(i, x, d);
+                if constexpr (ACT == SS_ACT_RELU) {
+                    widen_run<DT>(rd[i], t);
+                } else {
+                    row_values<DT, MODE>(rd[i], q.c, q.left, p.C, dy);
+                    before_act<DT, ACT>(k, d, x, dy, t);
+                }
 #pragma unroll
-                for (int e = 0; e < 8; e++) t[e] = r[e % G] * __builtin_fmaf(-xh[e], K[e % G], __builtin_fmaf(w[e], t[e], -A[e % G]));
+                for (int e = 0; e < 8; e++) t[e] = __builtin_fmaf(d[e], c1[e % G], __builtin_fmaf(t[e], k.a[e], c0[e % G]));
                 store8<DT>(p.out + ((first + (long long)i * h.slots) * p.ldout + q.c) * B, q.left, t);
             }
     });

@@ -65,12 +65,80 @@ __device__ __forceinline__ float slope(float z, int act)
     return __builtin_fmaf(z, 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z), normal_cdf<DT>(z));
 }
 
-// Is z = (x - mean) r w + b above zero?  A sum of 32 bits next to the corner of a ReLU may be on the wrong side, which is no small error of the gradient; there the sum is made in 64.
-__device__ __forceinline__ bool above_corner(float z, float x, float mean, float r, float w, float b)
+__device__ __forceinline__ int group_of(const GroupArgs &p, int c) { return (int)(((unsigned long long)(unsigned)c * p.cg_mul) >> p.cg_sh); }
+
+// f(the activation, known at compile time): a thread's loops over its rows stand inside.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F &&f)
 {
-    bool above = z > 0.f;
-    if (fabsf(z) <= 0x1p-20f * fabsf(b) || fabsf(z) < 0x1p-100f) above = ((double)x - (double)mean) * (double)r * (double)w + (double)b > 0.0;
-    return above;
+    if (act == SS_ACT_RELU)
+        f(std::integral_constant<int, SS_ACT_RELU>{});
+    else if (act == SS_ACT_SILU)
+        f(std::integral_constant<int, SS_ACT_SILU>{});
+    else if (act == SS_ACT_GELU)
+        f(std::integral_constant<int, SS_ACT_GELU>{});
+    else
+        f(std::integral_constant<int, SS_ACT_NONE>{});
+}
+
+// The constants of eight channels from c on, of G groups (1, or up to 8): z = (x - mean) a + b.
+template <int G>
+struct Channels {
+    float mean[G], r[G], a[8], b[8];
+    const float *w;                        // of these channels, or NULL
+    int left;                              // how many there are
+    __device__ __forceinline__ Channels(const GroupArgs &p, int n, int c) : w(p.w != nullptr ? p.w + c : nullptr), left(p.C - c)
+    {
+        if (w != nullptr)
+            load8<SS_F32>(w, left, a);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; e++) a[e] = 1.f;
+        if (p.b != nullptr)
+            load8<SS_F32>(p.b + c, left, b);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; e++) b[e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < G; e++) {
+            const float2 s = p.stats[(long long)n * p.groups + group_of(p, min(c + e, p.C - 1))];
+            mean[e] = s.x;
+            r[e] = s.y;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) a[e] *= r[e % G];
+    }
+};
+
+// t = dy act'(z) of eight channels of a pixel, d = x - mean.
+// A sum of 32 bits next to the corner of a ReLU may be on its wrong side, which is no small error of the gradient: where any of the eight is, they are summed in 64.
+template <int DT, int ACT, int G>
+__device__ __forceinline__ void before_act(const Channels<G> &k, const float (&d)[8], const float (&x)[8], const float (&dy)[8], float (&t)[8])
+{
+    if constexpr (ACT == SS_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) t[e] = dy[e];
+    } else if constexpr (ACT == SS_ACT_RELU) {
+        float z[8], near = 1.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            z[e] = __builtin_fmaf(d[e], k.a[e], k.b[e]);
+            near = fminf(near, fabsf(z[e]) - fmaxf(fabsf(k.b[e]) * 0x1p-20f, 0x1p-100f));
+        }
+        if (near <= 0.f) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const double w = k.w != nullptr && e < k.left ? k.w[e] : 1.f;
+                const double exact = ((double)x[e] - (double)k.mean[e % G]) * (double)k.r[e % G] * w + (double)k.b[e];
+                z[e] = exact > 0.0 ? 1.f : exact <= 0.0 ? 0.f : z[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) t[e] = z[e] <= 0.f ? 0.f : dy[e];          // (a NaN in the group comes in by xh)
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) t[e] = dy[e] * slope<DT>(__builtin_fmaf(d[e], k.a[e], k.b[e]), ACT);
+    }
 }
 
 // Where a thread works: eight channels from c on, of rows slot, slot + slots, ...
@@ -93,8 +161,6 @@ __device__ __forceinline__ Place group_place(const GroupArgs &p)
     q.count = q.idle ? 0 : max(0, (q.last - q.first - q.slot + p.slots - 1) / p.slots);
     return q;
 }
-
-__device__ __forceinline__ int group_of(const GroupArgs &p, int c) { return (int)(((unsigned long long)(unsigned)c * p.cg_mul) >> p.cg_sh); }
 
 // mean and M2 of n values, joined with those of k more
 __device__ __forceinline__ void join_moments(float n, float &mean, float &m2, float k, float mean_k, float m2_k)
@@ -185,29 +251,6 @@ __device__ __forceinline__ float block_sum(float v, float *shared)
     return s;
 }
 
-// The channels' constants of a thread.
-struct Channels {
-    float mean[8], r[8], w[8], b[8];
-    __device__ __forceinline__ Channels(const GroupArgs &p, int n, int c)
-    {
-        const int left = p.C - c;
-        if (p.w != nullptr)
-            load8<SS_F32>(p.w + c, left, w);
-        else
-            for (int e = 0; e < 8; e++) w[e] = 1.f;
-        if (p.b != nullptr)
-            load8<SS_F32>(p.b + c, left, b);
-        else
-            for (int e = 0; e < 8; e++) b[e] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const float2 s = p.stats[(long long)n * p.groups + group_of(p, min(c + e, p.C - 1))];
-            mean[e] = s.x;
-            r[e] = s.y;
-        }
-    }
-};
-
 template <int DT, int MODE>
 __global__ __launch_bounds__(kGroupThreads) void group_apply_kernel(GroupArgs p)
 {
@@ -215,50 +258,28 @@ __global__ __launch_bounds__(kGroupThreads) void group_apply_kernel(GroupArgs p)
     const Place q = group_place(p);
     if (q.count == 0) return;
     const int n = p.C - q.c;
-    const Channels k(p, q.n, q.c);
-    float a[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) a[e] = k.r[e] * k.w[e];
+    const Channels<8> k(p, q.n, q.c);
     const long long base = (long long)q.n * p.pixels + q.first + q.slot;
-    for (int i = 0; i < q.count; i += U) {
-        Run<DT> raw[U];
+    with_act(p.act, [&](auto act) {
+        for (int i = 0; i < q.count; i += U) {
+            Run<DT> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; u++) raw[u] = row_run<DT, MODE>(p.x + (base + (long long)min(i + u, q.count - 1) * p.slots) * p.ldx * B, q.c, n, p.C);
+            for (int u = 0; u < U; u++) raw[u] = row_run<DT, MODE>(p.x + (base + (long long)min(i + u, q.count - 1) * p.slots) * p.ldx * B, q.c, n, p.C);
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            float v[8];
-            row_values<DT, MODE>(raw[u], q.c, n, p.C, v);
+            for (int u = 0; u < U; u++) {
+                float v[8];
+                row_values<DT, MODE>(raw[u], q.c, n, p.C, v);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = activate<DT>(__builtin_fmaf(v[e] - k.mean[e], a[e], k.b[e]), p.act);
-            if (i + u < q.count) store8<DT>(p.out + ((base + (long long)(i + u) * p.slots) * p.ldout + q.c) * B, n, v);
+                for (int e = 0; e < 8; e++) v[e] = activate<DT>(__builtin_fmaf(v[e] - k.mean[e], k.a[e], k.b[e]), decltype(act)::value);
+                if (i + u < q.count) store8<DT>(p.out + ((base + (long long)(i + u) * p.slots) * p.ldout + q.c) * B, n, v);
+            }
         }
-    }
+    });
 }
 
 // ---------------------------------------------------------------------------------------------
 // gradient
 // ---------------------------------------------------------------------------------------------
-// t, the gradient before the activation, from dy.
-template <int DT>
-__device__ __forceinline__ float gradient_before(float dy, float xh, float x, float mean, float r, float w, float b, int act)
-{
-    if (act == SS_ACT_NONE) return dy;
-    const float z = __builtin_fmaf(xh, w, b);
-    if (act == SS_ACT_RELU) return above_corner(z, x, mean, r, w, b) ? dy : z != z ? z : 0.f;
-    return dy * slope<DT>(z, act);
-}
-
-// t and xh of eight channels of a pixel.
-template <int DT>
-__device__ __forceinline__ void group_gradient(const Channels &k, const float (&x)[8], const float (&dy)[8], int act, float (&t)[8], float (&xh)[8])
-{
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-        xh[e] = (x[e] - k.mean[e]) * k.r[e];
-        t[e] = gradient_before<DT>(dy[e], xh[e], x[e], k.mean[e], k.r[e], k.w[e], k.b[e], act);
-    }
-}
-
 // S0 and S1 of each channel over a chunk.
 template <int DT, int MODE>
 __global__ __launch_bounds__(kGroupThreads) void group_sums_kernel(GroupArgs p)
@@ -269,30 +290,36 @@ __global__ __launch_bounds__(kGroupThreads) void group_sums_kernel(GroupArgs p)
     const int n = q.idle ? 0 : p.C - q.c, t = threadIdx.x;
     float s0[8] = {}, s1[8] = {};
     if (q.count > 0) {
-        const Channels k(p, q.n, q.c);
+        const Channels<8> k(p, q.n, q.c);
         const long long base = (long long)q.n * p.pixels + q.first + q.slot;
-        for (int i = 0; i < q.count; i += U) {
-            Run<DT> rx[U], rd[U];
+        with_act(p.act, [&](auto act) {
+            for (int i = 0; i < q.count; i += U) {
+                Run<DT> rx[U], rd[U];
 #pragma unroll
-            for (int u = 0; u < U; u++) {
-                const long long row = base + (long long)min(i + u, q.count - 1) * p.slots;
-                rx[u] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, n, p.C);
-                rd[u] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, n, p.C);
-            }
+                for (int u = 0; u < U; u++) {
+                    const long long row = base + (long long)min(i + u, q.count - 1) * p.slots;
+                    rx[u] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, n, p.C);
+                    rd[u] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, n, p.C);
+                }
 #pragma unroll
-            for (int u = 0; u < U; u++) {
-                float x[8], d[8], g[8], xh[8];
-                row_values<DT, MODE>(rx[u], q.c, n, p.C, x);
-                row_values<DT, MODE>(rd[u], q.c, n, p.C, d);
-                group_gradient<DT>(k, x, d, p.act, g, xh);
-                if (i + u >= q.count) break;
+                for (int u = 0; u < U; u++) {
+                    float x[8], dy[8], d[8], g[8];
+                    row_values<DT, MODE>(rx[u], q.c, n, p.C, x);
+                    row_values<DT, MODE>(rd[u], q.c, n, p.C, dy);
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    s0[e] += g[e];
-                    s1[e] = __builtin_fmaf(g[e], xh[e], s1[e]);
+                    for (int e = 0; e < 8; e++) d[e] = x[e] - k.mean[e];
+                    before_act<DT, decltype(act)::value>(k, d, x, dy, g);
+                    if (i + u >= q.count) break;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        s0[e] += g[e];
+                        s1[e] = __builtin_fmaf(g[e], d[e], s1[e]);
+                    }
                 }
             }
-        }
+        });
+#pragma unroll
+        for (int e = 0; e < 8; e++) s1[e] *= k.r[e];
     }
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -324,30 +351,38 @@ __global__ __launch_bounds__(kGroupThreads) void group_grad_kernel(GroupArgs p)
     const Place q = group_place(p);
     if (q.count == 0) return;
     const int n = p.C - q.c;
-    const Channels k(p, q.n, q.c);
-    float2 coef[8];
+    const Channels<8> k(p, q.n, q.c);
+    float c0[8], c1[8];                                    // dx = a t - r A - (r B) xh = a t + c0 + c1 d
 #pragma unroll
-    for (int e = 0; e < 8; e++) coef[e] = p.coef[(long long)q.n * p.groups + group_of(p, min(q.c + e, p.C - 1))];
-    const long long base = (long long)q.n * p.pixels + q.first + q.slot;
-    for (int i = 0; i < q.count; i += U) {
-        Run<DT> rx[U], rd[U];
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const long long row = base + (long long)min(i + u, q.count - 1) * p.slots;
-            rx[u] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, n, p.C);
-            rd[u] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, n, p.C);
-        }
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            float x[8], d[8], t[8], xh[8];
-            row_values<DT, MODE>(rx[u], q.c, n, p.C, x);
-            row_values<DT, MODE>(rd[u], q.c, n, p.C, d);
-            group_gradient<DT>(k, x, d, p.act, t, xh);
-#pragma unroll
-            for (int e = 0; e < 8; e++) d[e] = k.r[e] * __builtin_fmaf(-xh[e], coef[e].y, __builtin_fmaf(k.w[e], t[e], -coef[e].x));
-            if (i + u < q.count) store8<DT>(p.out + ((base + (long long)(i + u) * p.slots) * p.ldout + q.c) * B, n, d);
-        }
+    for (int e = 0; e < 8; e++) {
+        const float2 coef = p.coef[(long long)q.n * p.groups + group_of(p, min(q.c + e, p.C - 1))];
+        c0[e] = -k.r[e] * coef.x;
+        c1[e] = -k.r[e] * k.r[e] * coef.y;
     }
+    const long long base = (long long)q.n * p.pixels + q.first + q.slot;
+    with_act(p.act, [&](auto act) {
+        for (int i = 0; i < q.count; i += U) {
+            Run<DT> rx[U], rd[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const long long row = base + (long long)min(i + u, q.count - 1) * p.slots;
+                rx[u] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, n, p.C);
+                rd[u] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, n, p.C);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                float x[8], dy[8], d[8], t[8];
+                row_values<DT, MODE>(rx[u], q.c, n, p.C, x);
+                row_values<DT, MODE>(rd[u], q.c, n, p.C, dy);
+#pragma unroll
+                for (int e = 0; e < 8; e++) d[e] = x[e] - k.mean[e];
+                before_act<DT, decltype(act)::value>(k, d, x, dy, t);
+#pragma unroll
+                for (int e = 0; e < 8; e++) t[e] = __builtin_fmaf(d[e], c1[e], __builtin_fmaf(t[e], k.a[e], c0[e]));
+                if (i + u < q.count) store8<DT>(p.out + ((base + (long long)(i + u) * p.slots) * p.ldout + q.c) * B, n, t);
+            }
+        }
+    });
 }
 
 template <int DT>
