@@ -66,30 +66,7 @@ __global__ __launch_bounds__(kGroupThreads) void group_coef_kernel(GroupArgs p)
     if (threadIdx.x == 0) p.coef[(long long)n * p.groups + g] = float2{a / m, b / m};
 }
 
-// dw and db: the images' sums, 16 channels to the workgroup and 16 slices of the images.
-__global__ __launch_bounds__(256) void group_vectors_kernel(GroupArgs p)
-{
-    __shared__ float2 s[16][17];
-    const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, c = (int)blockIdx.x * 16 + lane;
-    float2 v = {0.f, 0.f};
-    if (c < p.C)
-#pragma unroll 4
-        for (int n = slice; n < p.images; n += 16) {
-            v.x += p.total[(long long)n * p.C + c].x;
-            v.y += p.total[(long long)n * p.C + c].y;
-        }
-    s[slice][lane] = v;
-    __syncthreads();
-    if (slice != 0 || c >= p.C) return;
-    float2 sum = {0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 16; k++) {
-        sum.x += s[k][lane].x;
-        sum.y += s[k][lane].y;
-    }
-    if (p.dw != nullptr) p.dw[c] = sum.y;
-    if (p.db != nullptr) p.db[c] = sum.x;
-}
+__global__ __launch_bounds__(kGroupThreads) void group_vectors_kernel(GroupArgs p) { group_vectors(p, (int)blockIdx.x); }
 
 constexpr int kMostChannels = 16384;
 constexpr int64_t kMostPixels = 1 << 24;   // (a group's values are counted in fp32)
@@ -116,13 +93,15 @@ HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pix
     const int C = d->channels, cg = C / d->groups, item = d->dtype == SS_F32 ? 4 : 2, most_rows = held_most_rows(d->dtype);
     const long long cus = std::max(compute_units(), 1);
     if (C < 8 || forced_tile() == GROUP_PASSES) return h;
-    // (bundles whose widths are whole runs of eight channels, where the groups allow it)
+    // Bundles of 64 bytes of a pixel and more, whose widths are whole runs of eight channels where the groups allow it (`unit` of them together); narrower ones, and then, of little to hold, any,
+    // where that gives fewer workgroups than compute units.  (Any, of much: gradient of 128 x 56 x 56 x 96 200 us, in passes 93.)
     int unit = 8;
     while (unit > 1 && cg * (unit / 2) % 8 == 0) unit /= 2;
-    for (int segment = 64; segment >= 16; segment /= 2) {
+    for (int k = 0; k < 6; k++) {
+        const int segment = 64 >> k % 3, together = k < 3 ? unit : 1;
         HeldShape s{};
         s.groups = std::max(1, (segment + cg * item - 1) / (cg * item));
-        s.groups = std::min(d->groups, (s.groups + unit - 1) / unit * unit);
+        s.groups = std::min(d->groups, (s.groups + together - 1) / together * together);
         s.width = s.groups * cg;
         s.bundles = (d->groups + s.groups - 1) / s.groups;
         s.lanes = (s.width + 7) / 8;
@@ -136,10 +115,13 @@ HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pix
             s.rows = (int)rows;
             if (rows <= 4 || images * s.bundles >= cus) break;
         }
-        if (s.threads == 0 || (h.threads != 0 && s.groups == h.groups)) continue;
+        if (s.threads == 0 || (h.threads != 0 && s.bundles <= h.bundles) || (k >= 3 && pixels * s.width * item > 16 << 10)) continue;
         h = s;
-        if (images * s.bundles >= cus) break;
+        if (images * s.bundles >= cus) return h;
     }
+    // Few workgroups with much to hold: the passes share it between more.  (8 images of 112 x 112 x 64, 64 workgroups of 200 KB, 30 us and 17; 2 of 32 x 32 x 640, 32 of
+    // 80 KB, 12 and 15.)
+    if (pixels * h.width * item > 96 << 10) h.threads = 0;
     return h;
 }
 
@@ -283,5 +265,5 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
     done = launched();
     if (done != SS_OK) return done;
     done = launch(a, d->dtype, 3, s);
-    return done != SS_OK ? done : vectors();
+    return done;
 }

@@ -84,6 +84,24 @@ __device__ __forceinline__ void held_sums(const HeldShape &h, int cg, const floa
     __syncthreads();
 }
 
+// The groups' sums of one value to the thread, where a thread's eight channels are of one group: v -> group[g].
+__device__ __forceinline__ void held_group_sums(const HeldShape &h, int cg, float v, float *shared, float *group)
+{
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = h.threads / 64, per = cg / 8;
+    shared[threadIdx.x] = v;
+    __syncthreads();
+    for (int g = wave; g < h.groups; g += waves) {
+        float s = 0.f;
+        for (int k = lane; k < h.slots * per; k += 64) {
+            const int slot = k / per;
+            s += shared[slot * h.lanes + g * per + k - slot * per];
+        }
+        s = lanes_sum<64>(s);
+        if (lane == 0) group[g] = s;
+    }
+    __syncthreads();
+}
+
 struct HeldPlace {
     int n, c0, c, slot, left, rows;        // image, the bundle's first channel, the thread's, its pixel, its channels in the bundle, its pixels
 };
@@ -126,7 +144,6 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
     int g[G];                                              // groups in the bundle
 #pragma unroll
     for (int e = 0; e < G; e++) g[e] = min(group_of(p, max(min(q.c + e, p.C - 1) - q.c0, 0)), h.groups - 1);
-    const auto one = [](int) { return 1.f; };
     const float inv = 1.f / ((float)p.pixels * (float)p.cg);
     float s[1][8] = {};
 #pragma unroll
@@ -137,7 +154,13 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
 #pragma unroll
             for (int e = 0; e < 8; e++) s[0][e] += v[e];
         }
-    held_sums<1>(h, p.cg, s, smem, channel, group, one);
+    const auto sums = [&] {
+        if constexpr (ONE)
+            held_group_sums(h, p.cg, ((s[0][0] + s[0][1]) + (s[0][2] + s[0][3])) + ((s[0][4] + s[0][5]) + (s[0][6] + s[0][7])), smem, group);
+        else
+            held_sums<1>(h, p.cg, s, smem, channel, group, [](int) { return 1.f; });
+    };
+    sums();
     float mean[G];
 #pragma unroll
     for (int e = 0; e < G; e++) mean[e] = group[g[e]] * inv;
@@ -156,7 +179,7 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
                 s[0][e] = __builtin_fmaf(d, d, s[0][e]);
             }
         }
-    held_sums<1>(h, p.cg, s, smem, channel, group, one);
+    sums();
     if (p.stats != nullptr && mine < h.groups) {
         const int at = group_of(p, q.c0) + mine;
         if (at < p.groups) p.stats[(long long)q.n * p.groups + at] = float2{mean_out, reciprocal_root(group[mine] * inv + p.eps)};

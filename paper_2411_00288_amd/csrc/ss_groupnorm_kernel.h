@@ -344,10 +344,37 @@ __global__ __launch_bounds__(kGroupThreads) void group_sums_kernel(GroupArgs p)
         if (e < n) out[e] = float2{s0[e], s1[e]};
 }
 
+// dw and db: the images' sums, 16 channels to the workgroup and 16 slices of the images (workgroups behind those of the last pass).
+__device__ __forceinline__ void group_vectors(const GroupArgs &p, int block)
+{
+    __shared__ float2 s[16][17];
+    const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, c = block * 16 + lane;
+    float2 v = {0.f, 0.f};
+    if (c < p.C)
+#pragma unroll 4
+        for (int n = slice; n < p.images; n += 16) {
+            v.x += p.total[(long long)n * p.C + c].x;
+            v.y += p.total[(long long)n * p.C + c].y;
+        }
+    s[slice][lane] = v;
+    __syncthreads();
+    if (slice != 0 || c >= p.C) return;
+    float2 sum = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 16; k++) {
+        sum.x += s[k][lane].x;
+        sum.y += s[k][lane].y;
+    }
+    if (p.dw != nullptr) p.dw[c] = sum.y;
+    if (p.db != nullptr) p.db[c] = sum.x;
+}
+
 template <int DT, int MODE>
 __global__ __launch_bounds__(kGroupThreads) void group_grad_kernel(GroupArgs p)
 {
     constexpr int U = 4, B = item_bytes<DT>();
+    const int vector_blocks = p.dw != nullptr || p.db != nullptr ? (p.C + 15) / 16 : 0, blocks = (int)gridDim.x - vector_blocks;
+    if ((int)blockIdx.x >= blocks) return group_vectors(p, (int)blockIdx.x - blocks);          // uniform
     const Place q = group_place(p);
     if (q.count == 0) return;
     const int n = p.C - q.c;
@@ -394,7 +421,7 @@ void launch_group(const GroupArgs &a, int stage, hipStream_t s)
         if (stage == 0) group_moments_kernel<DT, MODE><<<grid, block, 0, s>>>(a);
         if (stage == 1) group_apply_kernel<DT, MODE><<<grid, block, 0, s>>>(a);
         if (stage == 2) group_sums_kernel<DT, MODE><<<grid, block, 0, s>>>(a);
-        if (stage == 3) group_grad_kernel<DT, MODE><<<grid, block, 0, s>>>(a);
+        if (stage == 3) group_grad_kernel<DT, MODE><<<dim3(grid.x + (a.dw != nullptr || a.db != nullptr ? (unsigned)((a.C + 15) / 16) : 0u)), block, 0, s>>>(a);
     };
     a.C < 8 ? pick(Mode<NARROW>{}) : a.C % 8 ? pick(Mode<CUT>{}) : pick(Mode<EVEN>{});
 }
