@@ -24,7 +24,8 @@ extern "C" {
  * a wave for each 32 intermediate channels (at most 512), 42 the same resident, with both layers' weights in LDS (96 and 128 channels at both ends); 60 to 65
  * the depthwise convolution on the vector ALU, on the matrix unit, and for few outputs with 1 x 2, 1 x 4, 2 x 4 and 4 x 4 outputs per thread; 70 to 74
  * the pointwise layer on MXFP4 codes in tiles of 64 x 64, 128 x 128 and 256 x 256, and for few rows 32 and 64 at a time; 75 to 78 the same layer on 16-bit
- * input for at most 32 rows, with 32 and 128 quantised rows in LDS, and as a quantisation with one of 70 to 74 behind it.  Ids the problem
+ * input for at most 32 rows, with 32 and 128 quantised rows in LDS, and as a quantisation with one of 70 to 74 behind it; 80 to 88 the same on FP8 with a scale for 128 values; 90 to 92
+ * the pointwise layer's weight gradient in tiles of 64 x 64, 128 x 128 and 256 x 256; 96 the group norm in passes, also where a workgroup could hold its share.  Ids the problem
  * has no kernel for fall back to the library's choice; with an id of 10 or more no split of the reduction is planned.  Process-wide, read with a relaxed
  * atomic load at every launch; meant for single-threaded tests.  Always returns SS_OK.  [host]
  */
@@ -34,7 +35,8 @@ int ss_debug_force_tile(int32_t id);
  * Forces the number of workgroups that share one output tile of the 16-bit convolutions, each taking a share of the
  * reduction (see ss_conv2d_workspace_bytes); the value is clamped to the number of reduction chunks, and layers whose
  * staging mode does not split ignore it.  (With the activation-stationary 1x1 kernel forced, the value is instead the
- * number of workgroups that share a pixel tile, each taking a share of the output channels; no workspace is involved.)
+ * number of workgroups that share a pixel tile, each taking a share of the output channels; no workspace is involved.  Of the
+ * pointwise layer's weight gradient it is the number of parts of the sum over the rows.)
  * 0 or a negative value returns the decision to the library.  The workspace
  * query answers for the forced value, so query after forcing.  Process-wide, as above.  Always returns SS_OK.  [host]
  */

@@ -83,8 +83,7 @@ int check_group(const ss_groupnorm_desc *d, int64_t images, int64_t pixels)
 
 bool rows_ok(const ss_groupnorm_desc *d, const void *p, int64_t ld) { return p && aligned(p, d->dtype == SS_F32 ? 4 : 2) && ld >= d->channels && ld <= INT32_MAX; }
 
-// The kernels, by the ids of the test hook.
-enum { GROUP_HELD = 95, GROUP_PASSES };
+constexpr int kGroupPasses = 96;            // the test hook's id of the passes
 
 // A workgroup's share of an image where it can be held; threads = 0: it cannot.
 HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pixels, bool backward)
@@ -92,7 +91,7 @@ HeldShape held_shape(const ss_groupnorm_desc *d, long long images, long long pix
     HeldShape h{};
     const int C = d->channels, cg = C / d->groups, item = d->dtype == SS_F32 ? 4 : 2, most_rows = held_most_rows(d->dtype);
     const long long cus = std::max(compute_units(), 1);
-    if (C < 8 || forced_tile() == GROUP_PASSES) return h;
+    if (C < 8 || forced_tile() == kGroupPasses) return h;
     // Bundles of 64 bytes of a pixel and more, whose widths are whole runs of eight channels where the groups allow it (`unit` of them together); narrower ones, and then, of little to hold, any,
     // where that gives fewer workgroups than compute units.  (Any, of much: gradient of 128 x 56 x 56 x 96 200 us, in passes 93.)
     int unit = 8;
@@ -165,6 +164,29 @@ GroupPlan group_plan(const ss_groupnorm_desc *d, long long images, long long pix
     return g;
 }
 
+// A call in pieces of images, so that no launch has 2^32 threads: f(arguments of a piece).
+template <typename F>
+int in_pieces(const GroupPlan &g, int item, F &&f)
+{
+    const GroupArgs &all = g.a;
+    const long long threads = g.held.threads != 0 ? (long long)g.held.threads * g.held.bundles : (long long)kGroupThreads * std::max(all.chunks * all.tiles, all.groups);
+    const long long piece = std::max(1ll, (1ll << 31) / threads);
+    for (long long at = 0; at < all.images; at += piece) {
+        GroupArgs a = all;
+        a.images = (int)std::min(piece, all.images - at);
+        a.x += at * a.pixels * a.ldx * item;
+        if (a.dy != nullptr) a.dy += at * a.pixels * a.lddy * item;
+        a.out += at * a.pixels * a.ldout * item;
+        if (a.stats != nullptr) a.stats += at * a.groups;
+        if (a.part != nullptr) a.part += at * a.chunks * a.C;
+        if (a.total != nullptr) a.total += at * a.C;
+        if (a.coef != nullptr) a.coef += at * a.groups;
+        const int st = f(a, piece >= all.images);
+        if (st != SS_OK) return st;
+    }
+    return SS_OK;
+}
+
 int launch(const GroupArgs &a, int dtype, int stage, hipStream_t s)
 {
     dtype == SS_F16 ? launch_group<SS_F16>(a, stage, s) : dtype == SS_BF16 ? launch_group<SS_BF16>(a, stage, s) : launch_group<SS_F32>(a, stage, s);
@@ -211,13 +233,19 @@ extern "C" int ss_groupnorm_fwd(const ss_groupnorm_desc *d, const void *x, int64
     a.b = b;
     a.part = reinterpret_cast<float2 *>(ws);
     a.stats = reinterpret_cast<float2 *>(stats);
-    if (g.held.threads != 0) return launch(a, g.held, d->dtype, false, s);
+    const int item = d->dtype == SS_F32 ? 4 : 2;
+    if (g.held.threads != 0) {
+        a.part = nullptr;
+        return in_pieces(g, item, [&](const GroupArgs &p, bool) { return launch(p, g.held, d->dtype, false, s); });
+    }
     if (!stats) a.stats = reinterpret_cast<float2 *>(ws + g.stats_at);
-    int done = launch(a, d->dtype, 0, s);
-    if (done != SS_OK) return done;
-    group_stats_kernel<<<dim3((unsigned)(images * a.groups)), dim3(kGroupThreads), 0, s>>>(a);
-    done = launched();
-    return done != SS_OK ? done : launch(a, d->dtype, 1, s);
+    return in_pieces(g, item, [&](const GroupArgs &p, bool) {
+        int done = launch(p, d->dtype, 0, s);
+        if (done != SS_OK) return done;
+        group_stats_kernel<<<dim3((unsigned)(p.images * p.groups)), dim3(kGroupThreads), 0, s>>>(p);
+        done = launched();
+        return done != SS_OK ? done : launch(p, d->dtype, 1, s);
+    });
 }
 
 extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int64_t lddy, const void *x, int64_t ldx, int64_t images, int64_t pixels, const float *stats,
@@ -252,18 +280,25 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
     a.w = w;
     a.b = b;
     a.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
+    const int item = d->dtype == SS_F32 ? 4 : 2;
+    if (g.held.threads != 0) {
+        if (images > 1) a.total = reinterpret_cast<float2 *>(ws + g.total_at);
+        const int held = in_pieces(g, item, [&](const GroupArgs &p, bool) { return launch(p, g.held, d->dtype, true, s); });
+        return held != SS_OK || images == 1 ? held : vectors();
+    }
     a.part = reinterpret_cast<float2 *>(ws);
     a.total = reinterpret_cast<float2 *>(ws + g.total_at);
     a.coef = reinterpret_cast<float2 *>(ws + g.coef_at);
-    if (g.held.threads != 0) {
-        const int held = launch(a, g.held, d->dtype, true, s);
-        return held != SS_OK || images == 1 ? held : vectors();
-    }
-    int done = launch(a, d->dtype, 2, s);
-    if (done != SS_OK) return done;
-    group_coef_kernel<<<dim3((unsigned)(images * a.groups)), dim3(kGroupThreads), 0, s>>>(a);
-    done = launched();
-    if (done != SS_OK) return done;
-    done = launch(a, d->dtype, 3, s);
-    return done;
+    bool joined = false;
+    const int done = in_pieces(g, item, [&](GroupArgs &p, bool only) {
+        int done = launch(p, d->dtype, 2, s);
+        if (done != SS_OK) return done;
+        group_coef_kernel<<<dim3((unsigned)(p.images * p.groups)), dim3(kGroupThreads), 0, s>>>(p);
+        done = launched();
+        if (done != SS_OK) return done;
+        joined = only;
+        if (!only) p.dw = p.db = nullptr;                  // (all pieces' sums, behind the last)
+        return launch(p, d->dtype, 3, s);
+    });
+    return done != SS_OK || joined ? done : vectors();
 }

@@ -259,7 +259,7 @@ __global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kerne
     held_sums<2>(h, p.cg, s, smem, channel, group, [&](int c) { return p.w != nullptr ? p.w[min(q.c0 + c, p.C - 1)] : 1.f; });
     for (int c = threadIdx.x; c < h.width && q.c0 + c < p.C; c += h.threads) {
         const float s0 = channel[c], s1 = channel[h.lanes * 8 + c];
-        if (p.images > 1) {
+        if (p.total != nullptr) {
             p.total[(long long)q.n * p.C + q.c0 + c] = float2{s0, s1};
         } else {
             if (p.dw != nullptr) p.dw[q.c0 + c] = s1;

@@ -20,7 +20,7 @@ struct GroupArgs {
     const float *w, *b;
     float2 *stats;                         // [images][groups]: mean, r
     float2 *part;                          // [images][chunks][C]: mean and M2, or S0 and S1, of a chunk
-    float2 *total;                         // backward: [images][C] S0 and S1
+    float2 *total;                         // backward: [images][C] S0 and S1, or NULL where one image's are dw and db
     float2 *coef;                          // backward: [images][groups] A and B
     float *dw, *db;
     long long ldx, lddy, ldout;

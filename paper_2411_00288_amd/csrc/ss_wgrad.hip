@@ -339,7 +339,7 @@ extern "C" int ss_pw_wgrad(const ss_weight_desc *desc, const void *dy, int64_t l
     j.n = (long long)desc->cout * desc->cin;
     j.cout = desc->cout;
     const auto join = [&](bool weights) {
-        const bool many = j.parts >= 16;
+        const bool many = j.parts >= 16 && j.n <= 1 << 28;     // (a thread to 64 / 256 of a value: fewer than 2^32)
         j.blocks = weights ? (unsigned)((j.n + (many ? 63 : 1023)) / (many ? 64 : 1024)) : 0u;
         const unsigned grid = j.blocks + (db ? (unsigned)((desc->cout + 15) / 16) : 0u);
         if (grid == 0) return (int)SS_OK;
