@@ -642,11 +642,12 @@ typedef struct {
 } ss_groupnorm_desc;
 
 /*
- *   x, y      [images][pixels][channels], pitches of a pixel in elements (images follow each other at that pitch), pixels from any element on; y may be x
+ *   x, y      [images][pixels][channels], pitches of a pixel in elements, at most 2^19 (images follow each other at that pitch), pixels from any element on; y may
+ *             be x
  *   w, b      [channels] fp32 or NULL (1 and 0)
  *   stats     [images][groups][2] fp32, written: mean and 1 / sqrt(var + eps), for the backward call; 8-byte aligned, or NULL
  *   workspace ss_groupnorm_workspace_bytes bytes, 16-byte aligned, not initialised; not shared by calls that may run at the same time
- * No images or no pixels: nothing is done.  At most 2^24 pixels to the image and 2^31 - 1 in all (SS_ERR_UNSUPPORTED).  Asynchronous on `stream`.
+ * No images or no pixels: nothing is done.  At most 2^24 pixels to the image and 2^31 - 1 in all (SS_ERR_UNSUPPORTED, as for wider pitches).  Asynchronous on `stream`.
  */
 int ss_groupnorm_workspace_bytes(const ss_groupnorm_desc *desc, int64_t images, int64_t pixels, int32_t backward, size_t *bytes /*[host] out*/);
 int ss_groupnorm_fwd(const ss_groupnorm_desc *desc, const void *x, int64_t ldx, int64_t images, int64_t pixels, const float *w, const float *b,

@@ -70,6 +70,7 @@ __global__ __launch_bounds__(kGroupThreads) void group_vectors_kernel(GroupArgs 
 
 constexpr int kMostChannels = 16384;
 constexpr int64_t kMostPixels = 1 << 24;   // (a group's values are counted in fp32)
+constexpr int64_t kMostPitch = 1 << 19;    // (1024 pixels of it are 2^31 bytes, a lane's offset)
 
 int check_group(const ss_groupnorm_desc *d, int64_t images, int64_t pixels)
 {
@@ -81,7 +82,7 @@ int check_group(const ss_groupnorm_desc *d, int64_t images, int64_t pixels)
     return SS_OK;
 }
 
-bool rows_ok(const ss_groupnorm_desc *d, const void *p, int64_t ld) { return p && aligned(p, d->dtype == SS_F32 ? 4 : 2) && ld >= d->channels && ld <= INT32_MAX; }
+bool rows_ok(const ss_groupnorm_desc *d, const void *p, int64_t ld) { return p && aligned(p, d->dtype == SS_F32 ? 4 : 2) && ld >= d->channels; }
 
 constexpr int kGroupPasses = 96;            // the test hook's id of the passes
 
@@ -220,6 +221,7 @@ extern "C" int ss_groupnorm_fwd(const ss_groupnorm_desc *d, const void *x, int64
     if (!aligned(w, 4) || !aligned(b, 4) || !aligned(stats, 8)) return SS_ERR_INVALID_ARG;
     if (images == 0 || pixels == 0) return SS_OK;
     if (!rows_ok(d, x, ldx) || !rows_ok(d, y, ldy)) return SS_ERR_INVALID_ARG;
+    if (ldx > kMostPitch || ldy > kMostPitch) return SS_ERR_UNSUPPORTED;
     GroupPlan g = group_plan(d, images, pixels, false);
     if (g.bytes > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes)) return SS_ERR_WORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -269,6 +271,7 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
         return vectors();
     }
     if (!stats || !rows_ok(d, x, ldx) || !rows_ok(d, dy, lddy) || !rows_ok(d, dx, lddx)) return SS_ERR_INVALID_ARG;
+    if (std::max({ldx, lddy, lddx}) > kMostPitch) return SS_ERR_UNSUPPORTED;
     if (g.bytes > 0 && (!workspace || !aligned(workspace, 16) || ws_bytes < g.bytes)) return SS_ERR_WORKSPACE;
     char *const ws = static_cast<char *>(workspace);
     a.x = static_cast<const char *>(x);

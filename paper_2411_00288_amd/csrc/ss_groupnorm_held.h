@@ -4,8 +4,8 @@
 // thread holds eight channels of every R-th pixel.  The mean is found first and the squares of the differences from it then.  Sums go over the threads in LDS:
 // first each channel's over the threads that hold it, then each group's over its channels.  Bundles of an image follow each other on one XCD, so that a line whose channels several
 // of them share is read and written once.
-// 64 images of 28 x 28 x 512 in bfloat16 24 us (4.2 TB/s), of 56 x 56 x 256, which takes 1024 threads and a compute unit for 200 KB, 46 to 55; the gradient of the former 47 us, bound by the
-// vector ALU (15 instructions to the value and the sums) and two workgroups to the compute unit; one image of 7 x 7 x 768 6 us with the host's share.
+// 64 images of 28 x 28 x 512 in bfloat16 24 us (4.2 TB/s), of 56 x 56 x 256, which takes 1024 threads and a compute unit for 200 KB, 45 to 53; the gradient of the former 46 us: two
+// workgroups of 256 threads to the compute unit (216 registers a lane), whose reads, sums and writes hardly overlap, the vector ALU busy a tenth of the time.  One image of 7 x 7 x 768 4.7 us.
 #ifndef SS_GROUPNORM_HELD_H_
 #define SS_GROUPNORM_HELD_H_
 #include "ss_groupnorm_kernel.h"
@@ -108,6 +108,23 @@ struct HeldPlace {
     int n, c0, c, slot, left, rows;        // image, the bundle's first channel, the thread's, its pixel, its channels in the bundle, its pixels
 };
 
+// Row i of a thread: a uniform address and the lane's 32 bits (the shape sees to it that they are enough), so that a row in flight takes no registers for its address.
+template <int DT, int MODE>
+__device__ __forceinline__ Run<DT> held_run(const char *image, long long ld, const HeldShape &h, const HeldPlace &q, int i, int C)
+{
+    constexpr int B = item_bytes<DT>();
+    const unsigned lane_at = ((unsigned)q.slot * (unsigned)ld + (unsigned)min(q.c, C - 8)) * B;
+    Run<DT> r;
+    const char *const p = image + (long long)i * h.slots * ld * B + lane_at;
+    if constexpr (DT == SS_F32) {
+        r.v[0] = reinterpret_cast<const Vec32 *>(p)[0].v;
+        r.v[1] = reinterpret_cast<const Vec32 *>(p)[1].v;
+    } else {
+        r.v[0] = reinterpret_cast<const Vec16 *>(p)->v;
+    }
+    return r;
+}
+
 __device__ __forceinline__ HeldPlace held_place(const GroupArgs &p, const HeldShape &h)
 {
     HeldPlace q;
@@ -130,11 +147,13 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
     extern __shared__ float smem[];
     const HeldPlace q = held_place(p, h);
     float *const channel = smem + 8 * h.threads, *const group = channel + h.lanes * 8;
-    const long long first = (long long)q.n * p.pixels + q.slot;
+    const char *const image = p.x + (long long)q.n * p.pixels * p.ldx * B;
+    char *const out = p.out + (long long)q.n * p.pixels * p.ldout * B;
+    const unsigned out_at = ((unsigned)q.slot * (unsigned)p.ldout + (unsigned)q.c) * B;
     Run<DT> raw[NR];
 #pragma unroll
     for (int i = 0; i < NR; i++)
-        if (q.rows > 0) raw[i] = row_run<DT, MODE>(p.x + (first + (long long)min(i, q.rows - 1) * h.slots) * p.ldx * B, q.c, q.left, p.C);
+        if (i < q.rows) raw[i] = held_run<DT, MODE>(image, p.ldx, h, q, i, p.C);
     float w[8], b[8];
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -142,7 +161,7 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
         w[e] = p.w != nullptr ? p.w[c] : 1.f;
         b[e] = p.b != nullptr ? p.b[c] : 0.f;
     }
-    const auto values = [&](int i, float (&v)[8]) { row_values<DT, MODE>(raw[i], q.c, i < q.rows ? q.left : 0, p.C, v); };
+    const auto values = [&](int i, float (&v)[8]) { row_values<DT, MODE>(raw[i], q.c, q.left, p.C, v); };
     int g[G];                                              // groups in the bundle
 #pragma unroll
     for (int e = 0; e < G; e++) g[e] = min(group_of(p, max(min(q.c + e, p.C - 1) - q.c0, 0)), h.groups - 1);
@@ -200,7 +219,7 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
                 values(i, v);
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[e] = activate<DT>(__builtin_fmaf(v[e] - mean[e % G], w[e], b[e]), ACT);
-                store8<DT>(p.out + ((first + (long long)i * h.slots) * p.ldout + q.c) * B, q.left, v);
+                store8<DT>(out + (long long)i * h.slots * p.ldout * B + out_at, q.left, v);
             }
     });
 }
@@ -212,14 +231,15 @@ __global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kerne
     extern __shared__ float smem[];
     const HeldPlace q = held_place(p, h);
     float *const channel = smem + 16 * h.threads, *const group = channel + 2 * h.lanes * 8;
-    const long long first = (long long)q.n * p.pixels + q.slot;
+    const char *const image = p.x + (long long)q.n * p.pixels * p.ldx * B, *const image_dy = p.dy + (long long)q.n * p.pixels * p.lddy * B;
+    char *const out = p.out + (long long)q.n * p.pixels * p.ldout * B;
+    const unsigned out_at = ((unsigned)q.slot * (unsigned)p.ldout + (unsigned)q.c) * B;
     Run<DT> rx[NR], rd[NR];
 #pragma unroll
     for (int i = 0; i < NR; i++)
-        if (q.rows > 0) {
-            const long long row = first + (long long)min(i, q.rows - 1) * h.slots;
-            rx[i] = row_run<DT, MODE>(p.x + row * p.ldx * B, q.c, q.left, p.C);
-            rd[i] = row_run<DT, MODE>(p.dy + row * p.lddy * B, q.c, q.left, p.C);
+        if (i < q.rows) {
+            rx[i] = held_run<DT, MODE>(image, p.ldx, h, q, i, p.C);
+            rd[i] = held_run<DT, MODE>(image_dy, p.lddy, h, q, i, p.C);
         }
     const Channels<G> k(p, q.n, min(q.c, p.C - 1));
     int g[G];
@@ -290,7 +310,7 @@ __global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kerne
                 }
 #pragma unroll
                 for (int e = 0; e < 8; e++) t[e] = __builtin_fmaf(d[e], c1[e % G], __builtin_fmaf(t[e], k.a[e], c0[e % G]));
-                store8<DT>(p.out + ((first + (long long)i * h.slots) * p.ldout + q.c) * B, q.left, t);
+                store8<DT>(out + (long long)i * h.slots * p.ldout * B + out_at, q.left, t);
             }
     });
 }

@@ -229,7 +229,7 @@ __device__ __forceinline__ void quantise_rows(const PwRowsArgs &r, long long row
 // units of the same channels side by side, so that their weights are in the L1).  The input is read once, whatever the number of channels, unless there are few
 // rows: then several workgroups share the channels of one's rows.  The next weights are on their way from the L2 while the current ones are multiplied or, with a
 // reduction of one block (SHORT), while the sums are finished.  One block: units of 64 channels; longer: units of 32.
-// Bound by memory: 96 -> 384 on 401408 rows 76 us (5.1 TB/s), 64 -> 256 on 200704 32, 384 -> 96 on 401408 84; with a residual, 64 -> 256 on 200704 69 (3.4 TB/s).
+// Bound by memory: 96 -> 384 on 401408 rows 76 us (5.1 TB/s), 64 -> 256 on 200704 32, 384 -> 96 on 401408 84; with a residual, 64 -> 256 on 200704 58 (4.0 TB/s).
 template <int DT, int NT, bool SHORT, bool WIDE, int THREADS>
 __global__ __launch_bounds__(THREADS, SHORT && NT == 1 ? 3 : 4) void pw_f8_rows_kernel(PwArgs p, PwRowsArgs r)
 {
@@ -472,7 +472,9 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
-    a.stream = (long long)rows * d->cout * 2 > 256ll << 20;
+    // Where a call moves more than most of the last-level cache its output's half lines are gone from there before their other halves come (64 -> 256 with a residual on 200704 rows, 231 MB,
+    // wrote 1.35 times its output: 69 us, and 58 in whole lines past the caches; without one, 128 MB, 32 us by the caches).
+    a.stream = (long long)rows * (d->cout * (residual ? 2 : 1) + d->cin) * 2 > 192ll << 20;
     return a;
 }
 

@@ -81,7 +81,7 @@ def test_group_norm():
                         (make(24, 3, 0, 0, -1e-9), INVALID), (make(24, 3, 0, 0, float("inf")), INVALID), (make(24, 3, 0, 0, float("nan")), INVALID), (make(16400, 1, 0), UNSUPPORTED)):
         assert fwd(bad) == status and bwd(bad) == status
     for args, status in ((dict(x=None), INVALID), (dict(x=ODD), INVALID), (dict(ldx=23), INVALID), (dict(images=-1), INVALID), (dict(pixels=-1), INVALID), (dict(images=1 << 31), UNSUPPORTED),
-                         (dict(pixels=(1 << 24) + 1), UNSUPPORTED), (dict(images=1 << 16, pixels=1 << 16), UNSUPPORTED), (dict(stats=ctypes.c_void_p(4100)), INVALID)):
+                         (dict(pixels=(1 << 24) + 1), UNSUPPORTED), (dict(images=1 << 16, pixels=1 << 16), UNSUPPORTED), (dict(ldx=(1 << 19) + 1), UNSUPPORTED), (dict(stats=ctypes.c_void_p(4100)), INVALID)):
         assert fwd(**args) == status and bwd(**args) == status, args
     assert fwd(y=None) == INVALID and fwd(ldy=23) == INVALID
     assert bwd(dy=None) == INVALID and bwd(lddy=23) == INVALID and bwd(dx=None) == INVALID and bwd(stats=None) == INVALID and bwd(ws=None) == WORKSPACE
