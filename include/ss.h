@@ -490,6 +490,7 @@ int ss_pw_mx4_q_fwd(const ss_weight_desc *desc, const void *codes, const void *s
  *
  * A quantised activation of `rows` rows (pixels, tokens) and `cols` channels, KB = ceil(cols/128):
  *   codes   [rows][64*ceil(cols/64)] bytes; those past the last channel are zero.  16-byte aligned.
+ *           No byte is E4M3's NaN (0x7F, 0xFF): a block with a NaN or an infinity has codes 0 and the scale byte 0xFF.  ss_pw_f8_q_fwd may give NaN in other rows for codes that hold one.
  *   scales  [rows][4*ceil(KB/4)] bytes, those past the KB-th zero.  4-byte aligned.
  * Rows of a 16- or 32-bit tensor may lie further apart than they are long (ld*, in elements), and begin at any element.  rows = 0 does nothing.  At most 2^22 channels.
  */

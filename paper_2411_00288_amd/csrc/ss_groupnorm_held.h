@@ -4,8 +4,9 @@
 // thread holds eight channels of every R-th pixel.  The mean is found first and the squares of the differences from it then.  Sums go over the threads in LDS:
 // first each channel's over the threads that hold it, then each group's over its channels.  Bundles of an image follow each other on one XCD, so that a line whose channels several
 // of them share is read and written once.
-// 64 images of 28 x 28 x 512 in bfloat16 24 us (4.2 TB/s), of 56 x 56 x 256, which takes 1024 threads and a compute unit for 200 KB, 45 to 53; the gradient of the former 46 us: two
-// workgroups of 256 threads to the compute unit (216 registers a lane), whose reads, sums and writes hardly overlap, the vector ALU busy a tenth of the time.  One image of 7 x 7 x 768 4.7 us.
+// 64 images of 28 x 28 x 512 in bfloat16 24 us (4.2 TB/s), of 56 x 56 x 256, which takes 1024 threads and a compute unit for 200 KB, 46 to 53; the gradient of the former 45 us and 48 with
+// the vectors' launch: two workgroups of 256 threads to the compute unit (216 registers a lane), memory read and written once and the vector ALU busy a tenth of the time, so that probably
+// too few reads are in flight while sums are joined and rows written.  One image of 7 x 7 x 768 5.0 us.
 #ifndef SS_GROUPNORM_HELD_H_
 #define SS_GROUPNORM_HELD_H_
 #include "ss_groupnorm_kernel.h"

@@ -472,9 +472,7 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
-    // Where a call moves more than most of the last-level cache its output's half lines are gone from there before their other halves come (64 -> 256 with a residual on 200704 rows, 231 MB,
-    // wrote 1.35 times its output: 69 us, and 58 in whole lines past the caches; without one, 128 MB, 32 us by the caches).
-    a.stream = (long long)rows * (d->cout * (residual ? 2 : 1) + d->cin) * 2 > 192ll << 20;
+    a.stream = rows * d->cout * 2ll > 256ll << 20;        // (an output that the last-level cache does not hold)
     return a;
 }
 
@@ -546,13 +544,17 @@ int product16(const PwArgs &a, const F8Dims &t, F8Kernel kernel, const void *x, 
         };
         const auto rows = [&](auto nt, auto brief, auto threads) -> int {
             constexpr int NT = decltype(nt)::value, THREADS = decltype(threads)::value;
+            // Where a call moves more than most of the last-level cache, half lines of its output are gone from there before their other halves come: 64 -> 256 with a residual on 200704 rows,
+            // 231 MB, wrote 1.35 times its output and took 69 us, and 1.14 times and 58 in whole lines past the caches.  (Tiles of codes, the same layer: 57 by the caches, 62 past them.)
+            PwArgs b = a;
+            b.stream = a.stream || a.P * (2ll * a.cout * (a.residual != nullptr ? 2 : 1) + 2ll * a.K) > 192ll << 20;
             r.step_row = THREADS / runs;
             r.step_run = THREADS % runs;
             const long long blocks = ((long long)a.P + 32 * NT - 1) / (32 * NT);
             const int splits = NT == 1 ? f8_rows_splits(t, a.P, std::max(compute_units(), 1)) : 1;
             r.blocks = (unsigned)blocks;
             r.units = ((decltype(brief)::value ? (t.Mt + 1) / 2 : t.Mt) + splits - 1) / splits;
-            return launch_lds<pw_f8_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, f8_rows_lds(t, 32 * NT), s, a, r);
+            return launch_lds<pw_f8_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, f8_rows_lds(t, 32 * NT), s, b, r);
         };
         if (kernel == F816_FEW) {
             const int waves = f8_few16_waves(t, a.P, a.K);
