@@ -118,14 +118,17 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_f8_tile_kernel(
     // Chunk q, its number modulo four known: while a group's products are made, the next group's pixels and the weights of the third step from it come; the
     // barrier stands before the last group, in front of the next chunk's first read and behind the last of the current one's, whose buffer is then filled with the
     // chunk after the next.  No branches: the compiler moves matrix instructions behind one, away from their loads; what is loaded behind the last chunk is not used.
-    auto chunk = [&](int q, auto number) {
+    // LOOP: within the loop, where every load has a reader.  Of the chunks behind it some have none, which the compiler removes: a count of them there would let pieces of the next chunk
+    // be on their way when other waves read them, so all is waited for.
+    auto chunk = [&](int q, auto number, auto loop) {
         constexpr int N = decltype(number)::value;
+        constexpr bool LOOP = decltype(loop)::value;
         uint8_t *const mine = N % 2 ? odd_s : even_s, *const other = N % 2 ? even_s : odd_s;
         const auto group = [&](auto which) {
             constexpr int W = decltype(which)::value, s = W / NG, g = W % NG, next = (W + 1) % (2 * NG);
             __builtin_amdgcn_sched_barrier(0);
             if (next == 0) {
-                wait_loads<4 * MI + (N == 1 ? MI + NI : 0)>();          // the next chunk is there: what came behind it may be under way
+                wait_loads<LOOP ? 4 * MI + (N == 1 ? MI + NI : 0) : 0>();           // the next chunk is there: what came behind it may be under way
                 lds_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 stage(q + 2, mine);
@@ -158,16 +161,16 @@ __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_f8_tile_kernel(
     // The largest tiles have no registers for a way out of the middle: they go on to a scale word's end, with zero weights.
     const int end = MI * NI >= 16 ? (Ks + 1) / 2 : whole - 3;
     for (; q < end; q += 4) {
-        chunk(q, Int<0>{});
-        chunk(q + 1, Int<1>{});
-        chunk(q + 2, Int<2>{});
-        chunk(q + 3, Int<3>{});
+        chunk(q, Int<0>{}, std::true_type{});
+        chunk(q + 1, Int<1>{}, std::true_type{});
+        chunk(q + 2, Int<2>{}, std::true_type{});
+        chunk(q + 3, Int<3>{}, std::true_type{});
     }
     if constexpr (MI * NI < 16) {
         const int left = whole - q;
-        if (left > 0) chunk(q, Int<0>{});
-        if (left > 1) chunk(q + 1, Int<1>{});
-        if (left > 2) chunk(q + 2, Int<2>{});
+        if (left > 0) chunk(q, Int<0>{}, std::false_type{});
+        if (left > 1) chunk(q + 1, Int<1>{}, std::false_type{});
+        if (left > 2) chunk(q + 2, Int<2>{}, std::false_type{});
         if (Ks % 2) {
             if (left == 0) step_f8<0, 0>(wa[0], xb[0], acc, sa, sb);
             if (left == 1) step_f8<1, 0>(wa[2], xb[0], acc, sa, sb);
