@@ -41,15 +41,22 @@ __device__ __forceinline__ float normal_cdf(float z)
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
+// From 256 on in magnitude the exponentials are 0 or infinity, and sigmoid, Phi and both slopes 0 or 1, whatever z is: bounded there, an infinity meets no 0 and gives the limit.
+constexpr float kActEnd = 256.f;
+
 template <int DT>
 __device__ __forceinline__ float activate(float z, int act)
 {
     if (act == SS_ACT_RELU) return floor_at(z, 0.f);
-    if (act == SS_ACT_SILU) return z * sigmoid(z);
+    if (act == SS_ACT_SILU) {
+        z = floor_at(z, -kActEnd);
+        return z * sigmoid(z);
+    }
     if (act == SS_ACT_GELU) {
-        if constexpr (DT == SS_F32)
+        if constexpr (DT == SS_F32) {
+            z = floor_at(z, -kActEnd);
             return z * normal_cdf<DT>(z);
-        else
+        } else
             return gelu_cdf<DT>(z);
     }
     return z;
@@ -59,6 +66,7 @@ __device__ __forceinline__ float activate(float z, int act)
 template <int DT>
 __device__ __forceinline__ float slope(float z, int act)
 {
+    z = -floor_at(-floor_at(z, -kActEnd), -kActEnd);
     if (act == SS_ACT_SILU) {
         const float s = sigmoid(z);
         return s * __builtin_fmaf(z, 1.f - s, 1.f);
