@@ -14,57 +14,110 @@ SS_HELD_LAUNCHES(extern, SS_F32)
 
 namespace {
 
-// An image's group: its chunks' and channels' moments together.
-__global__ __launch_bounds__(kGroupThreads) void group_stats_kernel(GroupArgs p)
+constexpr int kMostJoinThreads = 1024;
+
+// Where a thread works that joins what the chunks of an image's group left: `lanes` threads side by side over its channels, `slices` of those over its chunks.
+struct JoinPlace {
+    int n, g, lanes, slices, lane, slice;
+    __device__ __forceinline__ explicit JoinPlace(const GroupArgs &p)
+    {
+        n = (int)(blockIdx.x / (unsigned)p.groups);
+        g = (int)blockIdx.x - n * p.groups;
+        lanes = min(p.cg, (int)blockDim.x);
+        slices = (int)blockDim.x / lanes;
+        slice = (int)threadIdx.x / lanes;
+        lane = (int)threadIdx.x - slice * lanes;
+    }
+};
+
+// The workgroup's sum, in a fixed order.
+__device__ __forceinline__ double join_sum(double v, double *shared)
 {
-    __shared__ float shared[kGroupThreads / 64];
-    const int n = (int)(blockIdx.x / (unsigned)p.groups), g = (int)blockIdx.x - n * p.groups;
-    const float2 *const part = p.part + (long long)n * p.chunks * p.C + (long long)g * p.cg;
-    const long long entries = (long long)p.chunks * p.cg;
-    const float m = (float)p.pixels * (float)p.cg;
-    const auto rows_of = [&](int chunk) { return (float)(min(p.pixels, (chunk + 1) * p.per_chunk) - chunk * p.per_chunk); };
-    float s = 0.f;
-    for (long long i = threadIdx.x; i < entries; i += kGroupThreads) {
-        const int chunk = (int)(i / p.cg), c = (int)(i - (long long)chunk * p.cg);
-        s = __builtin_fmaf(part[(long long)chunk * p.C + c].x, rows_of(chunk) / m, s);
-    }
-    const float mean = block_sum(s, shared);
-    s = 0.f;
-    for (long long i = threadIdx.x; i < entries; i += kGroupThreads) {
-        const int chunk = (int)(i / p.cg), c = (int)(i - (long long)chunk * p.cg);
-        const float2 v = part[(long long)chunk * p.C + c];
-        const float d = v.x - mean;
-        s += __builtin_fmaf(d * d, rows_of(chunk), v.y);
-    }
-    const float m2 = block_sum(s, shared);
-    if (threadIdx.x == 0) p.stats[(long long)n * p.groups + g] = float2{mean, reciprocal_root(m2 / m + p.eps)};
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) v += __shfl_xor(v, step);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int k = 0; k < (int)blockDim.x / 64; k++) s += shared[k];
+    return s;
 }
 
-// An image's group: its channels' sums over the chunks, and A and B.
-__global__ __launch_bounds__(kGroupThreads) void group_coef_kernel(GroupArgs p)
+// An image's group: its chunks' and channels' moments together.  With a channel's mean d away from a value k of the group, over `rows` pixels, mean = k + sum of rows d / m and
+// M2 = sum of (M2 + rows d^2) - m (mean - k)^2: in 64 bits, where neither the number of chunks nor the difference takes what 32 hold.
+__global__ __launch_bounds__(kMostJoinThreads) void group_stats_kernel(GroupArgs p)
 {
-    __shared__ float shared[kGroupThreads / 64];
-    const int n = (int)(blockIdx.x / (unsigned)p.groups), g = (int)blockIdx.x - n * p.groups;
-    float a = 0.f, b = 0.f;
-    for (int i = threadIdx.x; i < p.cg; i += kGroupThreads) {
-        const int c = g * p.cg + i;
-        const float2 *part = p.part + (long long)n * p.chunks * p.C + c;
-        float2 s = {0.f, 0.f};
-#pragma unroll 4
-        for (int k = 0; k < p.chunks; k++) {
-            s.x += part[(long long)k * p.C].x;
-            s.y += part[(long long)k * p.C].y;
-        }
-        p.total[(long long)n * p.C + c] = s;
-        const float w = p.w != nullptr ? p.w[c] : 1.f;
-        a = __builtin_fmaf(w, s.x, a);
-        b = __builtin_fmaf(w, s.y, b);
-    }
-    a = block_sum(a, shared);
-    b = block_sum(b, shared);
-    const float m = (float)p.pixels * (float)p.cg;
-    if (threadIdx.x == 0) p.coef[(long long)n * p.groups + g] = float2{a / m, b / m};
+    __shared__ double shared[kMostJoinThreads / 64];
+    const JoinPlace q(p);
+    const float2 *const part = p.part + (long long)q.n * p.chunks * p.C + (long long)q.g * p.cg;
+    const double m = (double)p.pixels * (double)p.cg, k = part[0].x;
+    const double rows = p.per_chunk, last = p.pixels - (p.chunks - 1) * p.per_chunk;
+    double s1 = 0.0, s2 = 0.0;
+    if (q.slice < q.slices)
+        for (int c = q.lane; c < p.cg; c += q.lanes)
+#pragma unroll 8
+            for (int chunk = q.slice; chunk < p.chunks; chunk += q.slices) {
+                const float2 v = part[(long long)chunk * p.C + c];
+                const double d = (double)v.x - k, t = (chunk + 1 < p.chunks ? rows : last) * d;
+                s1 += t;
+                s2 += __builtin_fma(t, d, (double)v.y);
+            }
+    s1 = join_sum(s1, shared);
+    s2 = join_sum(s2, shared);
+    const double d = s1 / m;
+    double var = s2 / m - d * d;
+    if (var < 0.0) var = 0.0;                              // (a NaN stays one)
+    if (threadIdx.x == 0) p.stats[(long long)q.n * p.groups + q.g] = float2{(float)(k + d), reciprocal_root((float)(var + (double)p.eps))};
 }
+
+// An image's group: its channels' sums over the chunks, and A and B; in 64 bits, as many chunks as there may be.
+__global__ __launch_bounds__(kMostJoinThreads) void group_coef_kernel(GroupArgs p)
+{
+    __shared__ double2 slice_s[kMostJoinThreads];
+    __shared__ double shared[kMostJoinThreads / 64];
+    const JoinPlace q(p);
+    double a = 0.0, b = 0.0;
+    for (int at = 0; at < p.cg; at += q.lanes) {           // (more than once: then there is one slice)
+        const int i = at + q.lane, c = q.g * p.cg + i;
+        const bool in = q.slice < q.slices && i < p.cg;
+        const float2 *const part = p.part + (long long)q.n * p.chunks * p.C + c;
+        double2 s = {0.0, 0.0};
+        if (in)
+#pragma unroll 8
+            for (int k = q.slice; k < p.chunks; k += q.slices) {
+                const float2 v = part[(long long)k * p.C];
+                s.x += v.x;
+                s.y += v.y;
+            }
+        if (q.slices > 1) {
+            slice_s[threadIdx.x] = s;
+            for (int left = q.slices; left > 1;) {
+                const int half = (left + 1) / 2;
+                __syncthreads();
+                if (q.slice + half < left) {
+                    const double2 o = slice_s[threadIdx.x + half * q.lanes];
+                    s.x += o.x;
+                    s.y += o.y;
+                    slice_s[threadIdx.x] = s;
+                }
+                left = half;
+            }
+        }
+        if (in && q.slice == 0) {
+            p.total[(long long)q.n * p.C + c] = float2{(float)s.x, (float)s.y};
+            const double w = p.w != nullptr ? p.w[c] : 1.f;
+            a = __builtin_fma(w, s.x, a);
+            b = __builtin_fma(w, s.y, b);
+        }
+    }
+    a = join_sum(a, shared);
+    b = join_sum(b, shared);
+    const double m = (double)p.pixels * (double)p.cg;
+    if (threadIdx.x == 0) p.coef[(long long)q.n * p.groups + q.g] = float2{(float)(a / m), (float)(b / m)};
+}
+
+// Threads that join a group's chunks: one to eight of its values.
+int join_threads(const GroupArgs &a) { return (int)std::clamp<long long>(((long long)a.chunks * a.cg / 8 + 63) / 64 * 64, 64, kMostJoinThreads); }
 
 __global__ __launch_bounds__(kGroupThreads) void group_vectors_kernel(GroupArgs p) { group_vectors(p, (int)blockIdx.x); }
 
@@ -131,7 +184,10 @@ struct GroupPlan {
     size_t total_at, coef_at, stats_at, bytes;
 };
 
-// Chunks: as many as give each compute unit eight workgroups, of at least eight rows to the thread.
+// Chunks: as many as give each compute unit eight workgroups, of at least eight rows to the thread and 32 in all, so that what they leave is at most an eighth of the data; for a group of many
+// channels, which one workgroup joins, so many that they leave it 128 values to the thread at most; but of at most 512 rows to the thread, which adds them in 32 bits.  (Of eight rows of 2048
+// channels the joins took most of the time: one image of 112 x 112 x 2048 in bfloat16 264 us and its gradient 173, in chunks of 32 rows and joined by more threads 40 and 53; 64 x 64 x 1280 in one group
+// 1813 and 230, 41 and 53.)
 GroupPlan group_plan(const ss_groupnorm_desc *d, long long images, long long pixels, bool backward)
 {
     GroupPlan g{};
@@ -148,8 +204,8 @@ GroupPlan group_plan(const ss_groupnorm_desc *d, long long images, long long pix
     a.lanes = std::min((a.C + 7) / 8, kGroupThreads);
     a.tiles = ((a.C + 7) / 8 + a.lanes - 1) / a.lanes;
     a.slots = kGroupThreads / a.lanes;
-    const long long want = std::max(1ll, 8 * cus / (images * a.tiles)), most = std::max(1ll, pixels / (8ll * a.slots));
-    const long long chunks = std::min(want, most);
+    const long long want = 8 * cus / (images * a.tiles), most = pixels / std::max(8ll * a.slots, 32ll), least = pixels / (512ll * a.slots);
+    const long long chunks = std::max({1ll, least, std::min({want, most, 128ll * kMostJoinThreads / a.cg})});
     a.per_chunk = (int)((pixels + chunks - 1) / chunks);
     a.chunks = (int)((pixels + a.per_chunk - 1) / a.per_chunk);
     const auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
@@ -170,7 +226,7 @@ template <typename F>
 int in_pieces(const GroupPlan &g, int item, F &&f)
 {
     const GroupArgs &all = g.a;
-    const long long threads = g.held.threads != 0 ? (long long)g.held.threads * g.held.bundles : (long long)kGroupThreads * std::max(all.chunks * all.tiles, all.groups);
+    const long long threads = g.held.threads != 0 ? (long long)g.held.threads * g.held.bundles : std::max((long long)kGroupThreads * all.chunks * all.tiles, (long long)kMostJoinThreads * all.groups);
     const long long piece = std::max(1ll, (1ll << 31) / threads);
     for (long long at = 0; at < all.images; at += piece) {
         GroupArgs a = all;
@@ -244,7 +300,7 @@ extern "C" int ss_groupnorm_fwd(const ss_groupnorm_desc *d, const void *x, int64
     return in_pieces(g, item, [&](const GroupArgs &p, bool) {
         int done = launch(p, d->dtype, 0, s);
         if (done != SS_OK) return done;
-        group_stats_kernel<<<dim3((unsigned)(p.images * p.groups)), dim3(kGroupThreads), 0, s>>>(p);
+        group_stats_kernel<<<dim3((unsigned)(p.images * p.groups)), dim3(join_threads(p)), 0, s>>>(p);
         done = launched();
         return done != SS_OK ? done : launch(p, d->dtype, 1, s);
     });
@@ -296,7 +352,7 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
     const int done = in_pieces(g, item, [&](GroupArgs &p, bool only) {
         int done = launch(p, d->dtype, 2, s);
         if (done != SS_OK) return done;
-        group_coef_kernel<<<dim3((unsigned)(p.images * p.groups)), dim3(kGroupThreads), 0, s>>>(p);
+        group_coef_kernel<<<dim3((unsigned)(p.images * p.groups)), dim3(join_threads(p)), 0, s>>>(p);
         done = launched();
         if (done != SS_OK) return done;
         joined = only;

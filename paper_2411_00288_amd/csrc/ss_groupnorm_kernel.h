@@ -6,9 +6,9 @@
 //     dx = r (w t - A - xh B),      A = sum over the group of w S0 / m,      B = sum of w S1 / m
 //
 // Images of any size: a kernel finds sums of each channel over a chunk of pixels, a second joins them for each image and group, a third applies what they give.  A channel's mean and
-// sum of squared differences are found around its first value, and joined by the differences of means: no small difference of large sums.  All sums are fp32,
-// in a fixed order.  Bound by memory, three times x forward (64 x 56 x 56 x 256 in bfloat16 62 us, 4.9 TB/s), five tensors backward (115 us, 4.5 TB/s), and by three launches: one image of
-// 64 x 64 x 320 17 and 22 us.
+// sum of squared differences are found around its first value, and joined by the differences of means: no small difference of large sums.  All sums are in 32 bits, over
+// the chunks in 64, in a fixed order.  Bound by memory, three times x forward (64 x 56 x 56 x 256 in bfloat16 62 us, 4.9 TB/s), five tensors backward (115 us, 4.5 TB/s), and by three launches: one image of
+// 64 x 64 x 320 16 and 19 us.
 #ifndef SS_GROUPNORM_KERNEL_H_
 #define SS_GROUPNORM_KERNEL_H_
 #include "ss_norm_kernel.h"
@@ -247,17 +247,6 @@ __global__ __launch_bounds__(kGroupThreads) void group_moments_kernel(GroupArgs 
 #pragma unroll
     for (int e = 0; e < 8; e++)
         if (e < n) out[e] = float2{s1[e], s2[e]};
-}
-
-__device__ __forceinline__ float block_sum(float v, float *shared)
-{
-    v = lanes_sum<64>(v);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int k = 0; k < (int)blockDim.x / 64; k++) s += shared[k];
-    return s;
 }
 
 template <int DT, int MODE>
