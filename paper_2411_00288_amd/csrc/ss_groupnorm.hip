@@ -119,7 +119,10 @@ __global__ __launch_bounds__(kMostJoinThreads) void group_coef_kernel(GroupArgs 
 // Threads that join a group's chunks: one to eight of its values.
 int join_threads(const GroupArgs &a) { return (int)std::clamp<long long>(((long long)a.chunks * a.cg / 8 + 63) / 64 * 64, 64, kMostJoinThreads); }
 
-__global__ __launch_bounds__(kGroupThreads) void group_vectors_kernel(GroupArgs p) { group_vectors(p, (int)blockIdx.x); }
+template <int SLICES>
+__global__ __launch_bounds__(SLICES * 16) void group_vectors_kernel(GroupArgs p) { group_vectors<SLICES>(p, (int)blockIdx.x); }
+
+constexpr int kManyImages = 512;            // 32 to a thread of 16 slices
 
 constexpr int kMostChannels = 16384;
 constexpr int64_t kMostPixels = 1 << 24;   // (a group's values are counted in fp32)
@@ -319,7 +322,11 @@ extern "C" int ss_groupnorm_bwd(const ss_groupnorm_desc *d, const void *dy, int6
     a.db = db;
     const auto vectors = [&] {
         if (!dw && !db) return (int)SS_OK;
-        group_vectors_kernel<<<dim3((unsigned)((a.C + 15) / 16)), dim3(256), 0, s>>>(a);
+        const dim3 grid((unsigned)((a.C + 15) / 16));
+        if (a.images < kManyImages)
+            group_vectors_kernel<16><<<grid, dim3(256), 0, s>>>(a);
+        else
+            group_vectors_kernel<64><<<grid, dim3(1024), 0, s>>>(a);
         return launched();
     };
     if (images == 0 || pixels == 0) {                       // sums over nothing

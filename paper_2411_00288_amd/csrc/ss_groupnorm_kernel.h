@@ -342,29 +342,31 @@ __global__ __launch_bounds__(kGroupThreads) void group_sums_kernel(GroupArgs p)
         if (e < n) out[e] = float2{s0[e], s1[e]};
 }
 
-// dw and db: the images' sums, 16 channels to the workgroup and 16 slices of the images (workgroups behind those of the last pass).
+// dw and db: the images' sums, in 64 bits, however many there are; 16 channels to the workgroup and `SLICES` slices of the images.
+template <int SLICES>
 __device__ __forceinline__ void group_vectors(const GroupArgs &p, int block)
 {
-    __shared__ float2 s[16][17];
+    __shared__ double2 s[SLICES][17];
     const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, c = block * 16 + lane;
-    float2 v = {0.f, 0.f};
+    double2 v = {0.0, 0.0};
     if (c < p.C)
 #pragma unroll 4
-        for (int n = slice; n < p.images; n += 16) {
-            v.x += p.total[(long long)n * p.C + c].x;
-            v.y += p.total[(long long)n * p.C + c].y;
+        for (int n = slice; n < p.images; n += SLICES) {
+            const float2 t = p.total[(long long)n * p.C + c];
+            v.x += t.x;
+            v.y += t.y;
         }
     s[slice][lane] = v;
     __syncthreads();
     if (slice != 0 || c >= p.C) return;
-    float2 sum = {0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 16; k++) {
+    double2 sum = {0.0, 0.0};
+#pragma unroll 8
+    for (int k = 0; k < SLICES; k++) {
         sum.x += s[k][lane].x;
         sum.y += s[k][lane].y;
     }
-    if (p.dw != nullptr) p.dw[c] = sum.y;
-    if (p.db != nullptr) p.db[c] = sum.x;
+    if (p.dw != nullptr) p.dw[c] = (float)sum.y;
+    if (p.db != nullptr) p.db[c] = (float)sum.x;
 }
 
 template <int DT, int MODE>
@@ -372,7 +374,7 @@ __global__ __launch_bounds__(kGroupThreads) void group_grad_kernel(GroupArgs p)
 {
     constexpr int U = 4, B = item_bytes<DT>();
     const int vector_blocks = p.dw != nullptr || p.db != nullptr ? (p.C + 15) / 16 : 0, blocks = (int)gridDim.x - vector_blocks;
-    if ((int)blockIdx.x >= blocks) return group_vectors(p, (int)blockIdx.x - blocks);          // uniform
+    if ((int)blockIdx.x >= blocks) return group_vectors<kGroupThreads / 16>(p, (int)blockIdx.x - blocks);           // uniform (workgroups behind those of the pass)
     const Place q = group_place(p);
     if (q.count == 0) return;
     const int n = p.C - q.c;
