@@ -41,22 +41,20 @@ __device__ __forceinline__ float normal_cdf(float z)
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
-// From 256 on in magnitude the exponentials are 0 or infinity, and sigmoid, Phi and both slopes 0 or 1, whatever z is: bounded there, an infinity meets no 0 and gives the limit.
+// From 256 on in magnitude the exponentials are 0 or infinity, and sigmoid, Phi and both slopes 0 or 1, whatever z is: a factor z bounded there meets no 0 as an infinity, and the product is
+// the limit.  (One instruction; it makes a number of a NaN, which the other factor keeps.)
 constexpr float kActEnd = 256.f;
+__device__ __forceinline__ float act_factor(float z, float end) { return __builtin_amdgcn_fmed3f(z, -kActEnd, end); }
 
 template <int DT>
 __device__ __forceinline__ float activate(float z, int act)
 {
     if (act == SS_ACT_RELU) return floor_at(z, 0.f);
-    if (act == SS_ACT_SILU) {
-        z = floor_at(z, -kActEnd);
-        return z * sigmoid(z);
-    }
+    if (act == SS_ACT_SILU) return act_factor(z, __builtin_inff()) * sigmoid(z);
     if (act == SS_ACT_GELU) {
-        if constexpr (DT == SS_F32) {
-            z = floor_at(z, -kActEnd);
-            return z * normal_cdf<DT>(z);
-        } else
+        if constexpr (DT == SS_F32)
+            return act_factor(z, __builtin_inff()) * normal_cdf<DT>(z);
+        else
             return gelu_cdf<DT>(z);
     }
     return z;
@@ -66,12 +64,12 @@ __device__ __forceinline__ float activate(float z, int act)
 template <int DT>
 __device__ __forceinline__ float slope(float z, int act)
 {
-    z = -floor_at(-floor_at(z, -kActEnd), -kActEnd);
+    const float f = act_factor(z, kActEnd);
     if (act == SS_ACT_SILU) {
         const float s = sigmoid(z);
-        return s * __builtin_fmaf(z, 1.f - s, 1.f);
+        return s * __builtin_fmaf(f, 1.f - s, 1.f);
     }
-    return __builtin_fmaf(z, 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z), normal_cdf<DT>(z));
+    return __builtin_fmaf(f, 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z), normal_cdf<DT>(z));
 }
 
 __device__ __forceinline__ int group_of(const GroupArgs &p, int c) { return (int)(((unsigned long long)(unsigned)c * p.cg_mul) >> p.cg_sh); }
