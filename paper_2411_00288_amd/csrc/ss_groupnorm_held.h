@@ -110,7 +110,7 @@ struct HeldPlace {
 };
 
 // Row i of a thread: a uniform address and the lane's 32 bits (the shape sees to it that they are enough), so that a row in flight takes no registers for its address.
-template <int DT, int MODE>
+template <int DT>
 __device__ __forceinline__ Run<DT> held_run(const char *image, long long ld, const HeldShape &h, const HeldPlace &q, int i, int C)
 {
     constexpr int B = item_bytes<DT>();
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(held_most_threads(false)) void group_held_kernel(Gr
     Run<DT> raw[NR];
 #pragma unroll
     for (int i = 0; i < NR; i++)
-        if (i < q.rows) raw[i] = held_run<DT, MODE>(image, p.ldx, h, q, i, p.C);
+        if (i < q.rows) raw[i] = held_run<DT>(image, p.ldx, h, q, i, p.C);
     float w[8], b[8];
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -239,8 +239,8 @@ __global__ __launch_bounds__(held_most_threads(true)) void group_held_grad_kerne
 #pragma unroll
     for (int i = 0; i < NR; i++)
         if (i < q.rows) {
-            rx[i] = held_run<DT, MODE>(image, p.ldx, h, q, i, p.C);
-            rd[i] = held_run<DT, MODE>(image_dy, p.lddy, h, q, i, p.C);
+            rx[i] = held_run<DT>(image, p.ldx, h, q, i, p.C);
+            rd[i] = held_run<DT>(image_dy, p.lddy, h, q, i, p.C);
         }
     const Channels<G> k(p, q.n, min(q.c, p.C - 1));
     int g[G];

@@ -8,7 +8,6 @@
 namespace ss {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-struct __attribute__((packed, aligned(2))) Half16 { u32x2 v; };        // four 16-bit values
 
 template <int N> using Int = std::integral_constant<int, N>;
 
@@ -29,7 +28,7 @@ struct PwArgs {
 struct PwRowsArgs {
     const uint16_t *x;
     long long ldx;
-    unsigned mul, sh;                      // division by a row's runs, 8 Ks
+    unsigned mul, sh;                      // division by a row's runs: 8 Ks in 4 bits, 16 KB in 8
     int step_row, step_run;                // the kernel's threads over and modulo the runs
     unsigned blocks;                       // workgroups that share the rows (the others take other output channels)
     int units;                             // units of output channels of a workgroup: 64 of them with one chunk, 32 with more
