@@ -7,7 +7,7 @@
 //
 // Images of any size: a kernel finds sums of each channel over a chunk of pixels, a second joins them for each image and group, a third applies what they give.  A channel's mean and
 // sum of squared differences are found around its first value, and joined by the differences of means: no small difference of large sums.  All sums are in 32 bits, over
-// the chunks in 64, in a fixed order.  Bound by memory, three times x forward (64 x 56 x 56 x 256 in bfloat16 62 us, 4.9 TB/s), five tensors backward (115 us, 4.5 TB/s), and by three launches: one image of
+// the chunks in 64, in a fixed order.  Bound by memory, three times x forward (64 x 56 x 56 x 256 in bfloat16 57 us, 5.4 TB/s), five tensors backward (95 us, 5.4 TB/s), and by three launches: one image of
 // 64 x 64 x 320 16 and 19 us.
 #ifndef SS_GROUPNORM_KERNEL_H_
 #define SS_GROUPNORM_KERNEL_H_
