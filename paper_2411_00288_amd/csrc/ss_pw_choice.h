@@ -107,6 +107,12 @@ inline int rows_waves(const Mx4Dims &t, long long rows, long long cus)
     return t.Kq == 1 || (rows >= 128 * cus && 4 * rows_lds(t, 32) <= kPwLds) ? 4 : 8;
 }
 
+// Does an output of the kernel with rows in LDS pass the caches by?  The lines of an output larger than the last-level cache are gone from it before anyone reads them, and leave in the order of
+// their rows only if they are not kept: 96 -> 384 on 401408 rows (308 MB) 126 -> 96 us, and 66 in whole lines; of 154 MB, on 200704 rows, 46 -> 52.  (Tiles of codes: 104 -> 88, and 38 -> 44.)
+// Beside a residual, which is read 16 bytes of a pixel at a time, also a small one with a reduction of one chunk, by itself and with a layer behind it that reads it (us kept and past the caches:
+// 64 -> 64 on 200704 rows 22 and 16, on 401408 38 and 28; 64 -> 256 on 12544 7.8 and 6.0, on 200704 58 and 42; 256 -> 1024 on 12544 17 and 16; GELU, 96 -> 384 on 100352 46 and 42).
+inline bool rows_past_caches(const Mx4Dims &t, long long rows, int cout, bool residual) { return rows * cout * 2 > 256ll << 20 || (residual && t.Kq == 1); }
+
 // Does the kernel take such a layer at all?
 inline bool fits16(const Mx4Dims &t, long long rows, PwKernel k)
 {

@@ -467,9 +467,7 @@ PwArgs pw_args(const ss_weight_desc *d, int64_t rows, const void *packed, const 
     a.cout = d->cout;
     a.K = d->cin;
     a.act = act;
-    // The lines of an output larger than the last-level cache are gone from it before anyone reads them, and leave in the order of their rows only if they are not
-    // kept: 96 -> 384 on 401408 rows (308 MB) in tiles 104 -> 88 us, with rows in LDS 126 -> 96 (and 66 in whole lines); of 154 MB, on 200704 rows, 38 -> 44 and 46 -> 52.
-    a.stream = (long long)rows * d->cout * 2 > 256ll << 20;
+    a.stream = rows_past_caches(t, rows, d->cout, false);   // (the kernel with rows in LDS looks again, at the residual)
     return a;
 }
 
@@ -543,7 +541,9 @@ int product16(const PwArgs &a, const Mx4Dims &t, PwKernel kernel, const void *x,
             r.blocks = (unsigned)blocks;
             r.units = (decltype(brief)::value ? (t.Mt + 1) / 2 : t.Mt) + splits - 1;
             r.units /= splits;
-            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, rows_lds(t, 32 * NT), s, a, r);
+            PwArgs b = a;
+            b.stream = a.stream || rows_past_caches(t, a.P, a.cout, a.residual != nullptr);
+            return launch_lds<pw_mx4_rows_kernel<DT, NT, decltype(brief)::value, WIDE, THREADS>>(blocks * splits, THREADS, rows_lds(t, 32 * NT), s, b, r);
         };
         if (kernel == PW16_FEW) {
             const int waves = few16_waves(t, a.P, a.K);
