@@ -32,7 +32,7 @@ __device__ __forceinline__ void step_f8(const u32x4 (&a)[MI][2], const u32x4 (&b
 //   activation  a chunk at a time, straight from memory into one of two LDS buffers, a chunk ahead; 16-byte pieces trade places within their row so that
 //               a wave's read of 32 rows does not meet a bank twice
 // Four chunks share a scale word, whose byte the instruction picks.  A chunk of which the rows have only half is worked on by half.
-// 8192^3 in tiles of 256 x 256 417 to 460 us from box to box (2.4 to 2.6 PFLOP/s of the 4.2 that the instruction sustains alone; 13 registers are spilled behind the loop), in 128 x 128 542; 8192 -> 1024 on 12544
+// 8192^3 in tiles of 256 x 256 417 to 460 us from card to card (2.4 to 2.6 PFLOP/s of the 4.2 that the instruction sustains alone; 13 registers are spilled behind the loop), in 128 x 128 542; 8192 -> 1024 on 12544
 // rows 99 and 127; 1024 -> 1024 on 65536 83 and 76.
 template <int DT, int MI, int NI, int WM, int OUT>
 __global__ __launch_bounds__(256, MI * NI >= 16 ? 1 : 2) void pw_f8_tile_kernel(PwArgs p, int tiles_m, int tiles_n)
